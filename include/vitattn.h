@@ -390,6 +390,137 @@ int vitattn_bwd_noalloc(const void* q, const void* k, const void* v, const float
                         const float* lse, float* dq, float* dk, float* dv, int B, int H, int N, int d, float scale,
                         void* stream);
 
+/* ------------------------------------------------------------------------
+ * Operators around the attention of a block, and differential attention.
+ * ------------------------------------------------------------------------ */
+
+enum vitattn_type { VITATTN_BF16 = 0, VITATTN_FP16 = 1, VITATTN_FP32 = 2 };
+
+/*
+ * Layer norm of B*H*N rows of D elements: with mu the row's mean,
+ * r = 1/sqrt(mean((x - mu)^2) + eps) and h = (x - mu) r,
+ *
+ *     y = h w + b,
+ *     dx = r (g - mean(g) - h mean(g h)) with g = dy w,
+ *     dw = sum over the rows of dy h,  db = sum over the rows of dy.
+ *
+ * A block's norm has B = H = 1; three row dimensions let the heads of q and k
+ * be normalised where a projection left them.
+ *   x, y, dy, dx: rows at any element strides >= 0 (the D elements of a row
+ *                 contiguous, no alignment beyond the element's); all of
+ *                 `type`. y and dx must not overlap themselves. y may be x (the
+ *                 same strides); dx may be dy (the same strides), except where
+ *                 dw or db is wanted and D is above 16,384 (fp32: 8,192); any
+ *                 other output whose address range meets an input's is rejected.
+ *   w, b, dw, db: [D], contiguous, of `weight_type` (x's type or fp32). w and b
+ *                 may be null (ones, zeros); so may dw and db (not wanted).
+ *   mean, rstd  : fp32, one per row in the order [B][H][N]; the forward takes
+ *                 null for both (not wanted).
+ *   eps         : finite, >= 0.
+ *   D           : 1 .. 2^24, else VITATTN_E_UNSUPPORTED; B*H*N below 2^31 - 2^20.
+ *   workspace   : vitattn_layer_norm_bwd_workspace_bytes() bytes, 16-byte
+ *                 aligned, if dw or db is wanted (partial sums; overwritten).
+ * Sums and statistics are fp32; y and dx are rounded once, to their type. dw
+ * and db are summed in a fixed order that depends on the sizes alone (no
+ * atomics): results are bitwise reproducible. Bound by HBM bandwidth.
+ */
+int vitattn_layer_norm_fwd(const void* x, vitattn_strides sx, const void* w, const void* b, void* y,
+                           vitattn_strides sy, float* mean, float* rstd, int B, int H, int N, int D, float eps,
+                           int type, int weight_type, void* stream);
+size_t vitattn_layer_norm_bwd_workspace_bytes(int B, int H, int N, int D, int type);
+int vitattn_layer_norm_bwd(const void* x, vitattn_strides sx, const void* w, const float* mean, const float* rstd,
+                           const void* dy, vitattn_strides sdy, void* dx, vitattn_strides sdx, void* dw, void* db,
+                           int B, int H, int N, int D, int type, int weight_type, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* types of the positions of vitattn_rotary */
+enum vitattn_pos_type { VITATTN_POS_I32 = 0, VITATTN_POS_I64 = 1, VITATTN_POS_F32 = 2 };
+#define VITATTN_ROTARY_INTERLEAVED 1 /* pair p is columns 2p and 2p + 1; else p and R + p */
+#define VITATTN_ROTARY_INVERSE 2     /* turn by the opposite angles: the gradient */
+#define VITATTN_ROTARY_JOINT 4       /* one run of frequencies over the pairs of all axes */
+#define VITATTN_ROTARY_MAX_AXES 8
+#define VITATTN_ROTARY_MAX_PAIRS 128
+
+/*
+ * Rotary positions with several axes (time, height, width): pair p of a row,
+ * belonging to axis a, turns by the angle t f_p with t the row's position on
+ * that axis. Axis a has sections[a] pairs (0 is allowed), in order; R = the sum
+ * of all, and the columns from 2 R on are left as they are. Pair i of the n of
+ * an axis has the frequency base^(-i/n); with VITATTN_ROTARY_JOINT pair p of
+ * all R has base^(-p/R).
+ *   q, k     : [B][Hq][N][d] and [B][Hk][N][d] (Hk = 0: no k), of `type`, at
+ *              any element strides >= 0, the d elements of a row contiguous, no
+ *              alignment beyond the element's.
+ *   q_out, k_out: written, of the same type; they must not overlap themselves.
+ *              Each may be its input (the same strides); if both are, q and k
+ *              may be interleaved heads of one tensor. Any other output whose
+ *              address range meets an input's is rejected.
+ *   positions: [B or 1][N][n_axes] of pos_type at element strides pos_batch (0:
+ *              shared by the samples), pos_row and pos_axis.
+ *   d        : 2 R <= d <= 65,536; R <= 128, n_axes <= 8 (VITATTN_E_UNSUPPORTED
+ *              above). B and Hq + Hk up to 65,535.
+ * Angles are formed in fp64 (positions of 1e6 and more keep an fp32 sine),
+ * products in fp32, rounded once. Bound by HBM bandwidth.
+ */
+int vitattn_rotary(const void* q, vitattn_strides sq, void* q_out, vitattn_strides sq_out, int Hq, const void* k,
+                   vitattn_strides sk, void* k_out, vitattn_strides sk_out, int Hk, const void* positions,
+                   long long pos_batch, long long pos_row, long long pos_axis, int pos_type, const int* sections,
+                   int n_axes, double base, int B, int N, int d, int type, int flags, void* stream);
+
+#define VITATTN_DIFF_MAX_D 80  /* head dim of q and k */
+#define VITATTN_DIFF_MAX_E 160 /* head dim of v and o */
+
+/*
+ * Differential attention: each head takes the difference of two softmax maps
+ * over the same values. q and k hold two maps per head, heads 2h and 2h + 1:
+ *
+ *     S_m = scale Q_m K_m^T,  P_m = softmax(S_m),  O_m = P_m V,  O = O_1 - lam_h O_2
+ *
+ * and the backward pass, given dO:
+ *
+ *     dP = dO V^T,  D_m,i = sum_c dO_ic O_m,ic,
+ *     dS_1 = P_1 o (dP - D_1),  dS_2 = -lam_h P_2 o (dP - D_2),
+ *     dQ_m = scale dS_m K_m,  dK_m = scale dS_m^T Q_m,  dV = (P_1 - lam_h P_2)^T dO,
+ *     dlam_h = -sum over b, i of D_2,i.
+ *
+ *   q        : bf16 [B][2H][Nq][d];  k: bf16 [B][2H][Nk][d];  v: bf16 [B][H][Nk][e].
+ *   lam      : [H], fp32 or bf16 (lam_type), contiguous.
+ *   key_lens : null, or int32 [B]: sample b attends to its first key_lens[b]
+ *              keys (brought into 0 .. Nk); the rest are not read. A sample
+ *              without keys has O = 0, LSE = -inf and no gradients.
+ *   o        : bf16 [B][H][Nq][e], written.
+ *   maps     : fp32 [B][2H][Nq][e], dense: each map's output O_m, which the
+ *              backward reads; lse: fp32 [B][2H][Nq], dense. Either may be null
+ *              in the forward (inference). The maps are kept in fp32 since
+ *              dP - D_m cancels to a small part where values share a mean.
+ *   dq, dk, dv: bf16, the shapes of q, k and v, written (rows of keys past
+ *              key_lens are zeros); dlam: [H] of lam_type, or null.
+ *   d, e     : multiples of 8 up to VITATTN_DIFF_MAX_D and VITATTN_DIFF_MAX_E
+ *              (e = 2 d is the usual choice), else VITATTN_E_UNSUPPORTED. The
+ *              kernels compute in tiles of width 64 (d up to 64) or 96, and 64,
+ *              128 or 160 (e), columns past d and e zero.
+ *   strides  : as for vitattn_fwd_strided (2H heads for q, k, dq and dk), with
+ *              (rows + 512) * row * 2 < 2^31. Outputs must not alias inputs.
+ *   sizes    : B*H*(max(Nq, Nk) + 512) below 2^30.
+ *   workspace: at least the bytes the matching function gives (the forward's is
+ *              0 unless few queries meet many keys; then the keys are split over
+ *              workgroups whose results are joined), 16-byte aligned.
+ * Scores, statistics, sums and the difference are fp32; P and dS are rounded
+ * to bf16 as operands of the matrix cores, o and the gradients once at the end. Results are bitwise deterministic, and a head's results do not depend
+ * on the call it is part of. No atomics.
+ */
+size_t vitattn_diff_fwd_workspace_bytes(int B, int H, int Nq, int Nk, int d, int e);
+int vitattn_diff_fwd(const void* q, vitattn_strides sq, const void* k, vitattn_strides sk, const void* v,
+                     vitattn_strides sv, const void* lam, int lam_type, const int* key_lens, void* o,
+                     vitattn_strides so, float* maps, float* lse, int B, int H, int Nq, int Nk, int d, int e, float scale,
+                     void* workspace, size_t workspace_bytes, void* stream);
+size_t vitattn_diff_bwd_workspace_bytes(int B, int H, int Nq, int Nk, int d, int e);
+int vitattn_diff_bwd(const void* q, vitattn_strides sq, const void* k, vitattn_strides sk, const void* v,
+                     vitattn_strides sv, const void* lam, int lam_type, const int* key_lens, const float* maps,
+                     const float* lse, const void* dout, vitattn_strides sdo, void* dq, vitattn_strides sdq, void* dk,
+                     vitattn_strides sdk, void* dv, vitattn_strides sdv, void* dlam, int B, int H, int Nq, int Nk, int d, int e, float scale, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
 /* Human-readable name of a status code (static storage, never NULL). */
 const char* vitattn_status_str(int status);
 

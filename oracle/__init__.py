@@ -26,3 +26,4 @@ from .segments import merge, segment_backward  # noqa: F401
 from . import ulysses  # noqa: F401
 from . import aggregation  # noqa: F401
 from . import naive  # noqa: F401
+from . import block  # noqa: F401

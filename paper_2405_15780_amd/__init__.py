@@ -1,4 +1,6 @@
-"""Exact non-causal multi-head attention (forward and backward) for MI355X.
+"""Exact non-causal multi-head attention (forward and backward) for MI355X, and
+the operators of a block around it: layer norm, rotary positions with several
+axes, differential attention.
 
 A thin ctypes binding over the C ABI in include/vitattn.h; it only marshals
 arguments. Every step of the computation runs in the library's HIP kernels.
@@ -22,9 +24,14 @@ from .binding import (  # noqa: F401
     bwd_dq_from_ds,
     bwd_noalloc,
     bwd_rowdot,
+    diff_bwd,
+    diff_fwd,
     fwd,
+    layer_norm_bwd,
+    layer_norm_fwd,
     library,
     merge,
+    rotary_fwd,
     status_str,
     strides_of,
     ulysses_pack,
@@ -35,4 +42,4 @@ from .binding import (  # noqa: F401
     workspace_bytes,
     workspace_bytes_kv,
 )
-from .autograd import attention  # noqa: F401,E402
+from .autograd import attention, diff_attention, layer_norm, rotary  # noqa: F401,E402

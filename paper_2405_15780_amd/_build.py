@@ -4,11 +4,14 @@ from __future__ import annotations
 import os
 import shutil
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libvitattn.so")
-SOURCES = ["vitattn_api.hip", "vitattn_fwd.hip", "vitattn_bwd.hip", "vitattn_merge.hip", "vitattn_ulysses.hip", "vitattn_agg.hip"]
+SOURCES = ["vitattn_api.hip", "vitattn_fwd.hip", "vitattn_bwd.hip", "vitattn_merge.hip", "vitattn_ulysses.hip", "vitattn_agg.hip",
+           "vitattn_block_api.hip", "vitattn_norm.hip", "vitattn_rotary.hip", "vitattn_diff_fwd.hip", "vitattn_diff_bwd.hip"]
 ARCH = "gfx950"
 
 HIP_FLAGS = [
@@ -16,7 +19,6 @@ HIP_FLAGS = [
     "-O3",
     "-std=c++17",
     "-fPIC",
-    "-shared",
     "-Wall", "-Wextra",
     # packed fp32 VALU forms stay disabled on this target
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -39,32 +41,42 @@ def hipcc() -> str:
 LDS_POISON_LIB_PATH = os.path.join(HERE, "libvitattn_ldspoison.so")
 
 
-def _command(out: str, extra=()) -> list:
-    return [hipcc(), *HIP_FLAGS, *extra, "-o", out, *[os.path.join(CSRC, s) for s in SOURCES]]
+def _run(cmds, verbose):
+    """Runs the commands, as many at a time as there are CPUs for; raises with
+    the output of those that failed."""
+    def one(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        return cmd, subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True)
+
+    jobs = min(len(os.sched_getaffinity(0)), int(os.environ.get("MAX_JOBS", "16")))
+    with ThreadPoolExecutor(max(1, jobs)) as ex:
+        failed = [f"{c[-1]}: hipcc failed ({p.returncode}):\n{p.stdout}\n{p.stderr}" for c, p in ex.map(one, cmds)
+                  if p.returncode != 0]
+    if failed:
+        raise RuntimeError("\n".join(failed))
 
 
 def build(verbose: bool = False, lds_poison: bool = True) -> str:
     """Always recompiles; writes LIB_PATH (and, with lds_poison, the LDS-poison
-    debug variant, compiled alongside) atomically and returns LIB_PATH."""
-    jobs = [(LIB_PATH, ())]
+    debug variant, compiled alongside) atomically and returns LIB_PATH. Each
+    source is compiled on its own, side by side."""
+    libs = [(LIB_PATH, ())]
     if lds_poison:
-        jobs.append((LDS_POISON_LIB_PATH, ("-DVITATTN_DEBUG_LDS_POISON",)))
-    procs = []
-    for path, extra in jobs:
-        tmp = path + f".tmp{os.getpid()}"
-        cmd = _command(tmp, extra)
-        if verbose:
-            print(" ".join(cmd), flush=True)
-        procs.append((path, tmp, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True)))
-    failed = []
-    for path, tmp, p in procs:
-        out, err = p.communicate()
-        if p.returncode != 0:
-            failed.append(f"{os.path.basename(path)}: hipcc failed ({p.returncode}):\n{out}\n{err}")
-        else:
-            os.replace(tmp, path)
-    if failed:
-        raise RuntimeError("\n".join(failed))
+        libs.append((LDS_POISON_LIB_PATH, ("-DVITATTN_DEBUG_LDS_POISON",)))
+    with tempfile.TemporaryDirectory() as tmp:
+        compiles, links = [], []
+        for n, (path, extra) in enumerate(libs):
+            objects = [os.path.join(tmp, f"{n}_{s}.o") for s in SOURCES]
+            compiles += [[hipcc(), *HIP_FLAGS, *extra, "-c", "-o", o, os.path.join(CSRC, s)]
+                         for s, o in zip(SOURCES, objects)]
+            links.append([hipcc(), f"--offload-arch={ARCH}", "-fPIC", "-shared", "-o", path + f".tmp{os.getpid()}", *objects])
+        # the longest compilations first
+        compiles.sort(key=lambda c: -os.path.getsize(c[-1]))
+        _run(compiles, verbose)
+        _run(links, verbose)
+    for path, _ in libs:
+        os.replace(path + f".tmp{os.getpid()}", path)
     return LIB_PATH
 
 

@@ -61,6 +61,19 @@ _SIGNATURES = {
     "vitattn_ulysses_pack_out": (c_int, [c_void_p] * 2 + [c_int] * 5 + [c_void_p]),
     "vitattn_ulysses_unpack_out": (c_int, [c_void_p] * 2 + [c_int] * 5 + [c_void_p]),
     "vitattn_bwd_noalloc": (c_int, [c_void_p] * 9 + [c_int] * 4 + [c_float, c_void_p]),
+    "vitattn_layer_norm_fwd": (c_int, [c_void_p, _S] + [c_void_p] * 3 + [_S] + [c_void_p] * 2 + [c_int] * 4
+                               + [c_float, c_int, c_int, c_void_p]),
+    "vitattn_layer_norm_bwd_workspace_bytes": (c_size_t, [c_int] * 5),
+    "vitattn_layer_norm_bwd": (c_int, [c_void_p, _S] + [c_void_p] * 4 + [_S, c_void_p, _S] + [c_void_p] * 2
+                               + [c_int] * 6 + [c_void_p, c_size_t, c_void_p]),
+    "vitattn_rotary": (c_int, ([c_void_p, _S] * 2 + [c_int]) * 2 + [c_void_p] + [ctypes.c_longlong] * 3 + [c_int]
+                       + [ctypes.POINTER(c_int), c_int, ctypes.c_double] + [c_int] * 5 + [c_void_p]),
+    "vitattn_diff_fwd_workspace_bytes": (c_size_t, [c_int] * 6),
+    "vitattn_diff_fwd": (c_int, [c_void_p, _S] * 3 + [c_void_p, c_int, c_void_p] + [c_void_p, _S] + [c_void_p] * 2
+                         + [c_int] * 6 + [c_float, c_void_p, c_size_t, c_void_p]),
+    "vitattn_diff_bwd_workspace_bytes": (c_size_t, [c_int] * 6),
+    "vitattn_diff_bwd": (c_int, [c_void_p, _S] * 3 + [c_void_p, c_int] + [c_void_p] * 3
+                         + [c_void_p, _S] * 4 + [c_void_p] + [c_int] * 6 + [c_float, c_void_p, c_size_t, c_void_p]),
     "vitattn_status_str": (ctypes.c_char_p, [c_int]),
     "vitattn_version": (ctypes.c_char_p, []),
 }
@@ -525,3 +538,309 @@ def agg_bwd(q, k, v, o, lse, dout, scale=None):
                                lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), M, H, C, d,
                                _default_scale(d, scale), ws.data_ptr(), ws.numel() * 4, _stream_ptr(k)))
     return dq, dk, dv
+
+
+# ------------------------------------------------------------------ layer norm, rotary positions
+
+VITATTN_BF16, VITATTN_FP16, VITATTN_FP32 = 0, 1, 2
+VITATTN_ROTARY_INTERLEAVED, VITATTN_ROTARY_INVERSE, VITATTN_ROTARY_JOINT = 1, 2, 4
+
+
+def _type_code(t, name, allowed):
+    torch = _torch()
+    codes = {torch.bfloat16: VITATTN_BF16, torch.float16: VITATTN_FP16, torch.float32: VITATTN_FP32}
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or codes.get(t.dtype) not in allowed:
+        names = ", ".join(str(d) for d, c in codes.items() if c in allowed)
+        raise TypeError(f"{name} must be a CUDA tensor of one of {names}")
+    return codes[t.dtype]
+
+
+class _on_device:
+    """The tensor's device made current for a call (nothing if it is)."""
+
+    def __init__(self, t):
+        torch = _torch()
+        self._ctx = None if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+
+    def __enter__(self):
+        if self._ctx is not None:
+            self._ctx.__enter__()
+
+    def __exit__(self, *a):
+        if self._ctx is not None:
+            self._ctx.__exit__(*a)
+
+
+def plain_memory(t):
+    """t, or a copy where its memory does not hold its values as they are: a
+    lazily negated view, zeros without memory, a last dim that is not contiguous."""
+    if (t.shape[-1] != 1 and t.stride(-1) != 1) or t.is_neg() or (t.numel() and t.data_ptr() == 0):
+        return _torch().empty(t.shape, dtype=t.dtype, device=t.device).copy_(t)
+    return t
+
+
+def _norm_view(t, name):
+    """t as the rows of a layer norm; more than three leading dims become one (by
+    a copy where t's layout needs it)."""
+    _type_code(t, name, (VITATTN_BF16, VITATTN_FP16, VITATTN_FP32))
+    if t.dim() < 1 or (t.shape[-1] != 1 and t.stride(-1) != 1):
+        raise TypeError(f"{name} must have at least one dim, the last with unit stride")
+    return t if t.dim() <= 4 else t.reshape(-1, t.shape[-1])
+
+
+def _norm_rows(*ts):
+    """The row dimensions of tensors of one shape (up to three): the order in
+    which the first tensor's memory has them (None: one dimension, all of them
+    contiguous) and their sizes padded to three."""
+    x = ts[0]
+    if all(t.is_contiguous() for t in ts):
+        return None, (1, 1, x.numel() // x.shape[-1])
+    lead = x.dim() - 1
+    order = sorted(range(lead), key=lambda i: (-x.stride(i), i))
+    return order, (1,) * (3 - lead) + tuple(x.shape[i] for i in order)
+
+
+def _norm_strides(t, order):
+    if order is None:
+        return Strides(0, 0, t.shape[-1])
+    return Strides(*[0] * (3 - len(order)), *(0 if t.shape[i] == 1 else t.stride(i) for i in order))
+
+
+def _norm_weights(x, weight, bias):
+    torch = _torch()
+    for t, n in ((weight, "weight"), (bias, "bias")):
+        if t is not None:
+            if not isinstance(t, torch.Tensor) or t.dtype not in (x.dtype, torch.float32):
+                raise TypeError(f"{n} must be a tensor of {x.dtype} or torch.float32")
+            _expect(t, n, t.dtype, (x.shape[-1],), x.device, dense=True)
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise TypeError("weight and bias must be of one type")
+    w = weight if weight is not None else bias
+    return x.dtype if w is None else w.dtype
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, out=None, stats=True):
+    """Layer norm over the last dim of x (bf16, fp16 or fp32; any strides with
+    that dim contiguous): y like x, and the rows' mean and 1/sqrt(var + eps) in
+    fp32 (x.shape[:-1]; None, None without stats). weight and bias: [D], of x's
+    type or fp32. out: the tensor to write, may be x."""
+    torch = _torch()
+    x4 = _norm_view(x, "x")
+    code = _type_code(x, "x", (VITATTN_BF16, VITATTN_FP16, VITATTN_FP32))
+    wt = _norm_weights(x, weight, bias)
+    if x.numel() == 0:
+        raise ValueError("layer_norm needs at least one row and one column")
+    shape = tuple(x.shape)
+    if out is None:
+        y = torch.empty_like(x) if x.dim() <= 4 else torch.empty(shape, dtype=x.dtype, device=x.device)
+    else:
+        y = _expect(out, "out", x.dtype, shape, x.device, dense=x.dim() > 4)
+    y4 = y.view(x4.shape)
+    order, n = _norm_rows(x4, y4)
+    mean = rstd = None
+    if stats:
+        mean, rstd = (torch.empty(n, dtype=torch.float32, device=x.device) for _ in range(2))
+    with _on_device(x):
+        _check(library().vitattn_layer_norm_fwd(x4.data_ptr(), _norm_strides(x4, order), _ptr(weight), _ptr(bias),
+                                                y.data_ptr(), _norm_strides(y4, order), _ptr(mean), _ptr(rstd), *n,
+                                                shape[-1], eps, code, VITATTN_FP32 if wt == torch.float32 else code,
+                                                _stream_ptr(x)))
+    if stats:
+        mean, rstd = (_norm_stat_out(t, order, x4, shape) for t in (mean, rstd))
+    return y, mean, rstd
+
+
+def _norm_stat_out(t, order, x4, shape):
+    """A statistic in the kernel's order of rows, as x.shape[:-1]."""
+    if order is not None:
+        t = t.view([x4.shape[i] for i in order]).permute(sorted(range(len(order)), key=lambda i: order[i]))
+    return t.reshape(shape[:-1])
+
+
+def layer_norm_bwd(x, weight, mean, rstd, dy, want_dweight=True, want_dbias=True, bias_dtype=None, workspace=None):
+    """dx, dweight and dbias of layer_norm_fwd for the upstream gradient dy (x's
+    shape and type); dweight is None without a weight or if not wanted, dbias if
+    not wanted. Without a weight dbias has bias_dtype (default x's)."""
+    torch = _torch()
+    x4 = _norm_view(x, "x")
+    code = _type_code(x, "x", (VITATTN_BF16, VITATTN_FP16, VITATTN_FP32))
+    shape = tuple(x.shape)
+    _expect(dy, "dy", x.dtype, shape, x.device)
+    for t, n in ((mean, "mean"), (rstd, "rstd")):
+        if not (isinstance(t, torch.Tensor) and t.device == x.device and t.dtype == torch.float32
+                and tuple(t.shape) == shape[:-1]):
+            raise TypeError(f"{n} must be a torch.float32 CUDA tensor of shape {shape[:-1]} on {x.device}")
+    wt = _norm_weights(x, weight, None)
+    if weight is None and bias_dtype is not None:
+        if bias_dtype not in (x.dtype, torch.float32):
+            raise TypeError(f"bias_dtype must be {x.dtype} or torch.float32")
+        wt = bias_dtype
+    if x.numel() == 0:
+        raise ValueError("layer_norm needs at least one row and one column")
+    D = shape[-1]
+    dx = torch.empty_like(x) if x.dim() <= 4 else torch.empty(shape, dtype=x.dtype, device=x.device)
+    dy4, dx4 = _norm_view(dy, "dy"), dx.view(x4.shape)
+    order, n = _norm_rows(x4, dy4, dx4)
+    if order is not None:
+        mean, rstd = (t.reshape(x4.shape[:-1]).permute(order) for t in (mean, rstd))
+    mean, rstd = mean.contiguous(), rstd.contiguous()
+    dw = torch.empty(D, dtype=wt, device=x.device) if want_dweight and weight is not None else None
+    db = torch.empty(D, dtype=wt, device=x.device) if want_dbias else None
+    lib = library()
+    need = int(lib.vitattn_layer_norm_bwd_workspace_bytes(*n, D, code)) if dw is not None or db is not None else 0
+    if workspace is None:
+        workspace = torch.empty(max(need, 4) // 4, dtype=torch.float32, device=x.device)
+    _expect_workspace(workspace, x.device)
+    with _on_device(x):
+        _check(lib.vitattn_layer_norm_bwd(x4.data_ptr(), _norm_strides(x4, order), _ptr(weight), mean.data_ptr(),
+                                          rstd.data_ptr(), dy4.data_ptr(), _norm_strides(dy4, order), dx4.data_ptr(),
+                                          _norm_strides(dx4, order), _ptr(dw), _ptr(db), *n, D, code,
+                                          VITATTN_FP32 if wt == torch.float32 else code, workspace.data_ptr(),
+                                          workspace.numel() * workspace.element_size(), _stream_ptr(x)))
+    return dx, dw, db
+
+
+def _strides_any(t):
+    """Strides of a [B, H, N, d] view, zeros for dims of size one."""
+    return Strides(*(0 if t.shape[i] == 1 else t.stride(i) for i in range(3)))
+
+
+def rotary_fwd(q, k, positions, sections, base=10000.0, interleaved=False, joint=False, inverse=False, out=None):
+    """q [B,Hq,N,d] and k [B,Hk,N,d] (or None) with pairs of columns turned by
+    their positions: sections[a] pairs for axis a, positions [N, A] or [B, N, A]
+    (int32, int64 or fp32). Pair p is columns p and R + p of the first 2 R (2p and
+    2p + 1 if interleaved); frequencies base^(-i/n) over an axis's n pairs, or
+    over all R (joint). inverse turns back: the gradient. out=(q', k') to write
+    into, which may be q and k. Returns q', or (q', k') if there is a k."""
+    torch = _torch()
+    code = _type_code(q, "q", (VITATTN_BF16, VITATTN_FP16, VITATTN_FP32))
+    for t, n in ((q, "q"), (k, "k")):
+        if t is not None and not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == q.dtype and t.dim() == 4
+                                  and t.device == q.device and (t.shape[3] == 1 or t.stride(3) == 1)):
+            raise TypeError(f"{n} must be a 4-D CUDA tensor [B, H, N, d] of q's type and device with unit stride along d")
+    B, Hq, N, d = q.shape
+    if k is not None and (k.shape[0], k.shape[2], k.shape[3]) != (B, N, d):
+        raise ValueError("k must be [B, Hk, N, d] with the B, N and d of q")
+    sections = tuple(int(s) for s in sections)
+    A = len(sections)
+    codes = {torch.int32: 0, torch.int64: 1, torch.float32: 2}
+    if not (isinstance(positions, torch.Tensor) and positions.device == q.device and positions.dtype in codes
+            and tuple(positions.shape) in ((N, A), (B, N, A))):
+        raise TypeError(f"positions must be an int32, int64 or float32 tensor [{N}, {A}] or [{B}, {N}, {A}] on {q.device}")
+    if out is None:
+        q_out, k_out = torch.empty_like(q), None if k is None else torch.empty_like(k)
+    else:
+        q_out, k_out = out if k is not None else ((out[0] if isinstance(out, (tuple, list)) else out), None)
+        for t, like, n in ((q_out, q, "out q"), (k_out, k, "out k")):
+            if like is not None:
+                _expect(t, n, q.dtype, like.shape, q.device)
+    pb = positions.stride(0) if positions.dim() == 3 else 0
+    flags = ((VITATTN_ROTARY_INTERLEAVED if interleaved else 0) | (VITATTN_ROTARY_INVERSE if inverse else 0)
+             | (VITATTN_ROTARY_JOINT if joint else 0))
+    zero = Strides(0, 0, 0)
+    with _on_device(q):
+        _check(library().vitattn_rotary(
+            q.data_ptr(), _strides_any(q), q_out.data_ptr(), _strides_any(q_out), Hq, _ptr(k),
+            zero if k is None else _strides_any(k), _ptr(k_out), zero if k is None else _strides_any(k_out),
+            0 if k is None else k.shape[1], positions.data_ptr(), pb, positions.stride(-2), positions.stride(-1),
+            codes[positions.dtype], (c_int * max(A, 1))(*sections), A, float(base), B, N, d, code, flags,
+            _stream_ptr(q)))
+    return q_out if k is None else (q_out, k_out)
+
+
+# ------------------------------------------------------------------ differential attention
+
+
+def _diff_strides(t):
+    """Strides of a [B, H, N, d] view as the attention takes them; those of dims
+    of size one do not matter and are replaced."""
+    return Strides(0 if t.shape[0] == 1 else t.stride(0), 0 if t.shape[1] == 1 else t.stride(1),
+                   t.shape[3] if t.shape[2] == 1 else t.stride(2))
+
+
+def _diff_args(q, k, v, lam, key_lens):
+    torch = _torch()
+    _as_input(q, "q")
+    for t, n in ((k, "k"), (v, "v")):
+        _as_input(t, n, q.device)
+    B, H2, Nq, d = q.shape
+    H, Nk, e = v.shape[1:]
+    if H2 != 2 * H or tuple(k.shape) != (B, H2, Nk, d) or v.shape[0] != B:
+        raise ValueError("q must be [B, 2H, Nq, d], k [B, 2H, Nk, d] and v [B, H, Nk, e]")
+    lam_code = _type_code(lam, "lam", (VITATTN_BF16, VITATTN_FP32))
+    _expect(lam, "lam", lam.dtype, (H,), q.device, dense=True)
+    if key_lens is not None:
+        _expect(key_lens, "key_lens", torch.int32, (B,), q.device, dense=True)
+    return (B, H, Nq, Nk, d, e), lam_code
+
+
+def _like_layout(t, shape):
+    """A new tensor [B, H, N, e] in t's order of heads and rows."""
+    torch = _torch()
+    B, H, N, e = shape
+    if t.shape[1] > 1 and t.shape[2] > 1 and t.stride(1) < t.stride(2):
+        return torch.empty((B, N, H, e), dtype=t.dtype, device=t.device).transpose(1, 2)
+    return torch.empty(shape, dtype=t.dtype, device=t.device)
+
+
+def _diff_workspace(workspace, need, device):
+    torch = _torch()
+    if workspace is None:
+        workspace = torch.empty(max(need, 4) // 4, dtype=torch.float32, device=device)
+    return _expect_workspace(workspace, device)
+
+
+def diff_fwd(q, k, v, lam, scale=None, key_lens=None, out=None, save=True, workspace=None):
+    """Differential attention: o (bf16 [B,H,Nq,e], in q's order of heads and rows)
+    = softmax(scale Q1 K1^T) V - lam softmax(scale Q2 K2^T) V for q [B,2H,Nq,d], k
+    [B,2H,Nk,d] (heads 2h and 2h + 1 are the two maps of head h), v [B,H,Nk,e] and
+    lam [H] (fp32 or bf16). key_lens: int32 [B], sample b attends to its first
+    key_lens[b] keys. Returns o and what diff_bwd needs: o2 (fp32 [B,2H,Nq,e], each
+    map's output before the difference) and lse (fp32 [B,2H,Nq]); None, None
+    unless save."""
+    torch = _torch()
+    sizes, lam_code = _diff_args(q, k, v, lam, key_lens)
+    B, H, Nq, Nk, d, e = sizes
+    o = _like_layout(q, (B, H, Nq, e)) if out is None else _expect(out, "out", torch.bfloat16, (B, H, Nq, e), q.device)
+    o2 = lse = None
+    if save:
+        o2 = torch.empty((B, 2 * H, Nq, e), dtype=torch.float32, device=q.device)
+        lse = torch.empty((B, 2 * H, Nq), dtype=torch.float32, device=q.device)
+    lib = library()
+    need = int(lib.vitattn_diff_fwd_workspace_bytes(*sizes))
+    ws = _diff_workspace(workspace, need, q.device) if need or workspace is not None else None
+    with _on_device(q):
+        _check(lib.vitattn_diff_fwd(q.data_ptr(), _diff_strides(q), k.data_ptr(), _diff_strides(k), v.data_ptr(),
+                                    _diff_strides(v), lam.data_ptr(), lam_code, _ptr(key_lens), o.data_ptr(),
+                                    _diff_strides(o), _ptr(o2), _ptr(lse), *sizes, _default_scale(d, scale), _ptr(ws),
+                                    0 if ws is None else ws.numel() * ws.element_size(), _stream_ptr(q)))
+    return o, o2, lse
+
+
+def diff_bwd(q, k, v, lam, o, o2, lse, dout, scale=None, key_lens=None, want_dlam=True, workspace=None):
+    """dq, dk, dv (bf16, like q, k and v) and dlam (lam's type, or None) of
+    diff_fwd for the upstream gradient dout (bf16 [B,H,Nq,e]). The kernels read
+    the unrounded outputs in o2; o is checked to belong to the same call's sizes."""
+    torch = _torch()
+    sizes, lam_code = _diff_args(q, k, v, lam, key_lens)
+    B, H, Nq, Nk, d, e = sizes
+    _expect(o, "o", torch.bfloat16, (B, H, Nq, e), q.device)
+    _expect(o2, "o2", torch.float32, (B, 2 * H, Nq, e), q.device, dense=True)
+    _expect(lse, "lse", torch.float32, (B, 2 * H, Nq), q.device, dense=True)
+    _expect(dout, "dout", torch.bfloat16, (B, H, Nq, e), q.device)
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    dlam = torch.empty_like(lam) if want_dlam else None
+    lib = library()
+    ws = _diff_workspace(workspace, int(lib.vitattn_diff_bwd_workspace_bytes(*sizes)), q.device)
+    with _on_device(q):
+        _check(lib.vitattn_diff_bwd(q.data_ptr(), _diff_strides(q), k.data_ptr(), _diff_strides(k), v.data_ptr(),
+                                    _diff_strides(v), lam.data_ptr(), lam_code, _ptr(key_lens), o2.data_ptr(),
+                                    lse.data_ptr(), dout.data_ptr(), _diff_strides(dout), dq.data_ptr(), _diff_strides(dq), dk.data_ptr(),
+                                    _diff_strides(dk), dv.data_ptr(), _diff_strides(dv), _ptr(dlam), *sizes,
+                                    _default_scale(d, scale), ws.data_ptr(), ws.numel() * ws.element_size(),
+                                    _stream_ptr(q)))
+    return dq, dk, dv, dlam

@@ -9,13 +9,14 @@
 #include <mutex>
 
 #include "../../include/vitattn.h"
+#include "vitattn_check.h"
 #include "vitattn_launch.h"
 
 #define VITATTN_VERSION "0.3.0"
 
 namespace {
 
-bool aligned16(const void* p) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+using namespace vitattn_check;
 
 // head dims of the attention kernels: multiples of 8 (16-byte rows) up to 160
 bool head_dim_ok(int d) { return d >= 8 && d <= 160 && d % 8 == 0; }
@@ -36,8 +37,6 @@ int check_sizes(int B, int H, int N, int d) {
   return check_rows(B, H, N, d);
 }
 
-bool scale_ok(float s) { return isfinite(s) && s > 0.f; }
-
 // Every launch must stay below 2^32 work-items (a dispatch's grid size is
 // 32-bit; a larger one would fail at launch, after the call's earlier
 // kernels had run). The forward and dQ kernels run 2 per query row plus the
@@ -47,7 +46,6 @@ bool scale_ok(float s) { return isfinite(s) && s > 0.f; }
 // each), the row-dot pass 8, 16 or 32 per row (head dims up to 64, 128,
 // 160) and the merge d/4 per row. These bounds bind only at head dims of 16
 // or less; wider rows run out of memory first.
-constexpr long long kMaxWorkItems = 1LL << 32;
 bool fwd_items_ok(int B, int H, int Nq) { return 2LL * B * H * (Nq + 383LL) < kMaxWorkItems; }
 bool bwd_items_ok(int B, int H, int Nq, int Nk, int d) {
   const long long bh = (long long)B * H, lpr = d <= 64 ? 8 : d <= 128 ? 16 : 32;
@@ -62,42 +60,6 @@ int check_sizes_kv(int B, int H, int Nq, int Nk, int d) {
   return st != VITATTN_OK ? st : check_sizes(B, H, Nk, d);
 }
 
-// One operand's strides (elements). Rows must be 16-byte aligned and must not
-// overlap (row >= d); every stride is non-negative and a multiple of
-// 16 / elem_bytes elements. Operands read through buffer resources (the bf16
-// inputs) must keep (N + 256) rows within 31-bit byte offsets. An output must
-// not overlap itself: sorted by stride, each dimension must step past the
-// span of the smaller ones. Inputs may repeat heads or batches (stride 0).
-int check_map(const vitattn_strides& m, int B, int H, int N, int d, int elem_bytes, bool output) {
-  const long long unit = 16 / elem_bytes;
-  if (m.batch < 0 || m.head < 0 || m.row < d) return VITATTN_E_INVAL;
-  if (m.batch % unit != 0 || m.head % unit != 0 || m.row % unit != 0) return VITATTN_E_INVAL;
-  if (m.row > 0x7fffffffLL) return VITATTN_E_INVAL;
-  if (elem_bytes == 2 && (long long)(N + 256) * m.row * 2 > 0x7fffffffLL) return VITATTN_E_INVAL;
-  // the largest element offset must fit comfortably in 64 bits
-  if ((double)(B - 1) * m.batch + (double)(H - 1) * m.head + (double)N * m.row > 4.0e18) return VITATTN_E_INVAL;
-  if (output) {
-    long long size[3] = {B, H, N}, stride[3] = {m.batch, m.head, m.row};
-    int idx[3] = {0, 1, 2};
-    for (int i = 0; i < 3; ++i)  // sort the three dimensions by stride
-      for (int j = i + 1; j < 3; ++j)
-        if (stride[idx[j]] < stride[idx[i]]) {
-          const int t = idx[i];
-          idx[i] = idx[j];
-          idx[j] = t;
-        }
-    long long span = d;  // elements covered by the dimensions taken so far (a row first)
-    for (int i = 0; i < 3; ++i) {
-      const int x = idx[i];
-      if (size[x] == 1) continue;
-      if (stride[x] < span) return VITATTN_E_INVAL;
-      span += (size[x] - 1) * stride[x];
-    }
-  }
-  return VITATTN_OK;
-}
-
-vitattn::Map to_map(const vitattn_strides& m) { return vitattn::Map{m.batch, m.head, (int)m.row}; }
 vitattn_strides dense(int H, int N, int d) {
   vitattn_strides m;
   m.batch = (long long)H * N * d;

@@ -1,0 +1,434 @@
+// Forward pass of differential attention for gfx950. Per (b, h), over the
+// first key_lens[b] keys:
+//
+//   O_m = softmax(scale Q_m K_m^T) V  (m = 1, 2),   O = O_1 - lam O_2
+//
+// Two softmaxes with statistics of their own over one V: each map is an online
+// softmax (running max and sum) as in vitattn_fwd.hip, and the difference is
+// taken in fp32 at the end. A workgroup of 2 QW waves owns 32 QW queries of
+// one (b, h); waves w and w + QW share 32 of them and take one map each, so
+// the tiles of V (and both maps' K) are fetched once for the two maps and both
+// land on the same SIMD (QW = 4), where one wave's exponentials run beside the
+// other's matrix ops. K_1, K_2 and V stream through LDS in tiles of 32 KB keys
+// (two slots each, K one tile ahead of V), rows past the sample's keys read
+// as zeros. The pipeline within a tile is vitattn_fwd.hip's: one stream of
+// score ops (tile j + 1) then PV ops (tile j), operands read two ops ahead,
+// exponentials, tile requests and the next maximum spread over it.
+//
+// P is rounded to bf16 as the matrix cores' operand (its sum is of the fp32
+// values); scores, statistics, sums and the difference are fp32; o is rounded
+// once, at the end. What the backward needs is kept in fp32: it subtracts dO .
+// O_m from every dP, and where values share a mean these cancel to a small part
+// (kept in bf16, dQ was 1.1 % off at 32,768 keys).
+//
+// Few queries over many keys (SPLIT): the grid also splits the keys, each
+// workgroup writes its maps' normalised outputs and LSE to the workspace, and
+// a second kernel joins them, O_m = sum_s exp(LSE_s - LSE) O_s. The split
+// depends on Nq and Nk alone, so a head's bits do not depend on the call it is
+// part of.
+#include "vitattn_diff.h"
+
+namespace vitattn {
+
+namespace {
+
+// see vitattn_fwd.hip: score e of 16*KB per lane is exponentiated in slot
+// e*W/(16*KB), two slots before the PV op that reads it
+constexpr bool exp_fits(int NS, int CPB, int KB, int W) {
+  for (int t = 0; t < 2 * KB; ++t)
+    if ((8 * t + 7) * W / (16 * KB) > NS + CPB * t - 2) return false;
+  return true;
+}
+constexpr int exp_window(int NS, int CPB, int KB, int NOPS) {
+  int w = NOPS - 5;
+  while (w > 1 && !exp_fits(NS, CPB, KB, w)) --w;
+  return w;
+}
+
+template <int DQ, int QS, int DV, int KB, int QW, bool SPLIT>
+__global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a, int n_qtiles, int n_split,
+                                                               int split_keys, int total, float c) {
+  constexpr int NW = 2 * QW;
+  constexpr int BM = 32 * QW, BN = 32 * KB;
+  constexpr int KT = BN * DQ * 2, VT = BN * DV * 2;  // bytes of a K and a V tile
+  constexpr int NS = KB * QS;                        // score ops per tile
+  constexpr int CPB = DV / 32;                       // PV ops per 16-key step
+  constexpr int NV = 2 * KB * CPB;                   // PV ops per tile
+  __shared__ __attribute__((aligned(1024))) char kbuf0[2 * KT];  // K_1, then K_2
+  __shared__ __attribute__((aligned(1024))) char kbuf1[2 * KT];
+  __shared__ __attribute__((aligned(1024))) char vbuf0[VT];
+  __shared__ __attribute__((aligned(1024))) char vbuf1[VT];
+  __shared__ float xbuf[QW][16][64];  // the second map's outputs, 32 columns at a time
+  char* const kbuf[2] = {kbuf0, kbuf1};
+  char* const vbuf[2] = {vbuf0, vbuf1};
+  debug_poison_lds(kbuf0, kbuf1, vbuf0, vbuf1, xbuf);
+
+  const int work = xcd_remap(blockIdx.x, total);
+  const int part = work / n_qtiles;
+  const int qt = work - part * n_qtiles;
+  const int bh = SPLIT ? part / n_split : part;
+  const int sp = SPLIT ? part - bh * n_split : 0;
+  const int b = bh / a.H, head = bh - b * a.H;
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int qw = wave % QW, map = wave / QW;
+  const int qrow = qt * BM + qw * 32 + (lane & 31);
+
+  // this workgroup's keys: [key_first, key_first + Nk)
+  const int all = keys_of(a.key_lens, b, a.Nk);
+  const int key_first = SPLIT ? min(sp * split_keys, all) : 0;
+  const int Nk = SPLIT ? min(all - key_first, split_keys) : all;
+  // SPLIT: rows of the workspace, [bh][split][map][query] of DV columns (a.e
+  // of them used), then as many LSE
+  const long long wrow = SPLIT ? (((long long)bh * n_split + sp) * 2 + map) * a.Nq + qrow : 0;
+  float* const wo = a.work + wrow * a.e;
+  float* const wl = a.work + (long long)a.B * a.H * n_split * 2 * a.Nq * a.e + wrow;
+  uint16_t* const orow = a.o + b * a.mo.sb + head * a.mo.sh + (long long)qrow * a.mo.ld;
+  float* const mrow = a.maps ? a.maps + (((long long)bh * 2 + map) * a.Nq + qrow) * a.e : nullptr;
+  float* const lrow = a.lse ? a.lse + ((long long)bh * 2 + map) * a.Nq + qrow : nullptr;
+
+  if (Nk == 0) {  // the whole workgroup: nothing to attend to, the output is zero
+    if (qrow < a.Nq) {
+      if (!SPLIT)
+        for (int col = 4 * h; col < a.e; col += 8) {
+          if (map == 0) put4_bf16(orow + col, 0.f, 0.f, 0.f, 0.f);
+          if (mrow) *reinterpret_cast<float4*>(mrow + col) = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+      if (h == 0) {
+        if (SPLIT) *wl = -INFINITY;  // its outputs are not read
+        else if (lrow) *lrow = -INFINITY;
+      }
+    }
+    return;
+  }
+
+  const int chr = a.d >> 3, chv = a.e >> 3;  // 16-byte chunks of a row that hold data
+  const int ldq = 2 * a.mq.ld, ldk = 2 * a.mk.ld, ldv = 2 * a.mv.ld;
+  const rsrc_t rq = make_rsrc(a.q + map_head(a.mq, b, head, map), (unsigned)(a.Nq * ldq));
+  const rsrc_t rk1 = make_rsrc(a.k + map_head(a.mk, b, head, 0) + (long long)key_first * a.mk.ld, (unsigned)(Nk * ldk));
+  const rsrc_t rk2 = make_rsrc(a.k + map_head(a.mk, b, head, 1) + (long long)key_first * a.mk.ld, (unsigned)(Nk * ldk));
+  const rsrc_t rv = make_rsrc(a.v + b * a.mv.sb + head * a.mv.sh + (long long)key_first * a.mv.ld, (unsigned)(Nk * ldv));
+
+  bf16x8 qf[QS];  // B operands of K Q^T
+#pragma unroll
+  for (int kk = 0; kk < QS; ++kk) qf[kk] = as_bf16x8(buffer_load16(rq, chunk_offset(qrow, 2 * kk + h, ldq, chr)));
+
+  TileDma<DQ, BN, NW> dma;
+  TileDma<DV, BN, NW> dmv;
+  dma.init(wave, lane, ldk, chr);
+  dmv.init(wave, lane, ldv, chv);
+  RowFrag<DQ> kfrag;
+  kfrag.init(lane);
+  TrFrag<DV> vfrag;
+  vfrag.init(lane);
+  // a tile's requests: K_1, K_2 (tile j + 2), V (tile j + 1)
+  constexpr int PK = decltype(dma)::PER_WAVE, PV = decltype(dmv)::PER_WAVE, NDMA = 2 * PK + PV;
+
+  f32x16 oacc[CPB];
+#pragma unroll
+  for (int cb = 0; cb < CPB; ++cb) oacc[cb] = zero16();
+  float m_run = -INFINITY;  // running max of scaled logits, log2 units
+  float l_part = 0.f;
+
+  const int n_kt = (Nk + BN - 1) / BN;
+  dma.issue(rk1, 0, ldk, kbuf[0]);
+  dma.issue(rk2, 0, ldk, kbuf[0] + KT);
+  dmv.issue(rv, 0, ldv, vbuf[0]);
+  dma.issue(rk1, BN, ldk, kbuf[1]);
+  dma.issue(rk2, BN, ldk, kbuf[1] + KT);
+  wait_vmem();
+  __syncthreads();
+
+  constexpr int NE = 16 * KB;
+  auto mask_ragged = [&](f32x16 (&s)[KB], int tile) {
+    const int key0 = tile * BN;
+    if (key0 + BN > Nk) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (key0 + kb * 32 + acc_row(r, h) >= Nk) s[kb][r] = -INFINITY;
+    }
+  };
+  auto max_quarter = [&](const f32x16 (&s)[KB], int q) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int e = q * NE / 4; e < (q + 1) * NE / 4; ++e) m = fmaxf(m, s[e / 16][e % 16]);
+    return m;
+  };
+  auto fold_max = [&](float mx) __attribute__((always_inline)) {
+    if (__any(mx * c > m_run)) {
+      const float m_new = fmaxf(m_run, max_halves(mx) * c);
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_part *= alpha;
+#pragma unroll
+      for (int cb = 0; cb < CPB; ++cb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[cb][r] *= alpha;
+    }
+  };
+
+  f32x16 sa[KB], sb[KB];
+  const int koff = map * KT;
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    if (i % QS == 0) sa[i / QS] = zero16();
+    sa[i / QS] = mfma32(lds_frag_row(kbuf[0] + koff, (i / QS) * 32 * 2 * DQ + kfrag.at(i % QS)), qf[i % QS], sa[i / QS]);
+  }
+  if (n_kt == 1) mask_ragged(sa, 0);
+  m_run = max_halves(fmaxf(fmaxf(max_quarter(sa, 0), max_quarter(sa, 1)), fmaxf(max_quarter(sa, 2), max_quarter(sa, 3)))) * c;
+  __syncthreads();  // kbuf[0] is refilled by the first stage
+
+  auto stage = [&](auto parity, auto has_next, f32x16 (&s)[KB], f32x16 (&sn)[KB], int j) {
+    constexpr int P = decltype(parity)::value;
+    constexpr bool NEXT = decltype(has_next)::value;
+    const char* ks = kbuf[1 - P] + koff;
+    const char* vs = vbuf[P];
+    const float m_cur = m_run;
+    float ls0 = 0.f, ls1 = 0.f;
+    u32x4 pq[2 * KB];
+    float xe[NE];
+    auto exp_slice = [&](auto I, auto WC) __attribute__((always_inline)) {
+      constexpr int i = decltype(I)::value;
+      constexpr int W = decltype(WC)::value;
+      static_for<0, NE>([&](auto EC) __attribute__((always_inline)) {
+        constexpr int e = decltype(EC)::value;
+        if constexpr (e * W / NE == i) {
+          xe[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e / 16][e % 16], c, -m_cur));
+          if constexpr ((e & 1) != 0) {
+            const bf16x2 pr2 = {(__bf16)xe[e - 1], (__bf16)xe[e]};
+            ls0 += xe[e - 1];
+            ls1 += xe[e];
+            pin(ls0);
+            pin(ls1);
+            constexpr int pr = e / 2;
+            pq[pr / 4][pr % 4] = __builtin_bit_cast(uint32_t, pr2);
+          }
+        }
+      });
+    };
+    auto pfrag = [&](int t) { return __builtin_bit_cast(bf16x8, pq[t]); };
+
+    if constexpr (NEXT) {
+      constexpr int NOPS = NS + NV;
+      constexpr int W = exp_window(NS, CPB, KB, NOPS);
+      static_assert(exp_fits(NS, CPB, KB, W), "probabilities must be ready before their PV op");
+      // requests on the odd ops where they fit there, else on every op
+      constexpr int STEP = 2 * NDMA <= NOPS ? 2 : 1;
+      static_assert(STEP * NDMA <= NOPS, "tile requests must fit the stream");
+      auto load_op = [&](int i) -> bf16x8 {
+        if (i < NS) return lds_frag_row(ks, (i % KB) * 32 * 2 * DQ + kfrag.at(i / KB));
+        const int t = i - NS;
+        return vfrag.load(vs, 16 * (t / CPB), t % CPB);
+      };
+      float mq[4];
+      bf16x8 opq[3];
+      opq[0] = load_op(0);
+      opq[1] = load_op(1);
+      sched_fence();
+      static_for<0, NOPS>([&](auto IC) __attribute__((always_inline)) {
+        constexpr int i = decltype(IC)::value;
+        if constexpr (i == 0) __builtin_amdgcn_s_setprio(2);
+        if constexpr (i == W) __builtin_amdgcn_s_setprio(1);
+        if constexpr (i == W + 4) __builtin_amdgcn_s_setprio(0);
+        if constexpr (i + 2 < NOPS) opq[(i + 2) % 3] = load_op(i + 2);
+        if constexpr (i < NS) {
+          if constexpr (i / KB == 0) sn[i % KB] = zero16();
+          sn[i % KB] = mfma32(opq[i % 3], qf[i / KB], sn[i % KB]);
+        } else {
+          constexpr int t = i - NS;
+          oacc[t % CPB] = mfma32(opq[i % 3], pfrag(t / CPB), oacc[t % CPB]);
+        }
+        if constexpr (i % STEP == STEP - 1 && i / STEP < NDMA) {
+          constexpr int q = i / STEP;
+          if constexpr (q < PK) dma.issue_one(rk1, (j + 2) * BN, ldk, kbuf[P], q);
+          else if constexpr (q < 2 * PK) dma.issue_one(rk2, (j + 2) * BN, ldk, kbuf[P] + KT, q - PK);
+          else dmv.issue_one(rv, (j + 1) * BN, ldv, vbuf[1 - P], q - 2 * PK);
+        }
+        exp_slice(IC, std::integral_constant<int, W>{});
+        if constexpr (i >= W && i < W + 4) {
+          if constexpr (i == W) mask_ragged(sn, j + 1);
+          mq[i - W] = max_quarter(sn, i - W);
+          pin(mq[i - W]);
+        }
+        sched_fence();
+      });
+      l_part += ls0 + ls1;
+      fold_max(fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])));
+      wait_vmem();
+      __syncthreads();
+    } else {
+      exp_slice(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
+      bf16x8 vq[3];
+      vq[0] = vfrag.load(vs, 0, 0);
+      vq[1] = vfrag.load(vs, 16 * (1 / CPB), 1 % CPB);
+      sched_fence();
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        if (i + 2 < NV) vq[(i + 2) % 3] = vfrag.load(vs, 16 * ((i + 2) / CPB), (i + 2) % CPB);
+        oacc[i % CPB] = mfma32(vq[i % 3], pfrag(i / CPB), oacc[i % CPB]);
+        sched_fence();
+      }
+      l_part += ls0 + ls1;
+    }
+  };
+
+  using P0 = std::integral_constant<int, 0>;
+  using P1 = std::integral_constant<int, 1>;
+  int j = 0;
+  for (; j + 2 < n_kt; j += 2) {
+    stage(P0{}, std::true_type{}, sa, sb, j);
+    stage(P1{}, std::true_type{}, sb, sa, j + 1);
+  }
+  if (j + 1 < n_kt) {
+    stage(P0{}, std::true_type{}, sa, sb, j);
+    stage(P1{}, std::false_type{}, sb, sa, j + 1);
+  } else {
+    stage(P0{}, std::false_type{}, sa, sb, j);
+  }
+
+  const float l = sum_halves(l_part);
+  const float inv = 1.0f / l;
+  const float lse = (m_run + __log2f(l)) * kLn2;
+  if constexpr (SPLIT) {
+    if (qrow < a.Nq) {
+#pragma unroll
+      for (int cb = 0; cb < CPB; ++cb)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int col = 32 * cb + 8 * g + 4 * h;
+          if (col < a.e)
+            *reinterpret_cast<float4*>(wo + col) = make_float4(oacc[cb][4 * g] * inv, oacc[cb][4 * g + 1] * inv,
+                                                               oacc[cb][4 * g + 2] * inv, oacc[cb][4 * g + 3] * inv);
+        }
+      if (h == 0) *wl = lse;
+    }
+  } else {
+    // the second map's wave hands its outputs over, 32 columns at a time
+    const float lam = lam_of(a.lam, a.lam_bf16, head);
+#pragma unroll
+    for (int cb = 0; cb < CPB; ++cb) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[cb][r] *= inv;
+      if (map == 1) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) xbuf[qw][r][lane] = oacc[cb][r];
+      }
+      if (mrow && qrow < a.Nq) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int col = 32 * cb + 8 * g + 4 * h;
+          if (col < a.e)
+            *reinterpret_cast<float4*>(mrow + col) =
+                make_float4(oacc[cb][4 * g], oacc[cb][4 * g + 1], oacc[cb][4 * g + 2], oacc[cb][4 * g + 3]);
+        }
+      }
+      __syncthreads();
+      if (map == 0 && qrow < a.Nq) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int col = 32 * cb + 8 * g + 4 * h;
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = oacc[cb][4 * g + e] - lam * xbuf[qw][4 * g + e][lane];
+          if (col < a.e) put4_bf16(orow + col, x[0], x[1], x[2], x[3]);
+        }
+      }
+      __syncthreads();
+    }
+    if (lrow && qrow < a.Nq && h == 0) *lrow = lse;
+  }
+}
+
+// Joins the splits of one query row: a wave per row (bh, query). Lane s of the
+// first pass weighs split s; the outputs are then added in split order.
+__global__ __launch_bounds__(256) void diff_join_kernel(const DiffArgs a, int n_split) {
+  const long long rows = (long long)a.B * a.H * a.Nq;
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= rows) return;
+  const int lane = threadIdx.x & 63;
+  const long long bh = row / a.Nq;
+  const int i = (int)(row - bh * a.Nq);
+  const int b = (int)(bh / a.H), head = (int)(bh - (long long)b * a.H);
+  const float* lses = a.work + rows * n_split * 2 * a.e;
+  float acc[2][3];  // columns lane, lane + 64, lane + 128
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    const long long base = (bh * n_split * 2 + m) * a.Nq + i, step = 2LL * a.Nq;
+    float top = -INFINITY, sum = 0.f;
+    for (int s = lane; s < n_split; s += 64) top = fmaxf(top, lses[base + s * step]);
+#pragma unroll
+    for (int x = 32; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+    const float ref = top == -INFINITY ? 0.f : top;  // no keys at all
+    for (int s = lane; s < n_split; s += 64) sum += expf(lses[base + s * step] - ref);
+#pragma unroll
+    for (int x = 32; x >= 1; x >>= 1) sum += __shfl_xor(sum, x, 64);
+    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+    if (lane == 0 && a.lse) a.lse[(bh * 2 + m) * a.Nq + i] = top == -INFINITY ? -INFINITY : ref + logf(sum);
+#pragma unroll
+    for (int t = 0; t < 3; ++t) acc[m][t] = 0.f;
+    for (int s = 0; s < n_split; ++s) {
+      const float l = lses[base + s * step];
+      if (l == -INFINITY) continue;  // an empty split wrote no outputs
+      const float w = expf(l - ref) * inv;
+      const float* src = a.work + (base + s * step) * a.e;
+#pragma unroll
+      for (int t = 0; t < 3; ++t)
+        if (lane + 64 * t < a.e) acc[m][t] += w * src[lane + 64 * t];
+    }
+  }
+  const float lam = lam_of(a.lam, a.lam_bf16, head);
+  uint16_t* o = a.o + b * a.mo.sb + head * a.mo.sh + (long long)i * a.mo.ld;
+#pragma unroll
+  for (int t = 0; t < 3; ++t) {
+    const int col = lane + 64 * t;
+    if (col >= a.e) continue;
+    o[col] = __builtin_bit_cast(uint16_t, (__bf16)(acc[0][t] - lam * acc[1][t]));
+    if (a.maps)
+#pragma unroll
+      for (int m = 0; m < 2; ++m) a.maps[((bh * 2 + m) * a.Nq + i) * a.e + col] = acc[m][t];
+  }
+}
+
+template <int DQ, int QS, int DV, int KB, int QW, bool SPLIT>
+hipError_t go(const DiffArgs& a, int split_keys, int n_split) {
+  const int n_qtiles = (a.Nq + 32 * QW - 1) / (32 * QW);
+  const int total = a.B * a.H * n_split * n_qtiles;
+  diff_fwd_kernel<DQ, QS, DV, KB, QW, SPLIT>
+      <<<total, 128 * QW, 0, a.stream>>>(a, n_qtiles, n_split, split_keys, total, a.scale * kLog2e);
+  return hipGetLastError();
+}
+
+template <int DQ, int QS, int DV, int KB>
+hipError_t go_tile(const DiffArgs& a) {
+  const int split_keys = diff_split_keys(a.Nq, a.Nk);
+  if (split_keys == 0) return a.Nq <= 64 ? go<DQ, QS, DV, KB, 2, false>(a, 0, 1) : go<DQ, QS, DV, KB, 4, false>(a, 0, 1);
+  const int n_split = (a.Nk + split_keys - 1) / split_keys;
+  const hipError_t err = go<DQ, QS, DV, KB, 2, true>(a, split_keys, n_split);
+  if (err != hipSuccess) return err;
+  const long long rows = (long long)a.B * a.H * a.Nq;
+  diff_join_kernel<<<(unsigned)((rows + 3) / 4), 256, 0, a.stream>>>(a, n_split);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int diff_split_keys(int Nq, int Nk) {
+  if (Nq > 64 || Nk < 1024) return 0;
+  return 512;
+}
+
+size_t diff_fwd_workspace_floats(int B, int H, int Nq, int Nk, int e) {
+  const int s = diff_split_keys(Nq, Nk);
+  return s ? (size_t)B * H * ((Nk + s - 1) / s) * 2 * Nq * (e + 1) : 0;
+}
+
+hipError_t launch_diff_fwd(const DiffArgs& a) {
+  const DiffTile t = diff_tile(a.d, a.e);
+  if (t.dq == 96) return go_tile<96, 5, 160, 1>(a);
+  if (t.dv == 128) return go_tile<64, 4, 128, 2>(a);
+  return t.qs == 2 ? go_tile<64, 2, 64, 2>(a) : go_tile<64, 4, 64, 2>(a);
+}
+
+}  // namespace vitattn

@@ -181,4 +181,88 @@ int agg_partials(int M);  // dq partials of the backward pass
 hipError_t launch_agg_fwd(const AggArgs& a);
 hipError_t launch_agg_bwd(const AggArgs& a);
 
+// element types of the row kernels (layer norm, rotary positions)
+enum { kBf16 = 0, kFp16 = 1, kFp32 = 2 };
+
+// Rows in up to three nested dimensions, the last one fastest, at these
+// element strides; the elements of a row are contiguous.
+struct RowMap {
+  long long s0, s1, s2;
+  __host__ __device__ long long at(long long i0, long long i1, long long i2) const {
+    return i0 * s0 + i1 * s1 + i2 * s2;
+  }
+};
+
+// Layer norm of n0 * n1 * n2 rows of D elements; see vitattn_norm.hip.
+struct NormArgs {
+  const void* x;
+  const void* dy;  // backward
+  const void* w;   // may be null
+  const void* b;   // may be null
+  void* y;         // y, or dx in the backward
+  float* mean;     // one per row; written by the forward unless null, read by the backward
+  float* rstd;
+  void* dw;        // may be null, like db
+  void* db;
+  float* partial;  // workspace: [norm_partials()][2][D], null if neither dw nor db is wanted
+  RowMap mx, mdy, my;
+  int rows, n1, n2, D, lanes;
+  float eps;
+  int type;
+  bool w_f32;  // w, b, dw and db are fp32, else of x's type
+  hipStream_t stream;
+};
+int norm_partials(int rows, int D, int elem_bytes);  // rows of the backward's partial sums
+hipError_t launch_norm_fwd(const NormArgs& a);
+hipError_t launch_norm_bwd(const NormArgs& a);
+
+// Rotary positions; see vitattn_rotary.hip.
+constexpr int kRotaryMaxPairs = 128;  // VITATTN_ROTARY_MAX_PAIRS
+struct RotaryArgs {
+  const void* x[2];  // up to two operands (queries and keys) at the same positions
+  void* y[2];
+  RowMap mx[2], my[2];  // batch, head, row
+  int heads[2];         // 0: no second operand
+  const void* pos;
+  long long pos_batch, pos_row, pos_axis;
+  int pos_type;  // 0: int32, 1: int64, 2: fp32
+  int B, N, d, pairs, type;
+  bool interleaved;
+  double freq[kRotaryMaxPairs];  // signed turns (angle / 2 pi) per unit of position
+  unsigned char axis[kRotaryMaxPairs];
+  hipStream_t stream;
+};
+hipError_t launch_rotary(const RotaryArgs& a);
+
+// Differential attention: q and k hold two maps per head (heads 2h and 2h + 1
+// of 2 H); see vitattn_diff_fwd.hip and vitattn_diff_bwd.hip.
+struct DiffArgs {
+  const uint16_t* q;    // [B][2H][Nq][d]
+  const uint16_t* k;    // [B][2H][Nk][d]
+  const uint16_t* v;    // [B][H][Nk][e]
+  const void* lam;      // [H], fp32 or bf16
+  const int* key_lens;  // [B] or null: keys of each sample, the first of Nk
+  uint16_t* o;          // [B][H][Nq][e]
+  float* maps;          // [B][2H][Nq][e], dense: each map's output (may be null in the forward)
+  float* lse;           // [B][2H][Nq], dense (may be null in the forward)
+  // backward
+  const uint16_t* dout;  // [B][H][Nq][e]
+  uint16_t* dq;
+  uint16_t* dk;
+  uint16_t* dv;
+  void* dlam;      // [H], lam's type
+  float* work;     // workspace (the layout is each pass's own)
+  Map mq, mk, mv, mo, mg, mdq, mdk, mdv;  // mo: o (forward); mg: dout
+  int B, H, Nq, Nk, d, e;
+  float scale;
+  bool lam_bf16;
+  hipStream_t stream;
+};
+// Keys per split of a forward call over few queries; 0: not split.
+int diff_split_keys(int Nq, int Nk);
+size_t diff_fwd_workspace_floats(int B, int H, int Nq, int Nk, int e);
+size_t diff_bwd_workspace_floats(int B, int H, int Nq);
+hipError_t launch_diff_fwd(const DiffArgs& a);
+hipError_t launch_diff_bwd(const DiffArgs& a);
+
 }  // namespace vitattn
