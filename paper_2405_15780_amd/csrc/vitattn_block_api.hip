@@ -98,6 +98,8 @@ int check_diff_sizes(int B, int H, int Nq, int Nk, int d, int e) {
   // rows of the two maps, and launches below 2^32 work-items: 4 per row, padded
   // to 128 rows, and 8 to 32 of each of 64 rows in the row pass
   if (2.0 * B * H * (N + 512.0) > 0x7fffffff || 4.0 * B * H * (N + 512.0) >= kMaxWorkItems) return VITATTN_E_INVAL;
+  // 1,024 per query row where the keys are split
+  if (vitattn::diff_split_keys(Nq, Nk) && 1024.0 * B * H * Nq >= kMaxWorkItems) return VITATTN_E_INVAL;
   return VITATTN_OK;
 }
 

@@ -150,7 +150,7 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
           if (key0 + kb * 32 + acc_row(r, h) >= Nk) s[kb][r] = -INFINITY;
     }
   };
-  auto max_quarter = [&](const f32x16 (&s)[KB], int q) {
+  auto max_share = [&](const f32x16 (&s)[KB], int q) {
     float m = -INFINITY;
 #pragma unroll
     for (int e = q * NE / 4; e < (q + 1) * NE / 4; ++e) m = fmaxf(m, s[e / 16][e % 16]);
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
     sa[i / QS] = mfma32(lds_frag_row(kbuf[0] + koff, (i / QS) * 32 * 2 * DQ + kfrag.at(i % QS)), qf[i % QS], sa[i / QS]);
   }
   if (n_kt == 1) mask_ragged(sa, 0);
-  m_run = max_halves(fmaxf(fmaxf(max_quarter(sa, 0), max_quarter(sa, 1)), fmaxf(max_quarter(sa, 2), max_quarter(sa, 3)))) * c;
+  m_run = max_halves(fmaxf(fmaxf(max_share(sa, 0), max_share(sa, 1)), fmaxf(max_share(sa, 2), max_share(sa, 3)))) * c;
   __syncthreads();  // kbuf[0] is refilled by the first stage
 
   auto stage = [&](auto parity, auto has_next, f32x16 (&s)[KB], f32x16 (&sn)[KB], int j) {
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
         exp_slice(IC, std::integral_constant<int, W>{});
         if constexpr (i >= W && i < W + 4) {
           if constexpr (i == W) mask_ragged(sn, j + 1);
-          mq[i - W] = max_quarter(sn, i - W);
+          mq[i - W] = max_share(sn, i - W);
           pin(mq[i - W]);
         }
         sched_fence();
@@ -341,54 +341,82 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
   }
 }
 
-// Joins the splits of one query row: a wave per row (bh, query). Lane s of the
-// first pass weighs split s; the outputs are then added in split order.
-__global__ __launch_bounds__(256) void diff_join_kernel(const DiffArgs a, int n_split) {
-  const long long rows = (long long)a.B * a.H * a.Nq;
-  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= rows) return;
-  const int lane = threadIdx.x & 63;
+// Joins the splits of one query row (bh, query), a workgroup per row: waves
+// 0 .. 7 take map 1 and 8 .. 15 map 2, each an eighth of the splits. A lane
+// weighs split s; the outputs are added in split order, eight in flight, then
+// the eighths in order.
+__global__ __launch_bounds__(1024) void diff_join_kernel(const DiffArgs a, int n_split) {
+  constexpr int Q = 8, U = 8;
+  __shared__ float tops[2 * Q], sums[2 * Q], acc[2][Q][192];
+  debug_poison_lds(tops, sums, acc);
+  const long long row = blockIdx.x, rows = (long long)a.B * a.H * a.Nq;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = wave / Q, share = wave % Q;
   const long long bh = row / a.Nq;
   const int i = (int)(row - bh * a.Nq);
   const int b = (int)(bh / a.H), head = (int)(bh - (long long)b * a.H);
-  const float* lses = a.work + rows * n_split * 2 * a.e;
-  float acc[2][3];  // columns lane, lane + 64, lane + 128
+  const long long base = (bh * n_split * 2 + m) * a.Nq + i, step = 2LL * a.Nq;
+  const float* lses = a.work + rows * n_split * 2 * a.e + base;
+  const float* outs = a.work + base * a.e;
+  float top = -INFINITY, sum = 0.f;
+  for (int s = share * 64 + lane; s < n_split; s += 64 * Q) top = fmaxf(top, lses[s * step]);
 #pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    const long long base = (bh * n_split * 2 + m) * a.Nq + i, step = 2LL * a.Nq;
-    float top = -INFINITY, sum = 0.f;
-    for (int s = lane; s < n_split; s += 64) top = fmaxf(top, lses[base + s * step]);
+  for (int x = 32; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+  if (lane == 0) tops[wave] = top;
+  __syncthreads();
 #pragma unroll
-    for (int x = 32; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
-    const float ref = top == -INFINITY ? 0.f : top;  // no keys at all
-    for (int s = lane; s < n_split; s += 64) sum += expf(lses[base + s * step] - ref);
+  for (int w = 0; w < Q; ++w) top = fmaxf(top, tops[m * Q + w]);
+  const float ref = top == -INFINITY ? 0.f : top;  // no keys at all
+  for (int s = share * 64 + lane; s < n_split; s += 64 * Q) sum += expf(lses[s * step] - ref);
 #pragma unroll
-    for (int x = 32; x >= 1; x >>= 1) sum += __shfl_xor(sum, x, 64);
-    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-    if (lane == 0 && a.lse) a.lse[(bh * 2 + m) * a.Nq + i] = top == -INFINITY ? -INFINITY : ref + logf(sum);
+  for (int x = 32; x >= 1; x >>= 1) sum += __shfl_xor(sum, x, 64);
+  if (lane == 0) sums[wave] = sum;
+  // columns lane, lane + 64, lane + 128 of this wave's splits
+  float o[3] = {0.f, 0.f, 0.f};
+  const int s0 = (int)((long long)n_split * share / Q), s1 = (int)((long long)n_split * (share + 1) / Q);
+  for (int s = s0; s < s1; s += U) {
+    float w[U], x[U][3];
 #pragma unroll
-    for (int t = 0; t < 3; ++t) acc[m][t] = 0.f;
-    for (int s = 0; s < n_split; ++s) {
-      const float l = lses[base + s * step];
-      if (l == -INFINITY) continue;  // an empty split wrote no outputs
-      const float w = expf(l - ref) * inv;
-      const float* src = a.work + (base + s * step) * a.e;
+    for (int u = 0; u < U; ++u) {
+      const bool on = s + u < s1;
+      const float l = on ? lses[(s + u) * step] : -INFINITY;
+      const bool any = l != -INFINITY;  // an empty split wrote no outputs
+      w[u] = any ? expf(l - ref) : 0.f;
 #pragma unroll
       for (int t = 0; t < 3; ++t)
-        if (lane + 64 * t < a.e) acc[m][t] += w * src[lane + 64 * t];
+        x[u][t] = any && lane + 64 * t < a.e ? outs[(s + u) * step * a.e + lane + 64 * t] : 0.f;
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int t = 0; t < 3; ++t) o[t] += w[u] * x[u][t];
+  }
+#pragma unroll
+  for (int t = 0; t < 3; ++t) acc[m][share][lane + 64 * t] = o[t];
+  __syncthreads();
+  float l[2];
+#pragma unroll
+  for (int mm = 0; mm < 2; ++mm) {
+    l[mm] = 0.f;
+#pragma unroll
+    for (int w = 0; w < Q; ++w) l[mm] += sums[mm * Q + w];
+  }
+  if (lane == 0 && share == 0 && a.lse)
+    a.lse[(bh * 2 + m) * a.Nq + i] = top == -INFINITY ? -INFINITY : ref + logf(m ? l[1] : l[0]);
+  const int col = threadIdx.x;
+  if (col >= a.e) return;
+  float y[2];
+#pragma unroll
+  for (int mm = 0; mm < 2; ++mm) {
+    const float inv = l[mm] > 0.f || l[mm] != l[mm] ? 1.f / l[mm] : 0.f;
+    y[mm] = 0.f;
+#pragma unroll
+    for (int w = 0; w < Q; ++w) y[mm] += acc[mm][w][col];
+    y[mm] *= inv;
+    if (a.maps) a.maps[((bh * 2 + mm) * a.Nq + i) * a.e + col] = y[mm];
   }
   const float lam = lam_of(a.lam, a.lam_bf16, head);
-  uint16_t* o = a.o + b * a.mo.sb + head * a.mo.sh + (long long)i * a.mo.ld;
-#pragma unroll
-  for (int t = 0; t < 3; ++t) {
-    const int col = lane + 64 * t;
-    if (col >= a.e) continue;
-    o[col] = __builtin_bit_cast(uint16_t, (__bf16)(acc[0][t] - lam * acc[1][t]));
-    if (a.maps)
-#pragma unroll
-      for (int m = 0; m < 2; ++m) a.maps[((bh * 2 + m) * a.Nq + i) * a.e + col] = acc[m][t];
-  }
+  a.o[b * a.mo.sb + head * a.mo.sh + (long long)i * a.mo.ld + col] =
+      __builtin_bit_cast(uint16_t, (__bf16)(y[0] - lam * y[1]));
 }
 
 template <int DQ, int QS, int DV, int KB, int QW, bool SPLIT>
@@ -407,8 +435,7 @@ hipError_t go_tile(const DiffArgs& a) {
   const int n_split = (a.Nk + split_keys - 1) / split_keys;
   const hipError_t err = go<DQ, QS, DV, KB, 2, true>(a, split_keys, n_split);
   if (err != hipSuccess) return err;
-  const long long rows = (long long)a.B * a.H * a.Nq;
-  diff_join_kernel<<<(unsigned)((rows + 3) / 4), 256, 0, a.stream>>>(a, n_split);
+  diff_join_kernel<<<(unsigned)(a.B * a.H * a.Nq), 1024, 0, a.stream>>>(a, n_split);
   return hipGetLastError();
 }
 
@@ -416,7 +443,8 @@ hipError_t go_tile(const DiffArgs& a) {
 
 int diff_split_keys(int Nq, int Nk) {
   if (Nq > 64 || Nk < 1024) return 0;
-  return 512;
+  const int keys = (Nk / 128 + 63) / 64 * 64;
+  return keys > 512 ? keys : 512;
 }
 
 size_t diff_fwd_workspace_floats(int B, int H, int Nq, int Nk, int e) {

@@ -10,9 +10,9 @@
 // their type.
 //
 // L lanes share a row, each holding NP pieces of 16 bytes (pieces lane, lane +
-// L, ..): a power of two of a wave's lanes for short rows, 64 / L rows per
-// wave, and the four waves of a workgroup for long ones. Rows too long for
-// registers (over 256 * 8 pieces) are read once per pass instead, from L2.
+// L, ..): L of a wave's 64 lanes for short rows, 64 / L rows per wave, and the
+// four waves of a workgroup for long ones. Rows too long for registers (over
+// 256 * 8 pieces) are read once per pass instead, from L2.
 //
 // The backward's workgroups each take a fixed run of row groups and keep their
 // share of dw and db in registers; at the end the workgroup adds its lanes'
@@ -29,7 +29,7 @@ constexpr int kThreads = 256;
 
 // row r -> its three indexes
 __device__ __forceinline__ void split_row(const NormArgs& a, int r, int& i0, int& i1, int& i2) {
-  const int t = r / a.n2;
+  const int t = a.n2 == a.rows ? 0 : r / a.n2;
   i2 = r - t * a.n2;
   i0 = t / a.n1;
   i1 = t - i0 * a.n1;
@@ -55,29 +55,76 @@ __device__ __forceinline__ void load_weights(const void* p, bool f32, long long 
   }
 }
 
-// Sum over the L lanes of a row (BLOCK: over the workgroup), the same in all.
+// Where a thread stands: its row of the workgroup's `per` at a time (outside
+// them: a wave's lanes behind its last whole row) and its lane of the row.
 template <bool BLOCK>
-__device__ __forceinline__ float row_sum(float x, int L, float* lds) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1)
-    if (BLOCK || m < L) x += __shfl_xor(x, m, 64);
-  if constexpr (BLOCK) {
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = lds[0] + lds[1] + lds[2] + lds[3];
+struct Place {
+  int L, lane, row, per;
+  __device__ __forceinline__ explicit Place(int lanes) : L(lanes) {
+    if constexpr (BLOCK) {
+      lane = threadIdx.x;
+      row = 0;
+      per = 1;
+    } else {
+      const int wl = threadIdx.x & 63, rpw = 64 / L, g = wl / L;
+      lane = wl - g * L;
+      per = rpw * (kThreads / 64);
+      row = g < rpw ? (int)(threadIdx.x >> 6) * rpw + g : -1;
+    }
   }
-  return x;
-}
+  // Sum over the row's lanes (BLOCK: over the workgroup), the same in all.
+  __device__ __forceinline__ float sum(float x, float* lds) const {
+    if (BLOCK || (L & (L - 1)) == 0) {
+#pragma unroll
+      for (int m = 32; m >= 1; m >>= 1)
+        if (BLOCK || m < L) x += __shfl_xor(x, m, 64);
+    } else {
+      const int at = threadIdx.x & 63;
+      for (int m = 32; m >= 1; m >>= 1) {
+        if (m >= L) continue;
+        const float y = __shfl(x, (at + m) & 63, 64);
+        x += lane + m < L ? y : 0.f;
+      }
+      x = __shfl(x, at - lane, 64);
+    }
+    if constexpr (BLOCK) {
+      __syncthreads();
+      if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+      __syncthreads();
+      x = lds[0] + lds[1] + lds[2] + lds[3];
+    }
+    return x;
+  }
+};
+
+// A row's pieces in this lane's registers.
+template <typename T, int NP>
+struct RowRegs {
+  Piece<T> p[NP];
+  __device__ __forceinline__ void load(const T* x, int lane, int L, int D, bool on) {
+    constexpr int V = Piece<T>::V;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int c = (lane + i * L) * V;
+      p[i].load(x + c, on ? min(max(D - c, 0), V) : 0);
+    }
+  }
+};
+
+// Rows of a lane in flight together: short rows give it one or two pieces each.
+constexpr int rows_at_once(int np) { return np == 1 ? 4 : np == 2 ? 2 : 1; }
+
+// The backward holds the next long row as well where there are registers for it.
+constexpr bool row_ahead(int np, int v) { return np * v <= 32; }
 
 template <typename T, int NP, bool BLOCK>
 __global__ __launch_bounds__(kThreads) void norm_fwd_kernel(const NormArgs a) {
   constexpr int V = Piece<T>::V;
+  constexpr int U = BLOCK ? 1 : rows_at_once(NP);
   __shared__ float lds[4];
   debug_poison_lds(lds);
-  const int L = a.lanes;
-  const int lane = threadIdx.x % L;
-  const int per = kThreads / L;  // rows of a workgroup at a time
+  const Place<BLOCK> at(a.lanes);
+  const int L = at.L, lane = at.lane, per = at.per;  // rows of a workgroup at a time, U times
   float w[NP][V], b[NP][V];
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
@@ -91,46 +138,66 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_kernel(const NormArgs a) {
     if (a.b) load_weights<T>(a.b, a.w_f32, c, n, b[i]);
   }
   const float inv = 1.f / (float)a.D;
-  for (int r0 = blockIdx.x * per; r0 < a.rows; r0 += gridDim.x * per) {
-    const int r = r0 + threadIdx.x / L;
-    const bool on = r < a.rows;
-    const T* x = static_cast<const T*>(a.x) + (on ? row_at(a, a.mx, r) : 0);
-    Piece<T> p[NP];
-    float s = 0.f;
+  auto load = [&](RowRegs<T, NP>& x, int r) __attribute__((always_inline)) {
+    const bool on = at.row >= 0 && r < a.rows;
+    x.load(static_cast<const T*>(a.x) + (on ? row_at(a, a.mx, r) : 0), lane, L, a.D, on);
+  };
+  RowRegs<T, NP> x[U], next;
+  const int step = gridDim.x * per * U;
+  int r0 = blockIdx.x * per * U + at.row;
+  if (BLOCK && r0 < a.rows) load(next, r0);
+  for (; r0 - at.row < a.rows; r0 += step) {
+    if constexpr (BLOCK) {
+      x[0] = next;
+      if (r0 + step < a.rows) load(next, r0 + step);  // on its way through this row's sums
+    } else {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int c = (lane + i * L) * V;
-      p[i].load(x + c, on ? min(max(a.D - c, 0), V) : 0);
-#pragma unroll
-      for (int e = 0; e < V; ++e) s += p[i].get(e);
+      for (int u = 0; u < U; ++u) load(x[u], r0 + u * per);
     }
-    const float mean = row_sum<BLOCK>(s, L, lds) * inv;
-    float q = 0.f;
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int n = a.D - (lane + i * L) * V;
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + u * per;
+      float s = 0.f;
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float d = p[i].get(e) - mean;
-        q += e < n ? d * d : 0.f;
+      for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) s += x[u].p[i].get(e);
+      const float mean = at.sum(s, lds) * inv;
+      float q = 0.f;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const int n = a.D - (lane + i * L) * V;
+        if (n >= V) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float d = x[u].p[i].get(e) - mean;
+            q = __builtin_fmaf(d, d, q);
+          }
+        } else if (n > 0) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float d = e < n ? x[u].p[i].get(e) - mean : 0.f;
+            q = __builtin_fmaf(d, d, q);
+          }
+        }
       }
-    }
-    const float rstd = rsqrtf(row_sum<BLOCK>(q, L, lds) * inv + a.eps);
-    if (!on) continue;
-    T* y = static_cast<T*>(a.y) + row_at(a, a.my, r);
+      const float rstd = rsqrtf(at.sum(q, lds) * inv + a.eps);
+      if (at.row < 0 || r >= a.rows) continue;
+      T* y = static_cast<T*>(a.y) + row_at(a, a.my, r);
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int c = (lane + i * L) * V;
-      float v[V];
+      for (int i = 0; i < NP; ++i) {
+        const int c = (lane + i * L) * V;
+        float v[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) v[e] = (p[i].get(e) - mean) * rstd * w[i][e] + b[i][e];
-      Piece<T> o;
-      o.set(v);
-      o.store(y + c, min(max(a.D - c, 0), V));
-    }
-    if (lane == 0 && a.mean) {
-      a.mean[r] = mean;
-      a.rstd[r] = rstd;
+        for (int e = 0; e < V; ++e) v[e] = __builtin_fmaf((x[u].p[i].get(e) - mean) * rstd, w[i][e], b[i][e]);
+        Piece<T> o;
+        o.set(v);
+        o.store(y + c, min(max(a.D - c, 0), V));
+      }
+      if (lane == 0 && a.mean) {
+        a.mean[r] = mean;
+        a.rstd[r] = rstd;
+      }
     }
   }
 }
@@ -152,7 +219,7 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_long_kernel(const NormArgs 
 #pragma unroll
       for (int e = 0; e < V; ++e) s += p.get(e);
     }
-    const float mean = row_sum<true>(s, 64, lds) * inv;
+    const float mean = Place<true>(kThreads).sum(s, lds) * inv;
     for (int c = threadIdx.x * V; c < a.D; c += kThreads * V) {
       Piece<T> p;
       p.load(x + c, min(a.D - c, V));
@@ -162,7 +229,7 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_long_kernel(const NormArgs 
         q += e < a.D - c ? d * d : 0.f;
       }
     }
-    const float rstd = rsqrtf(row_sum<true>(q, 64, lds) * inv + a.eps);
+    const float rstd = rsqrtf(Place<true>(kThreads).sum(q, lds) * inv + a.eps);
     for (int c = threadIdx.x * V; c < a.D; c += kThreads * V) {
       const int n = min(a.D - c, V);
       Piece<T> p;
@@ -193,12 +260,13 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_long_kernel(const NormArgs 
 template <typename T, int NP, bool BLOCK>
 __global__ __launch_bounds__(kThreads) void norm_bwd_kernel(const NormArgs a) {
   constexpr int V = Piece<T>::V;
+  constexpr int U = 1;  // (more rows at once leave too few registers)
+  constexpr bool AHEAD = BLOCK && row_ahead(NP, V);
   __shared__ float lds[4];
-  __shared__ float part[BLOCK ? 1 : 4][BLOCK ? 1 : 64][V];
+  __shared__ float part[BLOCK ? 1 : kThreads][V];
   debug_poison_lds(lds, part);
-  const int L = a.lanes;
-  const int lane = threadIdx.x % L;
-  const int per = kThreads / L;
+  const Place<BLOCK> at(a.lanes);
+  const int L = at.L, lane = at.lane, per = at.per;
   float w[NP][V], dw[NP][V], db[NP][V];
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
@@ -211,46 +279,61 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_kernel(const NormArgs a) {
     if (a.w) load_weights<T>(a.w, a.w_f32, c, n, w[i]);
   }
   const float inv = 1.f / (float)a.D;
-  for (int r0 = blockIdx.x * per; r0 < a.rows; r0 += gridDim.x * per) {
-    const int r = r0 + threadIdx.x / L;
-    const bool on = r < a.rows;
-    const T* x = static_cast<const T*>(a.x) + (on ? row_at(a, a.mx, r) : 0);
-    const T* dy = static_cast<const T*>(a.dy) + (on ? row_at(a, a.mdy, r) : 0);
-    const float mean = on ? a.mean[r] : 0.f, rstd = on ? a.rstd[r] : 0.f;
-    Piece<T> p[NP], g[NP];
+  struct Row {
+    RowRegs<T, NP> x, g;
+    float mean, rstd;
+  };
+  auto load = [&](Row& w_, int r) __attribute__((always_inline)) {
+    const bool on = at.row >= 0 && r < a.rows;
+    w_.x.load(static_cast<const T*>(a.x) + (on ? row_at(a, a.mx, r) : 0), lane, L, a.D, on);
+    w_.g.load(static_cast<const T*>(a.dy) + (on ? row_at(a, a.mdy, r) : 0), lane, L, a.D, on);
+    w_.mean = on ? a.mean[r] : 0.f;
+    w_.rstd = on ? a.rstd[r] : 0.f;
+  };
+  Row row[U], next;
+  const int step = gridDim.x * per * U;
+  int r0 = blockIdx.x * per * U + at.row;
+  if (AHEAD && r0 < a.rows) load(next, r0);
+  for (; r0 - at.row < a.rows; r0 += step) {
+    if constexpr (AHEAD) {
+      row[0] = next;
+      if (r0 + step < a.rows) load(next, r0 + step);
+    } else {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int c = (lane + i * L) * V, n = on ? min(max(a.D - c, 0), V) : 0;
-      p[i].load(x + c, n);
-      g[i].load(dy + c, n);
+      for (int u = 0; u < U; ++u) load(row[u], r0 + u * per);
     }
-    // lanes past the row hold dy = 0 and add nothing to any sum
-    float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-    for (int i = 0; i < NP; ++i)
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + u * per;
+      const float mean = row[u].mean, rstd = row[u].rstd;
+      // lanes past the row hold dy = 0 and add nothing to any sum
+      float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float d = g[i].get(e), h = (p[i].get(e) - mean) * rstd, gw = d * w[i][e];
-        s1 += gw;
-        s2 += gw * h;
-        dw[i][e] += d * h;
-        db[i][e] += d;
+      for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float d = row[u].g.p[i].get(e), h = (row[u].x.p[i].get(e) - mean) * rstd, gw = d * w[i][e];
+          s1 += gw;
+          s2 = __builtin_fmaf(gw, h, s2);
+          dw[i][e] = __builtin_fmaf(d, h, dw[i][e]);
+          db[i][e] += d;
+        }
+      const float m1 = -at.sum(s1, lds) * inv * rstd, m2 = -at.sum(s2, lds) * inv * rstd;
+      if (at.row < 0 || r >= a.rows) continue;
+      T* dx = static_cast<T*>(a.y) + row_at(a, a.my, r);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const int c = (lane + i * L) * V;
+        float v[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float h = (row[u].x.p[i].get(e) - mean) * rstd;
+          v[e] = __builtin_fmaf(row[u].g.p[i].get(e) * w[i][e], rstd, __builtin_fmaf(h, m2, m1));
+        }
+        Piece<T> o;
+        o.set(v);
+        o.store(dx + c, min(max(a.D - c, 0), V));
       }
-    const float m1 = row_sum<BLOCK>(s1, L, lds) * inv, m2 = row_sum<BLOCK>(s2, L, lds) * inv;
-    if (!on) continue;
-    T* dx = static_cast<T*>(a.y) + row_at(a, a.my, r);
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int c = (lane + i * L) * V;
-      float v[V];
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float h = (p[i].get(e) - mean) * rstd;
-        v[e] = rstd * (g[i].get(e) * w[i][e] - m1 - h * m2);
-      }
-      Piece<T> o;
-      o.set(v);
-      o.store(dx + c, min(max(a.D - c, 0), V));
     }
   }
   if (!a.partial) return;
@@ -263,19 +346,16 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_kernel(const NormArgs a) {
 #pragma unroll
       for (int e = 0; e < V; ++e) v[e] = k ? db[i][e] : dw[i][e];
       if constexpr (!BLOCK) {
-        // the wave's rows, then the four waves
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-          for (int m = L; m < 64; m <<= 1) v[e] += __shfl_xor(v[e], m, 64);
+        // the workgroup's rows, in their order
         __syncthreads();
+        if (at.row >= 0)
 #pragma unroll
-        for (int e = 0; e < V; ++e) part[threadIdx.x >> 6][threadIdx.x & 63][e] = v[e];
+          for (int e = 0; e < V; ++e) part[at.row * L + lane][e] = v[e];
         __syncthreads();
+        if (at.row != 0) continue;
+        for (int r = 1; r < per; ++r)
 #pragma unroll
-        for (int e = 0; e < V; ++e)
-          v[e] = part[0][threadIdx.x & 63][e] + part[1][threadIdx.x & 63][e] + part[2][threadIdx.x & 63][e] +
-                 part[3][threadIdx.x & 63][e];
-        if ((int)threadIdx.x >= L) continue;
+          for (int e = 0; e < V; ++e) v[e] += part[r * L + lane][e];
       }
 #pragma unroll
       for (int e = 0; e < V; ++e)
@@ -320,8 +400,8 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_long_kernel(const NormArgs 
         }
       }
       if (!pass) {
-        m1 = row_sum<true>(s1, 64, lds) * inv;
-        m2 = row_sum<true>(s2, 64, lds) * inv;
+        m1 = Place<true>(kThreads).sum(s1, lds) * inv;
+        m2 = Place<true>(kThreads).sum(s2, lds) * inv;
       }
     }
   }
@@ -345,21 +425,34 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_columns_kernel(const NormAr
   out[a.D + c] = db;
 }
 
-// dw and db from n partial rows: a workgroup takes 64 of the 2 D columns, its
-// waves a quarter of the rows each, added in a fixed order.
+// dw and db from n partial rows: a workgroup takes 64 of the 2 D columns, its 16
+// waves every 16th row each, eight loads in flight, added in a fixed order.
+constexpr int kWeightWaves = 16;
 template <typename T>
-__global__ __launch_bounds__(kThreads) void norm_weights_kernel(const NormArgs a, int n) {
-  __shared__ float part[4][64];
+__global__ __launch_bounds__(64 * kWeightWaves) void norm_weights_kernel(const NormArgs a, int n) {
+  __shared__ float part[kWeightWaves][64];
   debug_poison_lds(part);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const long long c = (long long)blockIdx.x * 64 + lane;
+  const long long c = (long long)blockIdx.x * 64 + lane, width = 2LL * a.D;
   float s = 0.f;
-  if (c < 2LL * a.D)
-    for (int p = wave; p < n; p += 4) s += a.partial[(long long)p * 2 * a.D + c];
+  if (c < width) {
+    const float* src = a.partial + c;
+    int p = wave;
+    for (; p + 7 * kWeightWaves < n; p += 8 * kWeightWaves) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = src[(p + u * kWeightWaves) * width];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += x[u];
+    }
+    for (; p < n; p += kWeightWaves) s += src[p * width];
+  }
   part[wave][lane] = s;
   __syncthreads();
-  if (wave != 0 || c >= 2LL * a.D) return;
-  s = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+  if (wave != 0 || c >= width) return;
+  s = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWeightWaves; ++w) s += part[w][lane];
   void* out = c < a.D ? a.dw : a.db;
   if (!out) return;
   const long long at = c < a.D ? c : c - a.D;
@@ -367,41 +460,84 @@ __global__ __launch_bounds__(kThreads) void norm_weights_kernel(const NormArgs a
   else static_cast<T*>(out)[at] = (T)s;
 }
 
-// pieces of a row, lanes that share it, pieces per lane; lanes = 0: too long
+// Lanes that share a row and pieces per lane (lanes = 0: too long for
+// registers). For short rows the fewest pieces per lane that keep three
+// quarters of a wave's lanes at work, or else the most lanes at work.
 struct Shape {
   int lanes, np;
 };
 Shape shape_of(int D, int V) {
   const int pieces = (D + V - 1) / V;
   if (pieces <= 256) {
-    int L = 1;
-    while (L < 64 && L < pieces) L *= 2;
-    const int np = (pieces + L - 1) / L;
-    return {L, np <= 2 ? np : 4};
+    Shape best = {0, 0};
+    int most = -1;
+    for (int np = 1; np <= 4; ++np) {
+      const int L = (pieces + np - 1) / np;
+      if (L > 64) continue;
+      const int used = pieces * (64 / L) * 12 / np;  // of 64 * 12
+      if (used >= 64 * 9) return {L, np};
+      if (used > most) {
+        most = used;
+        best = {L, np};
+      }
+    }
+    return best;
   }
   const int np = (pieces + kThreads - 1) / kThreads;
-  if (np > 8) return {0, 0};
-  return {kThreads, np <= 2 ? np : np <= 4 ? 4 : 8};
+  return np > 8 ? Shape{0, 0} : Shape{kThreads, np == 7 ? 8 : np};
 }
 
-template <typename T, int NP, bool BLOCK, bool FWD>
-void go(const NormArgs& a, int grid) {
-  if constexpr (FWD) norm_fwd_kernel<T, NP, BLOCK><<<grid, kThreads, 0, a.stream>>>(a);
-  else norm_bwd_kernel<T, NP, BLOCK><<<grid, kThreads, 0, a.stream>>>(a);
+// Workgroups of the backward that a CU holds, from the registers of a lane:
+// five fp32 values per element (w, dw, db and the row's h and g), the rows as
+// they are and about 48 more, at most four. The grid is this many for each of
+// 256 CUs: one round, so that no workgroup waits for others to end (at D = 72
+// and 320,016 rows 1,024 workgroups where 768 fit took 67 us, 512 took 50).
+// The number is the sizes' alone: dw and db do not depend on the device.
+constexpr int bwd_resident(int np, int v, bool block) {
+  const int regs = 5 * np * v + (block && row_ahead(np, v) ? 16 : 8) * np + 48;
+  return regs <= 128 ? 4 : regs <= 170 ? 3 : regs <= 270 ? 2 : 1;
+}
+
+// Rows of a workgroup at a time.
+int rows_of(const Shape& s, bool fwd) {
+  return s.lanes > 64 ? 1 : 64 / s.lanes * (kThreads / 64) * (fwd ? rows_at_once(s.np) : 1);
+}
+int groups_of(const Shape& s, int rows, bool fwd) {
+  return (int)(((long long)rows + rows_of(s, fwd) - 1) / rows_of(s, fwd));
+}
+
+// The forward's grid is what the device holds at once (its rows do not depend on it).
+template <typename T, int NP, bool BLOCK>
+hipError_t go_fwd(const NormArgs& a, int groups) {
+  static ResidentCache cache;
+  const int most = cache.get(reinterpret_cast<const void*>(norm_fwd_kernel<T, NP, BLOCK>), kThreads).workgroups;
+  norm_fwd_kernel<T, NP, BLOCK><<<min(groups, most > 0 ? most : 1024), kThreads, 0, a.stream>>>(a);
+  return hipGetLastError();
+}
+template <typename T, int NP, bool BLOCK>
+hipError_t go_bwd(const NormArgs& a, int grid) {
+  norm_bwd_kernel<T, NP, BLOCK><<<grid, kThreads, 0, a.stream>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, bool FWD, int NP, bool BLOCK>
+hipError_t go(const NormArgs& a, int n) {
+  if constexpr (FWD) return go_fwd<T, NP, BLOCK>(a, n);
+  else return go_bwd<T, NP, BLOCK>(a, n);
 }
 
 template <typename T, bool FWD>
-hipError_t go_shape(const NormArgs& a, const Shape& s, int grid) {
-  if (s.lanes <= 64) {
-    if (s.np == 1) go<T, 1, false, FWD>(a, grid);
-    else if (s.np == 2) go<T, 2, false, FWD>(a, grid);
-    else go<T, 4, false, FWD>(a, grid);
-  } else {
-    if (s.np == 2) go<T, 2, true, FWD>(a, grid);
-    else if (s.np == 4) go<T, 4, true, FWD>(a, grid);
-    else go<T, 8, true, FWD>(a, grid);
+hipError_t go_shape(const NormArgs& a, const Shape& s, int n) {
+  const bool block = s.lanes > 64;
+  switch (s.np) {
+    case 1: return go<T, FWD, 1, false>(a, n);  // (long rows have two pieces per lane or more)
+    case 2: return block ? go<T, FWD, 2, true>(a, n) : go<T, FWD, 2, false>(a, n);
+    case 3: return block ? go<T, FWD, 3, true>(a, n) : go<T, FWD, 3, false>(a, n);
+    case 4: return block ? go<T, FWD, 4, true>(a, n) : go<T, FWD, 4, false>(a, n);
+    case 5: return go<T, FWD, 5, true>(a, n);
+    case 6: return go<T, FWD, 6, true>(a, n);
+    default: return go<T, FWD, 8, true>(a, n);
   }
-  return hipGetLastError();
 }
 
 template <typename T>
@@ -412,8 +548,7 @@ hipError_t fwd_t(NormArgs a) {
     return hipGetLastError();
   }
   a.lanes = s.lanes;
-  const int per = kThreads / s.lanes;
-  return go_shape<T, true>(a, s, min((a.rows + per - 1) / per, 2048));
+  return go_shape<T, true>(a, s, groups_of(s, a.rows, true));
 }
 
 template <typename T>
@@ -431,7 +566,7 @@ hipError_t bwd_t(NormArgs a) {
     err = go_shape<T, false>(a, s, n);
   }
   if (err != hipSuccess || !a.partial) return err;
-  norm_weights_kernel<T><<<(int)((2LL * a.D + 63) / 64), kThreads, 0, a.stream>>>(a, n);
+  norm_weights_kernel<T><<<(int)((2LL * a.D + 63) / 64), 64 * kWeightWaves, 0, a.stream>>>(a, n);
   return hipGetLastError();
 }
 
@@ -439,9 +574,8 @@ hipError_t bwd_t(NormArgs a) {
 
 int norm_partials(int rows, int D, int elem_bytes) {
   const Shape s = shape_of(D, 16 / elem_bytes);
-  const int groups = s.lanes == 0 ? rows : (rows + kThreads / s.lanes - 1) / (kThreads / s.lanes);
-  const int most = s.lanes == 0 ? 64 : 1024;
-  return groups < most ? groups : most;
+  if (s.lanes == 0) return rows < 64 ? rows : 64;
+  return min(groups_of(s, rows, false), 256 * bwd_resident(s.np, 16 / elem_bytes, s.lanes > 64));
 }
 
 hipError_t launch_norm_fwd(const NormArgs& a) {

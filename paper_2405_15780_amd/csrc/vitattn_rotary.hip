@@ -72,41 +72,53 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, in
   }
   const int heads = a.heads[0] + a.heads[1];
   const int h1 = min(heads, ((int)blockIdx.y + 1) * group);
-  for (int h = blockIdx.y * group; h < h1; ++h) {
-    const int o = h >= a.heads[0];
-    const int hh = o ? h - a.heads[0] : h;
-    const T* x = static_cast<const T*>(a.x[o]) + a.mx[o].at(b, hh, n);
-    T* y = static_cast<T*>(a.y[o]) + a.my[o].at(b, hh, n);
-    Piece<T> u, v;
-    u.load(x + c0, n0);
-    v.load(x + c1, n1);
-    if (turn) {
-      float p[V], q[V];
+  constexpr int U = 4;  // heads in flight
+  for (int h0 = blockIdx.y * group; h0 < h1; h0 += U) {
+    Piece<T> u[U], v[U];
+    T* y[U];
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        if (INTERLEAVED) {  // pair e: elements 2e and 2e + 1 of the 2 V loaded
-          const int i = 2 * e;
-          const float first = i < V ? u.get(i % V) : v.get(i % V);
-          const float second = i < V ? u.get(i % V + 1) : v.get(i % V + 1);
-          const float f = first * cs[e] - second * sn[e], s = second * cs[e] + first * sn[e];
-          if (i < V) {
-            p[i % V] = f;
-            p[i % V + 1] = s;
-          } else {
-            q[i % V] = f;
-            q[i % V + 1] = s;
-          }
-        } else {
-          const float first = u.get(e), second = v.get(e);
-          p[e] = first * cs[e] - second * sn[e];
-          q[e] = second * cs[e] + first * sn[e];
-        }
+    for (int i = 0; i < U; ++i) {
+      const int h = h0 + i < h1 ? h0 + i : h1 - 1;
+      const int o = h >= a.heads[0];
+      const int hh = o ? h - a.heads[0] : h;
+      const T* x = static_cast<const T*>(a.x[o]) + a.mx[o].at(b, hh, n);
+      y[i] = static_cast<T*>(a.y[o]) + a.my[o].at(b, hh, n);
+      if (h0 + i < h1) {
+        u[i].load(x + c0, n0);
+        v[i].load(x + c1, n1);
       }
-      u.set(p);
-      v.set(q);
     }
-    u.store(y + c0, n0);
-    v.store(y + c1, n1);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (h0 + i >= h1) break;
+      if (turn) {
+        float p[V], q[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          if (INTERLEAVED) {  // pair e: elements 2e and 2e + 1 of the 2 V loaded
+            const int k = 2 * e;
+            const float first = k < V ? u[i].get(k % V) : v[i].get(k % V);
+            const float second = k < V ? u[i].get(k % V + 1) : v[i].get(k % V + 1);
+            const float f = first * cs[e] - second * sn[e], s = second * cs[e] + first * sn[e];
+            if (k < V) {
+              p[k % V] = f;
+              p[k % V + 1] = s;
+            } else {
+              q[k % V] = f;
+              q[k % V + 1] = s;
+            }
+          } else {
+            const float first = u[i].get(e), second = v[i].get(e);
+            p[e] = first * cs[e] - second * sn[e];
+            q[e] = second * cs[e] + first * sn[e];
+          }
+        }
+        u[i].set(p);
+        v[i].set(q);
+      }
+      u[i].store(y[i] + c0, n0);
+      v[i].store(y[i] + c1, n1);
+    }
   }
 }
 
@@ -119,7 +131,9 @@ hipError_t go(const RotaryArgs& a) {
   const int pieces = turned + rest;
   const int heads = a.heads[0] + a.heads[1];
   const long long blocks = ((long long)a.N * pieces + kThreads - 1) / kThreads;
-  const int group = blocks * a.B >= 2048 ? 16 : 1;
+  // heads per thread: as many as leave eight workgroups per CU
+  int group = 16;
+  while (group > 1 && blocks * a.B * ((heads + group - 1) / group) < 2048) group /= 2;
   const dim3 grid((unsigned)blocks, (heads + group - 1) / group, a.B);
   if (a.interleaved) rotary_kernel<T, true><<<grid, kThreads, 0, a.stream>>>(a, turned, pieces, group);
   else rotary_kernel<T, false><<<grid, kThreads, 0, a.stream>>>(a, turned, pieces, group);
