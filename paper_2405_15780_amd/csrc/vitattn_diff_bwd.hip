@@ -6,7 +6,7 @@
 //   dQ_m = scale dS_m K_m,  dK_m = scale dS_m^T Q_m,  dV = (P_1 - lam P_2)^T dO,
 //   dlam = - sum_i D_2.
 //
-//   1. row pass: -D_1, -D_2 and LSE_m * log2(e) per query, and a partial sum of
+//   1. row pass: -D_1, D_1 - D_2 and LSE_m * log2(e) per query, and a partial sum of
 //      D_2 per workgroup (HBM-bound; O_1 and O_2 in fp32, see the forward).
 //   2. dK/dV kernel: a workgroup per 32 KBW keys; two waves per 32 keys split the
 //      work (as in vitattn_bwd.hip): role V holds K_1, K_2, forms both maps' P
@@ -15,8 +15,11 @@
 //      e = 2 d both have 16 matrix ops per 32 x 32 block.
 //   3. dQ kernel: 32 queries per wave, Q_1, Q_2 and dO held; streams K_1, K_2, V.
 //
-// P and dS are rounded to bf16 as matrix-core operands; everything else is fp32
-// until the outputs are rounded once. No atomics: the sums of dlam's partials
+// P_1 - lam P_2 and dS are rounded to bf16 as matrix-core operands, and P where
+// role V hands it over (fp16 would save its unpacking, 1 % of the time, and lose
+// keys with P below 1e-12); everything else is fp32 until the outputs are rounded
+// once. One of the two differences dP - D comes from the matrix cores, whose
+// accumulator starts at -D_1; the other is that plus D_1 - D_2. No atomics: the sums of dlam's partials
 // are added in a fixed order, and each output row by one workgroup.
 #include "vitattn_diff.h"
 
@@ -24,7 +27,7 @@ namespace vitattn {
 
 namespace {
 
-// Workspace: per (b, h) and block of 32 queries 128 floats, [-D_1 | -D_2 |
+// Workspace: per (b, h) and block of 32 queries 128 floats, [-D_1 | D_1 - D_2 |
 // LSE_1 log2 e | LSE_2 log2 e] of 32 each; then the partial sums of D_2,
 // [bh][row-pass workgroup]. Rows past the last query hold zeros and an LSE of
 // +inf, which makes their P zero; so do rows without keys.
@@ -79,7 +82,7 @@ __global__ __launch_bounds__(256) void diff_rowdot_kernel(const DiffArgs a, floa
       }
       float* s = st + (row >> 5) * kStat + (row & 31);
       s[0] = -d1;
-      s[32] = -d2;
+      s[32] = d1 - d2;
       s[64] = l1;
       s[96] = l2;
     }
@@ -102,14 +105,18 @@ constexpr int row_window(int NS, int half) {
 
 // ------------------------------------------------------------------ dK / dV
 //
-// Steps of 32 queries. In step j role V turns S_m(j) into P_m(j), hands it to
-// its partner, runs dV += P(j)^T dO(j) and the scores of block j + 1; role K
-// turns the P(j-1) it was handed and dP(j-1) into dS_m(j-1), runs dK_m +=
-// dS_m(j-1)^T Q_m(j-1) and dP(j). So Q and dO of blocks j-1 .. j+1 are read
-// while block j + RING - 2 is fetched into the slot of block j - 2. Block -1 and
-// the blocks past the last are zeros (P is then 0 or 1, and dO, dS and Q are
-// zero): they add nothing, and the steps group by the ring depth, so that every
-// slot is a compile-time constant.
+// Steps of 32 queries. In step j role V turns S_m(j) into P_m(j), which it hands
+// to its partner, while the matrix cores run dV += (P_1 - lam P_2)(j-1)^T dO(j-1)
+// and the scores of block j + 1. Role K turns the P(j-1) it was handed and
+// dP(j-1) into dS_m(j-1), while they run dK_m += dS_m(j-LAG)^T Q_m(j-LAG) and
+// dP(j). With a ring of six LAG is 2, and the vector work of a step feeds only
+// the next step's ops; a ring of four (the widest tile) holds one block less, so
+// dP(j) goes first there and dK follows with this step's dS. The stream of ops
+// runs through the barriers: the first two operands of a step are of blocks that
+// the step before may read already, and are read before the barrier.
+// Blocks below 0 and past the last are zeros (P is then 0 or 1, and dO, dS and Q
+// are zero): they add nothing, and the steps group by the ring depth, so that
+// every slot is a compile-time constant.
 template <int DQ, int QS, int DV, int RING, int KBW>
 __global__ __launch_bounds__(128 * KBW, KBW / 2) void diff_dkdv_kernel(const DiffArgs a,
                                                                        const float* __restrict__ stats, int n_ktiles,
@@ -212,7 +219,8 @@ __global__ __launch_bounds__(128 * KBW, KBW / 2) void diff_dkdv_kernel(const Dif
 #pragma unroll
   for (int i = 0; i < NACC; ++i) acc[i] = zero16();
 
-  constexpr int PF = RING - 2;  // blocks fetched ahead
+  constexpr int LAG = RING > 4 ? 2 : 1;
+  constexpr int PF = RING - 1 - LAG;  // blocks fetched ahead
   auto end_step = [&]() __attribute__((always_inline)) {
     // requests of the last PF - 2 steps may stay in flight
     wait_vmem_leave<(PF - 2) * (PQ + (decltype(dmg)::ALL_ACTIVE ? PG : 0))>();
@@ -230,16 +238,17 @@ __global__ __launch_bounds__(128 * KBW, KBW / 2) void diff_dkdv_kernel(const Dif
 #pragma unroll
       for (int r = 0; r < NREQ; ++r) request(T, decltype(T)::value, r);
     });
-    // block -1: zero rows (as those of block nb are) and P = 0
+    // blocks -1 and -LAG: zero rows (as those of block nb are) and P = 0
     static_for<0, NREQ>([&](auto R) __attribute__((always_inline)) {
       request(std::integral_constant<int, RING - 1>{}, nb, decltype(R)::value);
+      if constexpr (LAG > 1) request(std::integral_constant<int, RING - LAG>{}, nb, decltype(R)::value);
     });
     if (!role_v)
 #pragma unroll
       for (int i = 0; i < 4; ++i) xbuf1[kb][i >> 1][i & 1][lane] = make_uint4(0, 0, 0, 0);
     wait_vmem();
     __syncthreads();
-    const int n_pad = (nb + RING) / RING * RING;  // at least one step past the last block, for role K
+    const int n_pad = (nb + LAG + RING - 1) / RING * RING;  // LAG steps past the last block
 
     if (role_v) {
       f32x16 sa[2], sb[2];  // scores of the current and the next block, per map
@@ -248,15 +257,20 @@ __global__ __launch_bounds__(128 * KBW, KBW / 2) void diff_dkdv_kernel(const Dif
         if (i < 2) sa[i] = zero16();
         sa[i & 1] = mfma32(lds_frag_row(qbuf[0] + (i & 1) * QT, rfq.at(i >> 1)), hf[(i & 1) * QS + (i >> 1)], sa[i & 1]);
       }
+      bf16x8 ob[2] = {};          // P_1 - lam P_2 of the block before
+      bf16x8 lead[2];             // the next step's first two operands
+      auto load_v = [&](const char* g, int t) -> bf16x8 { return tfg.load(g, 16 * (t / NCV), t % NCV); };
+      lead[0] = load_v(gbuf[RING - 1], 0);
+      lead[1] = load_v(gbuf[RING - 1], 1);
       auto step = [&](auto slot_tag, f32x16 (&cur)[2], f32x16 (&nxt)[2], int j) __attribute__((always_inline)) {
         constexpr int SL = decltype(slot_tag)::value;
-        constexpr int NX = (SL + 1) % RING, RF = (SL + PF) % RING;
-        constexpr int NS = 2 * QS, NV = 2 * NCV, NOPS = NS + NV, W = row_window(NS, NCV);
+        constexpr int PR = (SL + RING - 1) % RING, NX = (SL + 1) % RING, RF = (SL + PF) % RING;
+        constexpr int NS = 2 * QS, NV = 2 * NCV, NOPS = NV + NS;
         constexpr int STEP = 2 * NREQ <= NOPS ? 2 : 1;
         static_assert(STEP * NREQ <= NOPS, "requests fit the op stream");
         const float* st = sbuf[SL];
         uint4(*xb)[2][64] = (SL & 1) ? xbuf1[kb] : xbuf0[kb];
-        bf16x8 ob[2];
+        bf16x8 on[2];
         float4 l1[4], l2[4];
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
@@ -276,36 +290,39 @@ __global__ __launch_bounds__(128 * KBW, KBW / 2) void diff_dkdv_kernel(const Dif
           if constexpr ((r & 7) == 7) {
             xb[0][r >> 3][lane] = __builtin_bit_cast(uint4, acc_to_operand(cur[0], r >> 3));
             xb[1][r >> 3][lane] = __builtin_bit_cast(uint4, acc_to_operand(cur[1], r >> 3));
-            ob[r >> 3] = acc_to_operand(wv, r >> 3);
+            on[r >> 3] = acc_to_operand(wv, r >> 3);
           }
         };
         auto load_op = [&](int i) -> bf16x8 {
-          if (i < NS) return lds_frag_row(qbuf[NX] + (i & 1) * QT, rfq.at(i >> 1));
-          const int t = i - NS;
-          return tfg.load(gbuf[SL], 16 * (t / NCV), t % NCV);
+          if (i < NV) return load_v(gbuf[PR], i);
+          if (i < NOPS) return lds_frag_row(qbuf[NX] + ((i - NV) & 1) * QT, rfq.at((i - NV) >> 1));
+          return load_v(gbuf[SL], i - NOPS);
         };
         bf16x8 aq[3];
-        aq[0] = load_op(0);
-        aq[1] = load_op(1);
+        aq[0] = lead[0];
+        aq[1] = lead[1];
         sched_fence();
         static_for<0, NOPS>([&](auto IC) __attribute__((always_inline)) {
           constexpr int i = decltype(IC)::value;
           if constexpr (i == 0) __builtin_amdgcn_s_setprio(1);
-          if constexpr (i == W) __builtin_amdgcn_s_setprio(0);
           if constexpr (i + 2 < NOPS) aq[(i + 2) % 3] = load_op(i + 2);
-          if constexpr (i < NS) {
-            if constexpr (i < 2) nxt[i] = zero16();
-            nxt[i & 1] = mfma32(aq[i % 3], hf[(i & 1) * QS + (i >> 1)], nxt[i & 1]);
+          else lead[i + 2 - NOPS] = load_op(i + 2);
+          if constexpr (i < NV) {
+            acc[i % NCV] = mfma32(aq[i % 3], ob[i / NCV], acc[i % NCV]);
           } else {
-            constexpr int t = i - NS;
-            acc[t % NCV] = mfma32(aq[i % 3], ob[t / NCV], acc[t % NCV]);
+            constexpr int t = i - NV;
+            if constexpr (t < 2) nxt[t] = zero16();
+            nxt[t & 1] = mfma32(aq[i % 3], hf[(t & 1) * QS + (t >> 1)], nxt[t & 1]);
           }
           if constexpr (i % STEP == STEP - 1 && i / STEP < NREQ) request(std::integral_constant<int, RF>{}, j + PF, i / STEP);
           static_for<0, 16>([&](auto RC) __attribute__((always_inline)) {
-            if constexpr (decltype(RC)::value * W / 16 == i) row(RC);
+            if constexpr (decltype(RC)::value * NOPS / 16 == i) row(RC);
           });
           sched_fence();
         });
+        __builtin_amdgcn_s_setprio(0);
+        ob[0] = on[0];
+        ob[1] = on[1];
         end_step();
       };
       for (int j = 0; j < n_pad; j += RING) {
@@ -320,26 +337,32 @@ __global__ __launch_bounds__(128 * KBW, KBW / 2) void diff_dkdv_kernel(const Dif
       }
     } else {
       f32x16 da, db = zero16();  // dP of the current (j - 1) and the next block
+      bf16x8 ob[2][2] = {};      // dS, [map][step], of the block before
+      bf16x8 lead[2];
+      // dK op t: contraction step t / (2 NCQ), map, column block
+      auto load_k = [&](const char* q, int t) -> bf16x8 {
+        const int u = t % (2 * NCQ);
+        return tfq.load(q + (u / NCQ) * QT, 16 * (t / (2 * NCQ)), u % NCQ);
+      };
+#pragma unroll
+      for (int t = 0; t < 2; ++t) lead[t] = LAG > 1 ? load_k(qbuf[RING - LAG], t) : lds_frag_row(gbuf[0], rfg.at(t));
       auto step = [&](auto slot_tag, f32x16& cur, f32x16& nxt, int j) __attribute__((always_inline)) {
         constexpr int SL = decltype(slot_tag)::value;  // of block j
-        constexpr int PR = (SL + RING - 1) % RING, RF = (SL + PF) % RING;
-        constexpr int NS = VS, NK = 4 * NCQ, NOPS = NS + NK, W = row_window(NS, 2 * NCQ);
+        constexpr int PR = (SL + RING - 1) % RING, KR = (SL + RING - LAG) % RING, RF = (SL + PF) % RING;
+        constexpr int NS = VS, NK = 4 * NCQ, NOPS = NS + NK;
+        constexpr int K0 = LAG > 1 ? 0 : NS, P0 = LAG > 1 ? NK : 0;  // first dK and dP op
         constexpr int STEP = 2 * NREQ <= NOPS ? 2 : 1;
         static_assert(STEP * NREQ <= NOPS, "requests fit the op stream");
-        const float* st = sbuf[PR];
         uint4(*xb)[2][64] = (SL & 1) ? xbuf0[kb] : xbuf1[kb];  // of block j - 1
-        bf16x8 ob[2][2];  // [map][step]
+        bf16x8 on[2][2];
         uint4 pm[2][2];
-        float4 d1[4], d2[4];
+        float4 dd[4];  // D_1 - D_2
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int s = 0; s < 2; ++s) pm[m][s] = xb[m][s][lane];
+          for (int m = 0; m < 2; ++m) pm[m][s] = xb[m][s][lane];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          d1[g] = *reinterpret_cast<const float4*>(st + 8 * g + 4 * h);
-          d2[g] = *reinterpret_cast<const float4*>(st + 32 + 8 * g + 4 * h);
-        }
+        for (int g = 0; g < 4; ++g) dd[g] = *reinterpret_cast<const float4*>(sbuf[PR] + 32 + 8 * g + 4 * h);
         f32x16 s1, s2;
         auto row = [&](auto RC) __attribute__((always_inline)) {
           constexpr int r = decltype(RC)::value;
@@ -348,45 +371,62 @@ __global__ __launch_bounds__(128 * KBW, KBW / 2) void diff_dkdv_kernel(const Dif
             const uint32_t w = w4[(r & 7) >> 1];
             return __uint_as_float((r & 1) ? (w & 0xffff0000u) : (w << 16));
           };
-          float x1 = p_of(0) * (cur[r] + d1[r >> 2][r & 3]);
-          float x2 = p_of(1) * (cur[r] + d2[r >> 2][r & 3]);
+          float x1 = p_of(0) * cur[r];
+          float x2 = p_of(1) * (cur[r] + dd[r >> 2][r & 3]);
           pin(x1);
           pin(x2);
           s1[r] = x1;
           s2[r] = x2;
           if constexpr ((r & 7) == 7) {
-            ob[0][r >> 3] = acc_to_operand(s1, r >> 3);
-            ob[1][r >> 3] = acc_to_operand(s2, r >> 3);
+            on[0][r >> 3] = acc_to_operand(s1, r >> 3);
+            on[1][r >> 3] = acc_to_operand(s2, r >> 3);
           }
         };
-        // dK op t: step t / (2 NCQ), map, column block
+        // the op on which row r rides: over the whole step behind the first two
+        // ops, whose time the handed P needs, or as ROW_W says
+        constexpr auto op_of = [](int r) { return LAG > 1 ? 2 + r * (NOPS - 2) / 16 : r * row_window(NS, 2 * NCQ) / 16; };
         auto load_op = [&](int i) -> bf16x8 {
-          if (i < NS) return lds_frag_row(gbuf[SL], rfg.at(i));
-          const int t = i - NS, u = t % (2 * NCQ);
-          return tfq.load(qbuf[PR] + (u / NCQ) * QT, 16 * (t / (2 * NCQ)), u % NCQ);
+          if (i >= NOPS) return LAG > 1 ? load_k(qbuf[PR], i - NOPS) : lds_frag_row(gbuf[(SL + 1) % RING], rfg.at(i - NOPS));
+          return i >= K0 && i < K0 + NK ? load_k(qbuf[KR], i - K0) : lds_frag_row(gbuf[SL], rfg.at(i - P0));
         };
         bf16x8 aq[3];
-        aq[0] = load_op(0);
-        aq[1] = load_op(1);
+        aq[0] = lead[0];
+        aq[1] = lead[1];
         sched_fence();
         static_for<0, NOPS>([&](auto IC) __attribute__((always_inline)) {
           constexpr int i = decltype(IC)::value;
           if constexpr (i == 0) __builtin_amdgcn_s_setprio(1);
-          if constexpr (i == W) __builtin_amdgcn_s_setprio(0);
           if constexpr (i + 2 < NOPS) aq[(i + 2) % 3] = load_op(i + 2);
-          if constexpr (i < NS) {
-            if constexpr (i == 0) nxt = zero16();
-            nxt = mfma32(aq[i % 3], hf[i], nxt);
+          else lead[i + 2 - NOPS] = load_op(i + 2);
+          if constexpr (i >= K0 && i < K0 + NK) {
+            constexpr int t = i - K0, u = t % (2 * NCQ);
+            if constexpr (LAG > 1) acc[u] = mfma32(aq[i % 3], ob[u / NCQ][t / (2 * NCQ)], acc[u]);
+            else acc[u] = mfma32(aq[i % 3], on[u / NCQ][t / (2 * NCQ)], acc[u]);
           } else {
-            constexpr int t = i - NS, u = t % (2 * NCQ);
-            acc[u] = mfma32(aq[i % 3], ob[u / NCQ][t / (2 * NCQ)], acc[u]);
+            constexpr int t = i - P0;
+            if constexpr (t == 0) {  // starts at -D_1 of its rows
+#pragma unroll
+              for (int g = 0; g < 4; ++g) {
+                const float4 x = *reinterpret_cast<const float4*>(sbuf[SL] + 8 * g + 4 * h);
+                nxt[4 * g] = x.x;
+                nxt[4 * g + 1] = x.y;
+                nxt[4 * g + 2] = x.z;
+                nxt[4 * g + 3] = x.w;
+              }
+            }
+            nxt = mfma32(aq[i % 3], hf[t], nxt);
           }
           if constexpr (i % STEP == STEP - 1 && i / STEP < NREQ) request(std::integral_constant<int, RF>{}, j + PF, i / STEP);
           static_for<0, 16>([&](auto RC) __attribute__((always_inline)) {
-            if constexpr (decltype(RC)::value * W / 16 == i) row(RC);
+            if constexpr (op_of(decltype(RC)::value) == i) row(RC);
           });
           sched_fence();
         });
+        __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) ob[m][x] = on[m][x];
         end_step();
       };
       for (int j = 0; j < n_pad; j += RING) {
@@ -510,7 +550,16 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void diff_dq_kernel(const DiffArgs
     return __builtin_bit_cast(
         float, __builtin_amdgcn_raw_buffer_load_b32(rs, ((qrow >> 5) * kStat + 32 * which + (qrow & 31)) * 4, 0, 0));
   };
-  const float nd1 = stat(0), nd2 = stat(1), l1 = stat(2), l2 = stat(3);
+  const float l1 = stat(2), l2 = stat(3), dd = stat(1);
+  const float nd1 = stat(0);
+  constexpr bool START = DV < 160;  // dP starts at -D_1 (the widest tile has no registers to hold that)
+  f32x16 start;
+  if constexpr (START) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) start[r] = nd1;
+  } else {
+    start = zero16();
+  }
 
   const rsrc_t rk1 = make_rsrc(a.k + map_head(a.mk, b, head, 0), (unsigned)(Nk * ldk));
   const rsrc_t rk2 = make_rsrc(a.k + map_head(a.mk, b, head, 1), (unsigned)(Nk * ldk));
@@ -571,8 +620,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void diff_dq_kernel(const DiffArgs
         if constexpr (i < 2) s[i] = zero16();
         s[i & 1] = mfma32(aq[i % 3], qf[i & 1][i >> 1], s[i & 1]);
       } else {
-        if constexpr (i == 2 * QS) dp = zero16();
-        dp = mfma32(aq[i % 3], gf[i - 2 * QS], dp);
+        dp = mfma32(aq[i % 3], gf[i - 2 * QS], i == 2 * QS ? start : dp);
         static_for<0, 16>([&](auto RC) __attribute__((always_inline)) {
           constexpr int r = decltype(RC)::value;
           if constexpr (r * W / 16 == i - 2 * QS) {
@@ -594,8 +642,9 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void diff_dq_kernel(const DiffArgs
         if (j * BN + acc_row(r, h) >= Nk) s[0][r] = s[1][r] = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      s[0][r] *= dp[r] + nd1;
-      s[1][r] *= dp[r] + nd2;
+      const float x = START ? dp[r] : dp[r] + nd1;
+      s[0][r] *= x;
+      s[1][r] *= x + dd;
     }
     bf16x8 ob[2][2];
 #pragma unroll
