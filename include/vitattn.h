@@ -497,8 +497,8 @@ int vitattn_rotary(const void* q, vitattn_strides sq, void* q_out, vitattn_strid
  *              key_lens are zeros); dlam: [H] of lam_type, or null.
  *   d, e     : multiples of 8 up to VITATTN_DIFF_MAX_D and VITATTN_DIFF_MAX_E
  *              (e = 2 d is the usual choice), else VITATTN_E_UNSUPPORTED. The
- *              kernels compute in tiles of width 64 (d up to 64) or 96, and 64,
- *              128 or 160 (e), columns past d and e zero.
+ *              kernels compute in tiles of width (d, e) = (32, 64), (64, 64),
+ *              (64, 128) or (96, 160), columns past d and e zero.
  *   strides  : as for vitattn_fwd_strided (2H heads for q, k, dq and dk), with
  *              (rows + 512) * row * 2 < 2^31. Outputs must not alias inputs.
  *   sizes    : B*H*(max(Nq, Nk) + 512) below 2^30.

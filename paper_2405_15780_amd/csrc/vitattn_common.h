@@ -17,7 +17,7 @@
 // LDS tiles are row-major [rows][D] bf16 with the 16-byte chunks of row r
 // XOR-swizzled by swz(r), so that both the row-fragment reads (32 rows x one
 // chunk) and the transposing reads (8 rows x 4 chunks) touch every bank
-// equally often. The tile width D is 64, 96, 128 or 160; a head dim d below
+// equally often. The tile width D is 32, 64, 96, 128 or 160; a head dim d below
 // D occupies the first d columns and the rest of each row holds zeros.
 #pragma once
 
@@ -52,14 +52,14 @@ __device__ __forceinline__ f32x16 zero16() {
 __device__ __forceinline__ bf16x8 as_bf16x8(uint4 u) { return __builtin_bit_cast(bf16x8, u); }
 
 // Swizzled byte offset of 16-byte chunk c of row r in a [rows][D] bf16 tile.
-// D = 128 and 64: 16 consecutive rows of one chunk cover all 64 banks. D = 96
-// and 160 (rows of 192 and 320 bytes): four consecutive rows already start in
+// D = 128 and 64: 16 consecutive rows of one chunk cover all 64 banks. D = 32,
+// 96 and 160 (rows of 64, 192 and 320 bytes): four consecutive rows already start in
 // four different 64-byte bank groups, so the swizzle permutes chunks only
 // within their aligned group of four (never past the end of the row) and
 // varies with rows 4 apart.
 template <int D>
 __device__ __forceinline__ int swz(int r) {
-  static_assert(D == 64 || D == 96 || D == 128 || D == 160, "tile width");
+  static_assert(D == 32 || D == 64 || D == 96 || D == 128 || D == 160, "tile width");
   if constexpr (D == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
   else if constexpr (D == 64) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
   else return (r >> 2) & 3;
@@ -79,7 +79,7 @@ __device__ __forceinline__ bf16x8 lds_frag_row(const char* lds, int off) {
 // Tile widths whose swizzle permutes chunks within aligned groups of four:
 // moving a fragment by one group (64 bytes) is then a plain constant offset.
 template <int D>
-constexpr bool kGrouped = (D == 96 || D == 160);
+constexpr bool kGrouped = (D == 32 || D == 96 || D == 160);
 
 // Per-lane offsets of the row fragments of rows r0 + l%32 (r0 a multiple of
 // 32, added by the caller as r0 * 2D), for every kk = 0 .. D/16 - 1. For the

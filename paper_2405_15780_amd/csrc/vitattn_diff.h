@@ -29,7 +29,7 @@ struct DiffTile {
   int dq, qs, dv;
 };
 inline DiffTile diff_tile(int d, int e) {
-  if (d <= 32 && e <= 64) return {64, 2, 64};
+  if (d <= 32 && e <= 64) return {32, 2, 64};
   if (d <= 64 && e <= 64) return {64, 4, 64};
   if (d <= 64 && e <= 128) return {64, 4, 128};
   return {96, 5, 160};

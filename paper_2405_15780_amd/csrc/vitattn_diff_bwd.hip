@@ -13,7 +13,8 @@
 //      and accumulates dV from P_1 - lam P_2, role K holds V, takes the P it is
 //      handed through LDS, forms both dS and accumulates dK_1 and dK_2. At
 //      e = 2 d both have 16 matrix ops per 32 x 32 block.
-//   3. dQ kernel: 32 queries per wave, Q_1, Q_2 and dO held; streams K_1, K_2, V.
+//   3. dQ kernel: 32 queries per wave, four waves, Q_1, Q_2 and dO held; streams
+//      K_1, K_2 and V.
 //
 // P_1 - lam P_2 and dS are rounded to bf16 as matrix-core operands, and P where
 // role V hands it over (fp16 would save its unpacking, 1 % of the time, and lose
@@ -33,6 +34,7 @@ namespace {
 // +inf, which makes their P zero; so do rows without keys.
 constexpr int kStat = 128;
 constexpr int kRowBlock = 64;  // query rows of a row-pass workgroup
+constexpr int kKeyBlock = 128;  // keys of a wide dK/dV workgroup, or of two narrow ones
 
 __host__ __device__ constexpr int query_blocks(int Nq) { return (Nq + 31) / 32; }
 __host__ __device__ constexpr int row_groups(int Nq) { return (Nq + kRowBlock - 1) / kRowBlock; }
@@ -117,11 +119,13 @@ constexpr int row_window(int NS, int half) {
 // Blocks below 0 and past the last are zeros (P is then 0 or 1, and dO, dS and Q
 // are zero): they add nothing, and the steps group by the ring depth, so that
 // every slot is a compile-time constant.
+// (four-wave workgroups of the wider tiles have a CU's LDS, and its registers, alone)
 template <int DQ, int QS, int DV, int RING, int KBW>
-__global__ __launch_bounds__(128 * KBW, KBW / 2) void diff_dkdv_kernel(const DiffArgs a,
+__global__ __launch_bounds__(128 * KBW, KBW == 2 && DV > 64 ? 1 : 2) void diff_dkdv_kernel(const DiffArgs a,
                                                                        const float* __restrict__ stats, int n_ktiles,
-                                                                       int total, float c) {
-  constexpr int NW = 2 * KBW, BK = 32 * KBW, BQ = 32;
+                                                                       int first, int total, float c) {
+  constexpr int NW = 2 * KBW, BQ = 32;
+  constexpr int PARTS = kKeyBlock / (32 * KBW);  // workgroups of a block of keys
   constexpr int VS = DV / 16, NCV = DV / 32;
   constexpr int NCQ = (QS + 1) / 2;  // 32-column blocks of d that may hold data
   constexpr int QT = BQ * DQ * 2, GT = BQ * DV * 2;
@@ -152,14 +156,14 @@ __global__ __launch_bounds__(128 * KBW, KBW / 2) void diff_dkdv_kernel(const Dif
   debug_poison_lds(qbuf0, qbuf1, qbuf2, qbuf3, qbuf4, qbuf5, gbuf0, gbuf1, gbuf2, gbuf3, gbuf4, gbuf5, sbuf0, sbuf1,
                    sbuf2, sbuf3, sbuf4, sbuf5, xbuf0, xbuf1);
 
-  const int work = xcd_remap(blockIdx.x, total);
-  const int bh = work / n_ktiles, kt = work - bh * n_ktiles;
+  const int work = xcd_remap(blockIdx.x, total), block = first + work / PARTS;
+  const int bh = block / n_ktiles, key_first = (block - bh * n_ktiles) * kKeyBlock + (work % PARTS) * 32 * KBW;
   const int b = bh / a.H, head = bh - b * a.H;
   const int lane = threadIdx.x & 63, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kb = wave % KBW;
   const bool role_v = wave < KBW;
-  const int key = kt * BK + kb * 32 + (lane & 31);
+  const int key = key_first + kb * 32 + (lane & 31);
   const int Nk = keys_of(a.key_lens, b, a.Nk);
   const float lam = lam_of(a.lam, a.lam_bf16, head);
 
@@ -223,11 +227,11 @@ __global__ __launch_bounds__(128 * KBW, KBW / 2) void diff_dkdv_kernel(const Dif
   constexpr int PF = RING - 1 - LAG;  // blocks fetched ahead
   auto end_step = [&]() __attribute__((always_inline)) {
     // requests of the last PF - 2 steps may stay in flight
-    wait_vmem_leave<(PF - 2) * (PQ + (decltype(dmg)::ALL_ACTIVE ? PG : 0))>();
+    wait_vmem_leave<(PF - 2) * ((decltype(dmq)::ALL_ACTIVE ? PQ : 0) + (decltype(dmg)::ALL_ACTIVE ? PG : 0))>();
     barrier_lds();
   };
 
-  if (kt * BK < Nk) {  // else every key of this workgroup is past the sample's last: zeros
+  if (key_first < Nk) {  // else every key of this workgroup is past the sample's last: zeros
     using S0 = std::integral_constant<int, 0>;
     using S1 = std::integral_constant<int, 1>;
     using S2 = std::integral_constant<int, 2>;
@@ -484,14 +488,14 @@ __global__ __launch_bounds__(128 * KBW, KBW / 2) void diff_dkdv_kernel(const Dif
 // LSE far below zero would make exp overflow). The workgroup of query tile 0 of
 // sample 0 also adds its head's partial sums of dlam.
 template <int DQ, int QS, int DV, int RING, int NW>
-__global__ __launch_bounds__(64 * NW, NW / 4) void diff_dq_kernel(const DiffArgs a, const float* __restrict__ stats,
+__global__ __launch_bounds__(64 * NW, DV > 128 ? 1 : 2) void diff_dq_kernel(const DiffArgs a, const float* __restrict__ stats,
                                                                   const float* __restrict__ partial, int groups,
                                                                   int n_qtiles, int total, float c) {
   constexpr int BM = 32 * NW, BN = 32;
   constexpr int VS = DV / 16;
   constexpr int NCQ = (QS + 1) / 2;
   constexpr int KT = BN * DQ * 2, VT = BN * DV * 2;
-  static_assert(RING == 4, "ring depth");
+  static_assert(RING == 4, "one variable per slot");
   __shared__ __attribute__((aligned(1024))) char kbuf0[2 * KT];
   __shared__ __attribute__((aligned(1024))) char kbuf1[2 * KT];
   __shared__ __attribute__((aligned(1024))) char kbuf2[2 * KT];
@@ -686,16 +690,46 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void diff_dq_kernel(const DiffArgs
   }
 }
 
+// `parts` workgroups for each of n blocks of keys from `first` on
+template <int DQ, int QS, int DV, int RING, int KBW>
+hipError_t go_dkdv(const DiffArgs& a, const float* stats, int first, int n) {
+  if (n == 0) return hipSuccess;
+  const int total = n * (kKeyBlock / (32 * KBW));
+  diff_dkdv_kernel<DQ, QS, DV, RING, KBW><<<total, 128 * KBW, 0, a.stream>>>(
+      a, stats, (a.Nk + kKeyBlock - 1) / kKeyBlock, first, total, a.scale * kLog2e);
+  return hipGetLastError();
+}
+
+// One wide workgroup is on a CU at a time. A narrow one (64 keys) takes 0.74-0.85
+// of its time alone on a CU, and 1.0-1.4 of it for two (N = 256 .. 16,384, every
+// tile): blocks left over by whole rounds go to narrow workgroups if these are at
+// most one per CU. Of the narrowest tile three fit on a CU, and take 0.83-1.08
+// (0.86-1.0 over many rounds): all of its blocks go to them. Each key's operations
+// are the same in both.
+template <int DQ, int QS, int DV, int RING>
+hipError_t launch_dkdv(const DiffArgs& a, const float* stats) {
+  const int n = a.B * a.H * ((a.Nk + kKeyBlock - 1) / kKeyBlock);
+  if constexpr (DQ == 32) {
+    return go_dkdv<DQ, QS, DV, 4, 2>(a, stats, 0, n);
+  } else {
+    static ResidentCache cache;
+    const int cus = cache.get(reinterpret_cast<const void*>(diff_dkdv_kernel<DQ, QS, DV, RING, 4>), 512).cus;
+    int narrow = cus > 0 ? n % cus : 0;
+    if (2 * narrow > cus || n - narrow > 8 * cus) narrow = 0;
+    const hipError_t err = go_dkdv<DQ, QS, DV, RING, 4>(a, stats, 0, n - narrow);
+    return err != hipSuccess ? err : go_dkdv<DQ, QS, DV, 4, 2>(a, stats, n - narrow, narrow);
+  }
+}
+
 template <int DQ, int QS, int DV, int RING>
 hipError_t go_tile(const DiffArgs& a, const float* stats, const float* partial, int groups) {
-  const float c = a.scale * kLog2e;
-  constexpr int KBW = 4, NW = 8;
-  const int n_ktiles = (a.Nk + 32 * KBW - 1) / (32 * KBW), kv = a.B * a.H * n_ktiles;
-  diff_dkdv_kernel<DQ, QS, DV, RING, KBW><<<kv, 128 * KBW, 0, a.stream>>>(a, stats, n_ktiles, kv, c);
-  const hipError_t err = hipGetLastError();
+  const hipError_t err = launch_dkdv<DQ, QS, DV, RING>(a, stats);
   if (err != hipSuccess) return err;
-  const int n_qtiles = (a.Nq + 32 * NW - 1) / (32 * NW), qs = a.B * a.H * n_qtiles;
-  diff_dq_kernel<DQ, QS, DV, 4, NW><<<qs, 64 * NW, 0, a.stream>>>(a, stats, partial, groups, n_qtiles, qs, c);
+  // workgroups of four waves: 0.44-1.02 of the time of eight (N = 256 .. 16,384)
+  constexpr int NW = 4;
+  const int n_qtiles = (a.Nq + 32 * NW - 1) / (32 * NW), total = a.B * a.H * n_qtiles;
+  diff_dq_kernel<DQ, QS, DV, 4, NW>
+      <<<total, 64 * NW, 0, a.stream>>>(a, stats, partial, groups, n_qtiles, total, a.scale * kLog2e);
   return hipGetLastError();
 }
 
@@ -719,7 +753,7 @@ hipError_t launch_diff_bwd(const DiffArgs& a) {
   const DiffTile t = diff_tile(a.d, a.e);
   if (t.dq == 96) return go_tile<96, 5, 160, 4>(a, stats, partial, groups);
   if (t.dv == 128) return go_tile<64, 4, 128, 6>(a, stats, partial, groups);
-  return t.qs == 2 ? go_tile<64, 2, 64, 6>(a, stats, partial, groups) : go_tile<64, 4, 64, 6>(a, stats, partial, groups);
+  return t.dq == 32 ? go_tile<32, 2, 64, 6>(a, stats, partial, groups) : go_tile<64, 4, 64, 6>(a, stats, partial, groups);
 }
 
 }  // namespace vitattn

@@ -58,10 +58,15 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
   __shared__ __attribute__((aligned(1024))) char kbuf1[2 * KT];
   __shared__ __attribute__((aligned(1024))) char vbuf0[VT];
   __shared__ __attribute__((aligned(1024))) char vbuf1[VT];
-  __shared__ float xbuf[QW][16][64];  // the second map's outputs, 32 columns at a time
+  // The second map's outputs, 32 columns at a time: over the K tiles where these
+  // are large enough (no wave reads K in the last stage), which leaves a CU room
+  // for another workgroup.
+  constexpr bool OVER_K = 2 * KT >= QW * 4096;
+  __shared__ float xown[OVER_K ? 1 : QW][16][64];
   char* const kbuf[2] = {kbuf0, kbuf1};
   char* const vbuf[2] = {vbuf0, vbuf1};
-  debug_poison_lds(kbuf0, kbuf1, vbuf0, vbuf1, xbuf);
+  debug_poison_lds(kbuf0, kbuf1, vbuf0, vbuf1, xown);
+  float(*const xbuf)[16][64] = OVER_K ? reinterpret_cast<float(*)[16][64]>(kbuf0) : xown;
 
   const int work = xcd_remap(blockIdx.x, total);
   const int part = work / n_qtiles;
@@ -428,10 +433,32 @@ hipError_t go(const DiffArgs& a, int split_keys, int n_split) {
   return hipGetLastError();
 }
 
+// Query waves of a workgroup, four (128 queries) or two. Of two of the wider tiles
+// two workgroups fit on a CU: they take 1.0-1.06 of the wide one's time, and one
+// alone 0.75-0.85 (N = 256 .. 16,384), so two are taken where they are one per CU
+// or fill the last round better. Of e <= 64 three fit, and take 0.75-1.07 (0.82-
+// 0.97 over many rounds up to N = 4,096, 0.97-1.03 at 16,384): always two there.
+// A row's operations are the same in both.
+template <int DQ, int QS, int DV, int KB>
+bool two_query_waves(const DiffArgs& a) {
+  if (a.Nq <= 64) return true;
+  static ResidentCache cache;
+  const int cus = cache.get(reinterpret_cast<const void*>(diff_fwd_kernel<DQ, QS, DV, KB, 4, false>), 512).cus;
+  if (cus <= 0) return false;
+  const long long wide = (long long)a.B * a.H * ((a.Nq + 127) / 128), narrow = (long long)a.B * a.H * ((a.Nq + 63) / 64);
+  const long long left = narrow % (2 * cus);
+  const double two = 1.04 * (narrow / (2 * cus)) + (left == 0 ? 0. : left <= cus ? 0.8 : 1.04);
+  return two < (double)((wide + cus - 1) / cus);
+}
+
 template <int DQ, int QS, int DV, int KB>
 hipError_t go_tile(const DiffArgs& a) {
   const int split_keys = diff_split_keys(a.Nq, a.Nk);
-  if (split_keys == 0) return a.Nq <= 64 ? go<DQ, QS, DV, KB, 2, false>(a, 0, 1) : go<DQ, QS, DV, KB, 4, false>(a, 0, 1);
+  if (split_keys == 0) {
+    if constexpr (DV > 64)
+      if (!two_query_waves<DQ, QS, DV, KB>(a)) return go<DQ, QS, DV, KB, 4, false>(a, 0, 1);
+    return go<DQ, QS, DV, KB, 2, false>(a, 0, 1);
+  }
   const int n_split = (a.Nk + split_keys - 1) / split_keys;
   const hipError_t err = go<DQ, QS, DV, KB, 2, true>(a, split_keys, n_split);
   if (err != hipSuccess) return err;
@@ -456,7 +483,7 @@ hipError_t launch_diff_fwd(const DiffArgs& a) {
   const DiffTile t = diff_tile(a.d, a.e);
   if (t.dq == 96) return go_tile<96, 5, 160, 1>(a);
   if (t.dv == 128) return go_tile<64, 4, 128, 2>(a);
-  return t.qs == 2 ? go_tile<64, 2, 64, 2>(a) : go_tile<64, 4, 64, 2>(a);
+  return t.dq == 32 ? go_tile<32, 2, 64, 2>(a) : go_tile<64, 4, 64, 2>(a);
 }
 
 }  // namespace vitattn
