@@ -13,10 +13,7 @@ from __future__ import annotations
 from . import binding as _b
 
 
-def _torch():
-    import torch
-
-    return torch
+_torch = _b._torch
 
 
 class _Attention:
@@ -88,7 +85,12 @@ class _LayerNorm:
 
 
 def _wants_grad(*ts):
-    return _torch().is_grad_enabled() and any(t is not None and t.requires_grad for t in ts)
+    if not _torch().is_grad_enabled():
+        return False
+    for t in ts:
+        if t is not None and t.requires_grad:
+            return True
+    return False
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
@@ -177,8 +179,9 @@ def diff_attention(q, k, v, lam, scale=None, key_lens=None):
     and 2h + 1 are the two maps of head h), v [B,H,Nk,e], lam [H] or one value for
     all heads (fp32 or bf16); scale defaults to 1/sqrt(d). key_lens (int32 [B]):
     sample b attends to its first key_lens[b] keys. Returns o, bf16 [B,H,Nq,e]."""
-    if lam.numel() == 1 and lam.shape != (v.shape[1],):
-        lam = lam.reshape(1).expand(v.shape[1])
+    if lam.dim() != 1 or lam.numel() != v.shape[1]:
+        if lam.numel() == 1:
+            lam = lam.reshape(1).expand(v.shape[1])
     lam = lam.contiguous()
     if not _wants_grad(q, k, v, lam):
         return _b.diff_fwd(q, k, v, lam, scale, key_lens, save=False)[0]

@@ -8,6 +8,7 @@ VitattnError on a non-zero status.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 import threading
@@ -124,15 +125,24 @@ def _check(status: int):
         raise VitattnError(status)
 
 
+@functools.lru_cache(maxsize=None)
 def _torch():
     import torch
 
     return torch
 
 
-def _stream_ptr(t) -> int:
+@functools.lru_cache(maxsize=None)
+def _raw_stream():
+    """The current stream's handle by device index (without making a Stream of
+    it, where torch offers that: 0.1 us instead of 1.9)."""
     torch = _torch()
-    return torch.cuda.current_stream(t.device).cuda_stream
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _stream_ptr(t) -> int:
+    return _raw_stream()(t.device.index)
 
 
 def _as_input(t, name, device=None):
@@ -546,29 +556,34 @@ VITATTN_BF16, VITATTN_FP16, VITATTN_FP32 = 0, 1, 2
 VITATTN_ROTARY_INTERLEAVED, VITATTN_ROTARY_INVERSE, VITATTN_ROTARY_JOINT = 1, 2, 4
 
 
-def _type_code(t, name, allowed):
+_ALL_TYPES, _LAM_TYPES = (VITATTN_BF16, VITATTN_FP16, VITATTN_FP32), (VITATTN_BF16, VITATTN_FP32)
+
+
+@functools.lru_cache(maxsize=None)
+def _type_codes():
     torch = _torch()
-    codes = {torch.bfloat16: VITATTN_BF16, torch.float16: VITATTN_FP16, torch.float32: VITATTN_FP32}
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or codes.get(t.dtype) not in allowed:
-        names = ", ".join(str(d) for d, c in codes.items() if c in allowed)
+    return {torch.bfloat16: VITATTN_BF16, torch.float16: VITATTN_FP16, torch.float32: VITATTN_FP32}
+
+
+def _type_code(t, name, allowed=_ALL_TYPES):
+    code = _type_codes().get(t.dtype) if isinstance(t, _torch().Tensor) and t.is_cuda else None
+    if code is None or code not in allowed:
+        names = ", ".join(str(d) for d, c in _type_codes().items() if c in allowed)
         raise TypeError(f"{name} must be a CUDA tensor of one of {names}")
-    return codes[t.dtype]
+    return code
 
 
-class _on_device:
-    """The tensor's device made current for a call (nothing if it is)."""
-
-    def __init__(self, t):
-        torch = _torch()
-        self._ctx = None if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
-
-    def __enter__(self):
-        if self._ctx is not None:
-            self._ctx.__enter__()
-
-    def __exit__(self, *a):
-        if self._ctx is not None:
-            self._ctx.__exit__(*a)
+def _call(t, fn, *args):
+    """fn(*args, stream) on t's device and its current stream."""
+    device = t.device.index
+    cuda = _torch().cuda
+    if device == cuda.current_device():
+        status = fn(*args, _raw_stream()(device))
+    else:
+        with cuda.device(device):
+            status = fn(*args, _raw_stream()(device))
+    if status != 0:
+        raise VitattnError(status)
 
 
 def plain_memory(t):
@@ -582,10 +597,10 @@ def plain_memory(t):
 def _norm_view(t, name):
     """t as the rows of a layer norm; more than three leading dims become one (by
     a copy where t's layout needs it)."""
-    _type_code(t, name, (VITATTN_BF16, VITATTN_FP16, VITATTN_FP32))
-    if t.dim() < 1 or (t.shape[-1] != 1 and t.stride(-1) != 1):
+    n = t.dim()
+    if n < 1 or (t.stride(-1) != 1 and t.shape[-1] != 1):
         raise TypeError(f"{name} must have at least one dim, the last with unit stride")
-    return t if t.dim() <= 4 else t.reshape(-1, t.shape[-1])
+    return t if n <= 4 else t.reshape(-1, t.shape[-1])
 
 
 def _norm_rows(*ts):
@@ -600,23 +615,26 @@ def _norm_rows(*ts):
     return order, (1,) * (3 - lead) + tuple(x.shape[i] for i in order)
 
 
-def _norm_strides(t, order):
+def _norm_strides(t, order, D):
     if order is None:
-        return Strides(0, 0, t.shape[-1])
+        return Strides(0, 0, D)
     return Strides(*[0] * (3 - len(order)), *(0 if t.shape[i] == 1 else t.stride(i) for i in order))
 
 
-def _norm_weights(x, weight, bias):
-    torch = _torch()
+def _norm_weights(x, D, weight, bias):
+    """The type of weight and bias, checked (x's without any)."""
+    wt = None
     for t, n in ((weight, "weight"), (bias, "bias")):
-        if t is not None:
-            if not isinstance(t, torch.Tensor) or t.dtype not in (x.dtype, torch.float32):
-                raise TypeError(f"{n} must be a tensor of {x.dtype} or torch.float32")
-            _expect(t, n, t.dtype, (x.shape[-1],), x.device, dense=True)
-    if weight is not None and bias is not None and weight.dtype != bias.dtype:
-        raise TypeError("weight and bias must be of one type")
-    w = weight if weight is not None else bias
-    return x.dtype if w is None else w.dtype
+        if t is None:
+            continue
+        torch = _torch()
+        if not (isinstance(t, torch.Tensor) and (t.dtype == x.dtype or t.dtype == torch.float32) and t.dim() == 1
+                and t.numel() == D and t.device == x.device and t.is_contiguous()):
+            raise TypeError(f"{n} must be a contiguous {x.dtype} or torch.float32 CUDA tensor of shape ({D},) on {x.device}")
+        if wt is not None and t.dtype != wt:
+            raise TypeError("weight and bias must be of one type")
+        wt = t.dtype
+    return x.dtype if wt is None else wt
 
 
 def _ptr(t):
@@ -629,28 +647,26 @@ def layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, out=None, stats=True):
     fp32 (x.shape[:-1]; None, None without stats). weight and bias: [D], of x's
     type or fp32. out: the tensor to write, may be x."""
     torch = _torch()
+    code = _type_code(x, "x")
     x4 = _norm_view(x, "x")
-    code = _type_code(x, "x", (VITATTN_BF16, VITATTN_FP16, VITATTN_FP32))
-    wt = _norm_weights(x, weight, bias)
+    D = x4.shape[-1]
+    wt = _norm_weights(x, D, weight, bias)
     if x.numel() == 0:
         raise ValueError("layer_norm needs at least one row and one column")
-    shape = tuple(x.shape)
     if out is None:
-        y = torch.empty_like(x) if x.dim() <= 4 else torch.empty(shape, dtype=x.dtype, device=x.device)
+        y = torch.empty_like(x) if x4 is x else torch.empty(x.shape, dtype=x.dtype, device=x.device)
     else:
-        y = _expect(out, "out", x.dtype, shape, x.device, dense=x.dim() > 4)
-    y4 = y.view(x4.shape)
+        y = _expect(out, "out", x.dtype, x.shape, x.device, dense=x4 is not x)
+    y4 = y if x4 is x else y.view(x4.shape)
     order, n = _norm_rows(x4, y4)
     mean = rstd = None
     if stats:
         mean, rstd = (torch.empty(n, dtype=torch.float32, device=x.device) for _ in range(2))
-    with _on_device(x):
-        _check(library().vitattn_layer_norm_fwd(x4.data_ptr(), _norm_strides(x4, order), _ptr(weight), _ptr(bias),
-                                                y.data_ptr(), _norm_strides(y4, order), _ptr(mean), _ptr(rstd), *n,
-                                                shape[-1], eps, code, VITATTN_FP32 if wt == torch.float32 else code,
-                                                _stream_ptr(x)))
+    _call(x, library().vitattn_layer_norm_fwd, x4.data_ptr(), _norm_strides(x4, order, D), _ptr(weight), _ptr(bias),
+          y.data_ptr(), _norm_strides(y4, order, D), _ptr(mean), _ptr(rstd), *n, D, eps, code,
+          VITATTN_FP32 if wt == torch.float32 else code)
     if stats:
-        mean, rstd = (_norm_stat_out(t, order, x4, shape) for t in (mean, rstd))
+        mean, rstd = (_norm_stat_out(t, order, x4, x.shape) for t in (mean, rstd))
     return y, mean, rstd
 
 
@@ -666,24 +682,24 @@ def layer_norm_bwd(x, weight, mean, rstd, dy, want_dweight=True, want_dbias=True
     shape and type); dweight is None without a weight or if not wanted, dbias if
     not wanted. Without a weight dbias has bias_dtype (default x's)."""
     torch = _torch()
+    code = _type_code(x, "x")
     x4 = _norm_view(x, "x")
-    code = _type_code(x, "x", (VITATTN_BF16, VITATTN_FP16, VITATTN_FP32))
     shape = tuple(x.shape)
+    D = shape[-1]
     _expect(dy, "dy", x.dtype, shape, x.device)
     for t, n in ((mean, "mean"), (rstd, "rstd")):
         if not (isinstance(t, torch.Tensor) and t.device == x.device and t.dtype == torch.float32
                 and tuple(t.shape) == shape[:-1]):
             raise TypeError(f"{n} must be a torch.float32 CUDA tensor of shape {shape[:-1]} on {x.device}")
-    wt = _norm_weights(x, weight, None)
+    wt = _norm_weights(x, D, weight, None)
     if weight is None and bias_dtype is not None:
         if bias_dtype not in (x.dtype, torch.float32):
             raise TypeError(f"bias_dtype must be {x.dtype} or torch.float32")
         wt = bias_dtype
     if x.numel() == 0:
         raise ValueError("layer_norm needs at least one row and one column")
-    D = shape[-1]
-    dx = torch.empty_like(x) if x.dim() <= 4 else torch.empty(shape, dtype=x.dtype, device=x.device)
-    dy4, dx4 = _norm_view(dy, "dy"), dx.view(x4.shape)
+    dx = torch.empty_like(x) if x4 is x else torch.empty(shape, dtype=x.dtype, device=x.device)
+    dy4, dx4 = _norm_view(dy, "dy"), dx if x4 is x else dx.view(x4.shape)
     order, n = _norm_rows(x4, dy4, dx4)
     if order is not None:
         mean, rstd = (t.reshape(x4.shape[:-1]).permute(order) for t in (mean, rstd))
@@ -695,18 +711,29 @@ def layer_norm_bwd(x, weight, mean, rstd, dy, want_dweight=True, want_dbias=True
     if workspace is None:
         workspace = torch.empty(max(need, 4) // 4, dtype=torch.float32, device=x.device)
     _expect_workspace(workspace, x.device)
-    with _on_device(x):
-        _check(lib.vitattn_layer_norm_bwd(x4.data_ptr(), _norm_strides(x4, order), _ptr(weight), mean.data_ptr(),
-                                          rstd.data_ptr(), dy4.data_ptr(), _norm_strides(dy4, order), dx4.data_ptr(),
-                                          _norm_strides(dx4, order), _ptr(dw), _ptr(db), *n, D, code,
-                                          VITATTN_FP32 if wt == torch.float32 else code, workspace.data_ptr(),
-                                          workspace.numel() * workspace.element_size(), _stream_ptr(x)))
+    _call(x, lib.vitattn_layer_norm_bwd, x4.data_ptr(), _norm_strides(x4, order, D), _ptr(weight), mean.data_ptr(),
+          rstd.data_ptr(), dy4.data_ptr(), _norm_strides(dy4, order, D), dx4.data_ptr(), _norm_strides(dx4, order, D),
+          _ptr(dw), _ptr(db), *n, D, code, VITATTN_FP32 if wt == torch.float32 else code, workspace.data_ptr(),
+          workspace.numel() * workspace.element_size())
     return dx, dw, db
 
 
 def _strides_any(t):
     """Strides of a [B, H, N, d] view, zeros for dims of size one."""
-    return Strides(*(0 if t.shape[i] == 1 else t.stride(i) for i in range(3)))
+    s, n = t.stride(), t.shape
+    return Strides(s[0] if n[0] != 1 else 0, s[1] if n[1] != 1 else 0, s[2] if n[2] != 1 else 0)
+
+
+@functools.lru_cache(maxsize=None)
+def _pos_codes():
+    torch = _torch()
+    return {torch.int32: 0, torch.int64: 1, torch.float32: 2}
+
+
+@functools.lru_cache(maxsize=256)
+def _c_ints(values):
+    """A C array of these ints, which nobody writes."""
+    return (c_int * max(len(values), 1))(*values)
 
 
 def rotary_fwd(q, k, positions, sections, base=10000.0, interleaved=False, joint=False, inverse=False, out=None):
@@ -717,40 +744,44 @@ def rotary_fwd(q, k, positions, sections, base=10000.0, interleaved=False, joint
     over all R (joint). inverse turns back: the gradient. out=(q', k') to write
     into, which may be q and k. Returns q', or (q', k') if there is a k."""
     torch = _torch()
-    code = _type_code(q, "q", (VITATTN_BF16, VITATTN_FP16, VITATTN_FP32))
+    code = _type_code(q, "q")
     for t, n in ((q, "q"), (k, "k")):
         if t is not None and not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == q.dtype and t.dim() == 4
-                                  and t.device == q.device and (t.shape[3] == 1 or t.stride(3) == 1)):
+                                  and t.device == q.device and (t.stride(3) == 1 or t.shape[3] == 1)):
             raise TypeError(f"{n} must be a 4-D CUDA tensor [B, H, N, d] of q's type and device with unit stride along d")
     B, Hq, N, d = q.shape
-    if k is not None and (k.shape[0], k.shape[2], k.shape[3]) != (B, N, d):
-        raise ValueError("k must be [B, Hk, N, d] with the B, N and d of q")
-    sections = tuple(int(s) for s in sections)
+    Hk = 0
+    if k is not None:
+        Bk, Hk, Nk, dk = k.shape
+        if (Bk, Nk, dk) != (B, N, d):
+            raise ValueError("k must be [B, Hk, N, d] with the B, N and d of q")
+    sections = tuple(map(int, sections))
     A = len(sections)
-    codes = {torch.int32: 0, torch.int64: 1, torch.float32: 2}
-    if not (isinstance(positions, torch.Tensor) and positions.device == q.device and positions.dtype in codes
-            and tuple(positions.shape) in ((N, A), (B, N, A))):
+    pos_code = _pos_codes().get(positions.dtype) if isinstance(positions, torch.Tensor) else None
+    if pos_code is None or positions.device != q.device or tuple(positions.shape) not in ((N, A), (B, N, A)):
         raise TypeError(f"positions must be an int32, int64 or float32 tensor [{N}, {A}] or [{B}, {N}, {A}] on {q.device}")
+    k_out, sk, sk_out = None, _NO_STRIDES, _NO_STRIDES
     if out is None:
-        q_out, k_out = torch.empty_like(q), None if k is None else torch.empty_like(k)
+        q_out = torch.empty_like(q)
+        if k is not None:
+            k_out = torch.empty_like(k)
     else:
         q_out, k_out = out if k is not None else ((out[0] if isinstance(out, (tuple, list)) else out), None)
         for t, like, n in ((q_out, q, "out q"), (k_out, k, "out k")):
             if like is not None:
                 _expect(t, n, q.dtype, like.shape, q.device)
-    pb = positions.stride(0) if positions.dim() == 3 else 0
+    if k is not None:
+        sk, sk_out = _strides_any(k), _strides_any(k_out)
+    sp = positions.stride()
     flags = ((VITATTN_ROTARY_INTERLEAVED if interleaved else 0) | (VITATTN_ROTARY_INVERSE if inverse else 0)
              | (VITATTN_ROTARY_JOINT if joint else 0))
-    zero = Strides(0, 0, 0)
-    with _on_device(q):
-        _check(library().vitattn_rotary(
-            q.data_ptr(), _strides_any(q), q_out.data_ptr(), _strides_any(q_out), Hq, _ptr(k),
-            zero if k is None else _strides_any(k), _ptr(k_out), zero if k is None else _strides_any(k_out),
-            0 if k is None else k.shape[1], positions.data_ptr(), pb, positions.stride(-2), positions.stride(-1),
-            codes[positions.dtype], (c_int * max(A, 1))(*sections), A, float(base), B, N, d, code, flags,
-            _stream_ptr(q)))
+    _call(q, library().vitattn_rotary, q.data_ptr(), _strides_any(q), q_out.data_ptr(), _strides_any(q_out), Hq,
+          _ptr(k), sk, _ptr(k_out), sk_out, Hk, positions.data_ptr(), sp[0] if len(sp) == 3 else 0, sp[-2], sp[-1],
+          pos_code, _c_ints(sections), A, float(base), B, N, d, code, flags)
     return q_out if k is None else (q_out, k_out)
 
+
+_NO_STRIDES = Strides(0, 0, 0)
 
 # ------------------------------------------------------------------ differential attention
 
@@ -758,23 +789,23 @@ def rotary_fwd(q, k, positions, sections, base=10000.0, interleaved=False, joint
 def _diff_strides(t):
     """Strides of a [B, H, N, d] view as the attention takes them; those of dims
     of size one do not matter and are replaced."""
-    return Strides(0 if t.shape[0] == 1 else t.stride(0), 0 if t.shape[1] == 1 else t.stride(1),
-                   t.shape[3] if t.shape[2] == 1 else t.stride(2))
+    s, n = t.stride(), t.shape
+    return Strides(s[0] if n[0] != 1 else 0, s[1] if n[1] != 1 else 0, s[2] if n[2] != 1 else n[3])
 
 
 def _diff_args(q, k, v, lam, key_lens):
-    torch = _torch()
     _as_input(q, "q")
-    for t, n in ((k, "k"), (v, "v")):
-        _as_input(t, n, q.device)
+    device = q.device
+    _as_input(k, "k", device)
+    _as_input(v, "v", device)
     B, H2, Nq, d = q.shape
-    H, Nk, e = v.shape[1:]
-    if H2 != 2 * H or tuple(k.shape) != (B, H2, Nk, d) or v.shape[0] != B:
+    Bv, H, Nk, e = v.shape
+    if H2 != 2 * H or Bv != B or tuple(k.shape) != (B, H2, Nk, d):
         raise ValueError("q must be [B, 2H, Nq, d], k [B, 2H, Nk, d] and v [B, H, Nk, e]")
-    lam_code = _type_code(lam, "lam", (VITATTN_BF16, VITATTN_FP32))
-    _expect(lam, "lam", lam.dtype, (H,), q.device, dense=True)
+    lam_code = _type_code(lam, "lam", _LAM_TYPES)
+    _expect(lam, "lam", lam.dtype, (H,), device, dense=True)
     if key_lens is not None:
-        _expect(key_lens, "key_lens", torch.int32, (B,), q.device, dense=True)
+        _expect(key_lens, "key_lens", _torch().int32, (B,), device, dense=True)
     return (B, H, Nq, Nk, d, e), lam_code
 
 
@@ -782,7 +813,8 @@ def _like_layout(t, shape):
     """A new tensor [B, H, N, e] in t's order of heads and rows."""
     torch = _torch()
     B, H, N, e = shape
-    if t.shape[1] > 1 and t.shape[2] > 1 and t.stride(1) < t.stride(2):
+    s, n = t.stride(), t.shape
+    if n[1] > 1 and n[2] > 1 and s[1] < s[2]:
         return torch.empty((B, N, H, e), dtype=t.dtype, device=t.device).transpose(1, 2)
     return torch.empty(shape, dtype=t.dtype, device=t.device)
 
@@ -813,11 +845,9 @@ def diff_fwd(q, k, v, lam, scale=None, key_lens=None, out=None, save=True, works
     lib = library()
     need = int(lib.vitattn_diff_fwd_workspace_bytes(*sizes))
     ws = _diff_workspace(workspace, need, q.device) if need or workspace is not None else None
-    with _on_device(q):
-        _check(lib.vitattn_diff_fwd(q.data_ptr(), _diff_strides(q), k.data_ptr(), _diff_strides(k), v.data_ptr(),
-                                    _diff_strides(v), lam.data_ptr(), lam_code, _ptr(key_lens), o.data_ptr(),
-                                    _diff_strides(o), _ptr(o2), _ptr(lse), *sizes, _default_scale(d, scale), _ptr(ws),
-                                    0 if ws is None else ws.numel() * ws.element_size(), _stream_ptr(q)))
+    _call(q, lib.vitattn_diff_fwd, q.data_ptr(), _diff_strides(q), k.data_ptr(), _diff_strides(k), v.data_ptr(),
+          _diff_strides(v), lam.data_ptr(), lam_code, _ptr(key_lens), o.data_ptr(), _diff_strides(o), _ptr(o2), _ptr(lse),
+          *sizes, _default_scale(d, scale), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
     return o, o2, lse
 
 
@@ -836,11 +866,8 @@ def diff_bwd(q, k, v, lam, o, o2, lse, dout, scale=None, key_lens=None, want_dla
     dlam = torch.empty_like(lam) if want_dlam else None
     lib = library()
     ws = _diff_workspace(workspace, int(lib.vitattn_diff_bwd_workspace_bytes(*sizes)), q.device)
-    with _on_device(q):
-        _check(lib.vitattn_diff_bwd(q.data_ptr(), _diff_strides(q), k.data_ptr(), _diff_strides(k), v.data_ptr(),
-                                    _diff_strides(v), lam.data_ptr(), lam_code, _ptr(key_lens), o2.data_ptr(),
-                                    lse.data_ptr(), dout.data_ptr(), _diff_strides(dout), dq.data_ptr(), _diff_strides(dq), dk.data_ptr(),
-                                    _diff_strides(dk), dv.data_ptr(), _diff_strides(dv), _ptr(dlam), *sizes,
-                                    _default_scale(d, scale), ws.data_ptr(), ws.numel() * ws.element_size(),
-                                    _stream_ptr(q)))
+    _call(q, lib.vitattn_diff_bwd, q.data_ptr(), _diff_strides(q), k.data_ptr(), _diff_strides(k), v.data_ptr(),
+          _diff_strides(v), lam.data_ptr(), lam_code, _ptr(key_lens), o2.data_ptr(), lse.data_ptr(), dout.data_ptr(),
+          _diff_strides(dout), dq.data_ptr(), _diff_strides(dq), dk.data_ptr(), _diff_strides(dk), dv.data_ptr(),
+          _diff_strides(dv), _ptr(dlam), *sizes, _default_scale(d, scale), ws.data_ptr(), ws.numel() * ws.element_size())
     return dq, dk, dv, dlam
