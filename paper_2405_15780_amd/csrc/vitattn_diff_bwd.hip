@@ -599,35 +599,53 @@ __global__ __launch_bounds__(64 * NW, DV > 128 ? 1 : 2) void diff_dq_kernel(cons
   wait_vmem();
   __syncthreads();
 
-  // tile j in slot SL; tile j + PF is requested into the slot of tile j - 1
+  // Tile j in slot SL; tile j + PF is requested into the slot of tile j - 1. One
+  // stream of ops: the scores, dP beside the exponentials, then dQ in four groups
+  // (map, contraction step), each beside the vector work of the next group's dS.
+  // Operands are read two ops ahead, through the barrier: the barrier before stage
+  // j waited for tile j + 1.
+  constexpr int NS = 2 * QS + VS, NQ = 4 * NCQ, AH = 2;
+  auto load_op = [&](auto slot_tag, int i) __attribute__((always_inline)) -> bf16x8 {
+    constexpr int SL = decltype(slot_tag)::value, NX = (SL + 1) % RING;
+    if (i >= NS + NQ) return lds_frag_row(kbuf[NX] + ((i - NS - NQ) & 1) * KT, rfk.at((i - NS - NQ) >> 1));
+    if (i < 2 * QS) return lds_frag_row(kbuf[SL] + (i & 1) * KT, rfk.at(i >> 1));
+    if (i < NS) return lds_frag_row(vbuf[SL], rfv.at(i - 2 * QS));
+    const int g = (i - NS) / NCQ;
+    return tfk.load(kbuf[SL] + (g >> 1) * KT, 16 * (g & 1), (i - NS) % NCQ);
+  };
+  bf16x8 lead[AH];
+#pragma unroll
+  for (int i = 0; i < AH; ++i) lead[i] = load_op(std::integral_constant<int, 0>{}, i);
   auto stage = [&](auto slot_tag, int j) __attribute__((always_inline)) {
     constexpr int SL = decltype(slot_tag)::value;
     constexpr int RF = (SL + PF) % RING;
-    constexpr int NS = 2 * QS + VS, NQ = 4 * NCQ;
     f32x16 s[2], dp;
-    auto load_op = [&](int i) -> bf16x8 {
-      if (i < 2 * QS) return lds_frag_row(kbuf[SL] + (i & 1) * KT, rfk.at(i >> 1));
-      if (i < NS) return lds_frag_row(vbuf[SL], rfv.at(i - 2 * QS));
-      const int t = i - NS, u = t % (2 * NCQ);
-      return tfk.load(kbuf[SL] + (u / NCQ) * KT, 16 * (t / (2 * NCQ)), u % NCQ);
+    bf16x8 ob[4];
+    bf16x8 aq[AH + 1];
+#pragma unroll
+    for (int i = 0; i < AH; ++i) aq[i] = lead[i];
+    // dS of row r of group g
+    auto row = [&](int g, int r) __attribute__((always_inline)) {
+      const int m = g >> 1;
+      if (!START && m == 0) dp[r] += nd1;
+      float x = s[m][r] * (m ? dp[r] + dd : dp[r]);
+      pin(x);
+      s[m][r] = x;
+      if ((r & 7) == 7) ob[g] = acc_to_operand(s[m], g & 1);
     };
-    bf16x8 aq[3];
-    aq[0] = load_op(0);
-    aq[1] = load_op(1);
     sched_fence();
-    // scores, then dP beside the exponentials
-    constexpr int W = VS;
-    static_for<0, NS>([&](auto IC) __attribute__((always_inline)) {
+    static_for<0, NS + NQ>([&](auto IC) __attribute__((always_inline)) {
       constexpr int i = decltype(IC)::value;
-      aq[(i + 2) % 3] = load_op(i + 2);
+      if constexpr (i + AH < NS + NQ) aq[(i + AH) % (AH + 1)] = load_op(slot_tag, i + AH);
+      else lead[i + AH - NS - NQ] = load_op(slot_tag, i + AH);
       if constexpr (i < 2 * QS) {
         if constexpr (i < 2) s[i] = zero16();
-        s[i & 1] = mfma32(aq[i % 3], qf[i & 1][i >> 1], s[i & 1]);
-      } else {
-        dp = mfma32(aq[i % 3], gf[i - 2 * QS], i == 2 * QS ? start : dp);
+        s[i & 1] = mfma32(aq[i % (AH + 1)], qf[i & 1][i >> 1], s[i & 1]);
+      } else if constexpr (i < NS) {
+        dp = mfma32(aq[i % (AH + 1)], gf[i - 2 * QS], i == 2 * QS ? start : dp);
         static_for<0, 16>([&](auto RC) __attribute__((always_inline)) {
           constexpr int r = decltype(RC)::value;
-          if constexpr (r * W / 16 == i - 2 * QS) {
+          if constexpr (r * VS / 16 == i - 2 * QS) {
             float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][r], c, -l1));
             float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[1][r], c, -l2));
             pin(x);
@@ -636,33 +654,28 @@ __global__ __launch_bounds__(64 * NW, DV > 128 ? 1 : 2) void diff_dq_kernel(cons
             s[1][r] = y;
           }
         });
+      } else {
+        constexpr int t = i - NS, g = t / NCQ, u = t % NCQ;
+        if constexpr (t == 0) {
+          if ((j + 1) * BN > Nk)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (j * BN + acc_row(r, h) >= Nk) s[0][r] = s[1][r] = 0.f;
+#pragma unroll
+          for (int r = 0; r < 8; ++r) row(0, r);
+        }
+        acc[(g >> 1) * NCQ + u] = mfma32(aq[i % (AH + 1)], ob[g], acc[(g >> 1) * NCQ + u]);
+        if constexpr (g < 3)
+          static_for<0, 8>([&](auto RC) __attribute__((always_inline)) {
+            constexpr int r = decltype(RC)::value;
+            if constexpr (r * NCQ / 8 == u) row(g + 1, 8 * ((g + 1) & 1) + r);
+          });
       }
       if constexpr (i < NREQ) request(std::integral_constant<int, RF>{}, j + PF, i);
       sched_fence();
     });
-    if ((j + 1) * BN > Nk)
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (j * BN + acc_row(r, h) >= Nk) s[0][r] = s[1][r] = 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float x = START ? dp[r] : dp[r] + nd1;
-      s[0][r] *= x;
-      s[1][r] *= x + dd;
-    }
-    bf16x8 ob[2][2];
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) ob[m][ks] = acc_to_operand(s[m], ks);
-    static_for<0, NQ>([&](auto IC) __attribute__((always_inline)) {
-      constexpr int t = decltype(IC)::value, i = NS + t, u = t % (2 * NCQ);
-      if constexpr (t + 2 < NQ) aq[(i + 2) % 3] = load_op(i + 2);
-      acc[u] = mfma32(aq[i % 3], ob[u / NCQ][t / (2 * NCQ)], acc[u]);
-      sched_fence();
-    });
-    // tile j + 1 was requested in stage j + 1 - PF
-    wait_vmem_leave<(PF - 1) * ((decltype(dma)::ALL_ACTIVE ? 2 * PK : 0) + (decltype(dmv)::ALL_ACTIVE ? PV : 0))>();
+    // tile j + 2 was requested in stage j + 2 - PF
+    wait_vmem_leave<(PF - 2) * ((decltype(dma)::ALL_ACTIVE ? 2 * PK : 0) + (decltype(dmv)::ALL_ACTIVE ? PV : 0))>();
     barrier_lds();
   };
   const int n_iter = (n_kt + RING - 1) / RING * RING;  // tiles past the last have P = 0
