@@ -13,6 +13,12 @@ __device__ __forceinline__ float lam_of(const void* lam, bool bf16, int h) {
 __device__ __forceinline__ int keys_of(const int* key_lens, int b, int Nk) {
   return key_lens ? min(max(key_lens[b], 0), Nk) : Nk;
 }
+// This workgroup's work item: each XCD takes a run of consecutive ones, which
+// share keys in its L2, unless samples differ in length. Then the runs would too
+// (a padded batch's short samples on some XCDs), and items go to the XCDs in turn.
+__device__ __forceinline__ int work_item(const int* key_lens, int total) {
+  return key_lens ? (int)blockIdx.x : xcd_remap(blockIdx.x, total);
+}
 // head of map m of (b, h) in a tensor of 2 H heads
 __device__ __forceinline__ long long map_head(const Map& m, int b, int h, int map) {
   return b * m.sb + (2LL * h + map) * m.sh;

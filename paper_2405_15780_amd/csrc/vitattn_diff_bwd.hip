@@ -170,7 +170,7 @@ __global__ __launch_bounds__(128 * KBW, KBW == 2 && DV > 64 ? 1 : 2) void diff_d
   debug_poison_lds(qbuf0, qbuf1, qbuf2, qbuf3, qbuf4, qbuf5, gbuf0, gbuf1, gbuf2, gbuf3, gbuf4, gbuf5, sbuf0, sbuf1,
                    sbuf2, sbuf3, sbuf4, sbuf5, xbuf0, xbuf1);
 
-  const int work = xcd_remap(blockIdx.x, total), block = first + work / PARTS;
+  const int work = work_item(a.key_lens, total), block = first + work / PARTS;
   const int bh = block / n_ktiles, key_first = (block - bh * n_ktiles) * kKeyBlock + (work % PARTS) * 32 * KBW;
   const int b = bh / a.H, head = bh - b * a.H;
   const int lane = threadIdx.x & 63, h = lane >> 5;
@@ -519,7 +519,7 @@ __global__ __launch_bounds__(64 * NW, DV > 128 ? 1 : 2) void diff_dq_kernel(cons
   char* const vbuf[RING] = {vbuf0, vbuf1, vbuf2, vbuf3};
   debug_poison_lds(kbuf0, kbuf1, kbuf2, kbuf3, vbuf0, vbuf1, vbuf2, vbuf3, sums);
 
-  const int work = xcd_remap(blockIdx.x, total);
+  const int work = work_item(a.key_lens, total);
   const int bh = work / n_qtiles, qt = work - bh * n_qtiles;
   const int b = bh / a.H, head = bh - b * a.H;
   const int lane = threadIdx.x & 63, h = lane >> 5;

@@ -68,7 +68,7 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
   debug_poison_lds(kbuf0, kbuf1, vbuf0, vbuf1, xown);
   float(*const xbuf)[16][64] = OVER_K ? reinterpret_cast<float(*)[16][64]>(kbuf0) : xown;
 
-  const int work = xcd_remap(blockIdx.x, total);
+  const int work = work_item(a.key_lens, total);
   const int part = work / n_qtiles;
   const int qt = work - part * n_qtiles;
   const int bh = SPLIT ? part / n_split : part;
