@@ -503,8 +503,8 @@ int vitattn_rotary(const void* q, vitattn_strides sq, void* q_out, vitattn_strid
  *              (rows + 512) * row * 2 < 2^31. Outputs must not alias inputs.
  *   sizes    : B*H*(max(Nq, Nk) + 512) below 2^30.
  *   workspace: at least the bytes the matching function gives (the forward's is
- *              0 unless few queries meet many keys; then the keys are split over
- *              workgroups whose results are joined), 16-byte aligned.
+ *              0 unless up to 256 queries meet many keys; then both passes split
+ *              the keys over workgroups whose results are joined), 16-byte aligned.
  * Scores, statistics, sums and the difference are fp32; P and dS are rounded
  * to bf16 as operands of the matrix cores, o and the gradients once at the end. Results are bitwise deterministic, and a head's results do not depend
  * on the call it is part of. No atomics.

@@ -346,7 +346,7 @@ int vitattn_diff_fwd(const void* q, vitattn_strides sq, const void* k, vitattn_s
 
 size_t vitattn_diff_bwd_workspace_bytes(int B, int H, int Nq, int Nk, int d, int e) {
   if (check_diff_sizes(B, H, Nq, Nk, d, e) != VITATTN_OK) return 0;
-  return vitattn::diff_bwd_workspace_floats(B, H, Nq) * sizeof(float);
+  return vitattn::diff_bwd_workspace_floats(B, H, Nq, Nk, d) * sizeof(float);
 }
 
 int vitattn_diff_bwd(const void* q, vitattn_strides sq, const void* k, vitattn_strides sk, const void* v,

@@ -14,7 +14,8 @@
 //      handed through LDS, forms both dS and accumulates dK_1 and dK_2. At
 //      e = 2 d both have 16 matrix ops per 32 x 32 block.
 //   3. dQ kernel: 32 queries per wave, four waves, Q_1, Q_2 and dO held; streams
-//      K_1, K_2 and V.
+//      K_1, K_2 and V. Few queries over many keys: the keys are split over
+//      workgroups as in the forward, and a fourth kernel adds the shares in order.
 //
 // P_1 - lam P_2 and dS are rounded to bf16 as matrix-core operands, and P to
 // fp16 where role V hands it over: 10 bits of fraction against bf16's 7 (dK is
@@ -32,7 +33,8 @@ namespace vitattn {
 
 namespace {
 
-// Workspace: per (b, h) and block of 32 queries 128 floats, [-D_1 | D_1 - D_2 |
+// Workspace: the shares of dQ where the keys are split, fp32 [bh][split][map]
+// [query][d]; then per (b, h) and block of 32 queries 128 floats, [-D_1 | D_1 - D_2 |
 // LSE_1 log2 e - 14 | LSE_2 log2 e - 14] of 32 each; then the partial sums of D_2,
 // [bh][row-pass workgroup]. Rows past the last query hold zeros and an LSE of
 // +inf, which makes their P zero; so do rows without keys.
@@ -495,12 +497,13 @@ __global__ __launch_bounds__(128 * KBW, KBW == 2 && DV > 64 ? 1 : 2) void diff_d
 // through a ring of LDS slots in tiles of 32 keys. Per tile:
 //   S_m^T = K_m Q_m^T, dP^T = V dO^T;  dS_m^T;  dQ_m^T += K_m^T dS_m^T
 // Keys past the sample's last have P = 0 (their scores are of zero rows, and an
-// LSE far below zero would make exp overflow). The workgroup of query tile 0 of
-// sample 0 also adds its head's partial sums of dlam.
-template <int DQ, int QS, int DV, int RING, int NW>
+// LSE far below zero would make exp overflow). The (first) workgroup of query tile
+// 0 of sample 0 also adds its head's partial sums of dlam.
+template <int DQ, int QS, int DV, int RING, int NW, bool SPLIT>
 __global__ __launch_bounds__(64 * NW, DV > 128 ? 1 : 2) void diff_dq_kernel(const DiffArgs a, const float* __restrict__ stats,
                                                                   const float* __restrict__ partial, int groups,
-                                                                  int n_qtiles, int total, float c) {
+                                                                  int n_qtiles, int n_split, int split_keys, int total,
+                                                                  float c) {
   constexpr int BM = 32 * NW, BN = 32;
   constexpr int VS = DV / 16;
   constexpr int NCQ = (QS + 1) / 2;
@@ -520,15 +523,19 @@ __global__ __launch_bounds__(64 * NW, DV > 128 ? 1 : 2) void diff_dq_kernel(cons
   debug_poison_lds(kbuf0, kbuf1, kbuf2, kbuf3, vbuf0, vbuf1, vbuf2, vbuf3, sums);
 
   const int work = work_item(a.key_lens, total);
-  const int bh = work / n_qtiles, qt = work - bh * n_qtiles;
+  const int part = work / n_qtiles, qt = work - part * n_qtiles;
+  const int bh = SPLIT ? part / n_split : part, sp = SPLIT ? part - bh * n_split : 0;
   const int b = bh / a.H, head = bh - b * a.H;
   const int lane = threadIdx.x & 63, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int qrow = qt * BM + wave * 32 + (lane & 31);
-  const int Nk = keys_of(a.key_lens, b, a.Nk);
+  // this workgroup's keys: [key_first, key_first + Nk)
+  const int all = keys_of(a.key_lens, b, a.Nk);
+  const int key_first = SPLIT ? min(sp * split_keys, all) : 0;
+  const int Nk = SPLIT ? min(all - key_first, split_keys) : all;
   const float lam = lam_of(a.lam, a.lam_bf16, head);
 
-  if (b == 0 && qt == 0 && a.dlam) {
+  if (b == 0 && qt == 0 && sp == 0 && a.dlam) {
     float s = 0.f;
     for (int i = threadIdx.x; i < a.B * groups; i += 64 * NW) {
       const int bb = i / groups;
@@ -575,9 +582,9 @@ __global__ __launch_bounds__(64 * NW, DV > 128 ? 1 : 2) void diff_dq_kernel(cons
     start = zero16();
   }
 
-  const rsrc_t rk1 = make_rsrc(a.k + map_head(a.mk, b, head, 0), (unsigned)(Nk * ldk));
-  const rsrc_t rk2 = make_rsrc(a.k + map_head(a.mk, b, head, 1), (unsigned)(Nk * ldk));
-  const rsrc_t rv = make_rsrc(a.v + b * a.mv.sb + head * a.mv.sh, (unsigned)(Nk * ldv));
+  const rsrc_t rk1 = make_rsrc(a.k + map_head(a.mk, b, head, 0) + (long long)key_first * a.mk.ld, (unsigned)(Nk * ldk));
+  const rsrc_t rk2 = make_rsrc(a.k + map_head(a.mk, b, head, 1) + (long long)key_first * a.mk.ld, (unsigned)(Nk * ldk));
+  const rsrc_t rv = make_rsrc(a.v + b * a.mv.sb + head * a.mv.sh + (long long)key_first * a.mv.ld, (unsigned)(Nk * ldv));
   TileDma<DQ, BN, NW> dma;
   TileDma<DV, BN, NW> dmv;
   dma.init(wave, lane, ldk, chr);
@@ -702,14 +709,40 @@ __global__ __launch_bounds__(64 * NW, DV > 128 ? 1 : 2) void diff_dq_kernel(cons
   for (int m = 0; m < 2; ++m) {
     const float f = (m ? -lam * a.scale : a.scale) * kUnshift;
     uint16_t* out = a.dq + map_head(a.mdq, b, head, m) + (long long)qrow * a.mdq.ld;
+    float* share = a.work + ((((long long)bh * n_split + sp) * 2 + m) * a.Nq + qrow) * a.d;
 #pragma unroll
     for (int cb = 0; cb < NCQ; ++cb)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int col = 32 * cb + 8 * g + 4 * h;
         const f32x16& x = acc[m * NCQ + cb];
-        if (col < a.d) put4_bf16(out + col, x[4 * g] * f, x[4 * g + 1] * f, x[4 * g + 2] * f, x[4 * g + 3] * f);
+        if (col >= a.d) continue;
+        if (SPLIT) *reinterpret_cast<float4*>(share + col) = make_float4(x[4 * g] * f, x[4 * g + 1] * f, x[4 * g + 2] * f, x[4 * g + 3] * f);
+        else put4_bf16(out + col, x[4 * g] * f, x[4 * g + 1] * f, x[4 * g + 2] * f, x[4 * g + 3] * f);
       }
+  }
+}
+
+// Adds the shares of dQ in split order, eight in flight: a wave per (bh, map,
+// query) row, a column per lane and 64 more.
+__global__ __launch_bounds__(256) void diff_dq_join_kernel(const DiffArgs a, int n_split) {
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), rows = 2LL * a.B * a.H * a.Nq;
+  if (row >= rows) return;
+  const long long bhm = row / a.Nq, bh = bhm >> 1;
+  const int i = (int)(row - bhm * a.Nq), m = (int)(bhm & 1), b = (int)(bh / a.H), head = (int)(bh - (long long)b * a.H);
+  const long long step = 2LL * a.Nq * a.d;
+  const float* src = a.work + ((bh * n_split * 2 + m) * a.Nq + i) * a.d;
+  uint16_t* out = a.dq + map_head(a.mdq, b, head, m) + (long long)i * a.mdq.ld;
+  for (int col = threadIdx.x & 63; col < a.d; col += 64) {
+    float s = 0.f;
+    for (int s0 = 0; s0 < n_split; s0 += 8) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = s0 + u < n_split ? src[(s0 + u) * step + col] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += x[u];
+    }
+    out[col] = __builtin_bit_cast(uint16_t, (__bf16)s);
   }
 }
 
@@ -751,20 +784,35 @@ hipError_t go_tile(const DiffArgs& a, const float* stats, const float* partial, 
   // workgroups of four waves: 0.44-1.02 of the time of eight (N = 256 .. 16,384)
   constexpr int NW = 4;
   const int n_qtiles = (a.Nq + 32 * NW - 1) / (32 * NW), total = a.B * a.H * n_qtiles;
-  diff_dq_kernel<DQ, QS, DV, 4, NW>
-      <<<total, 64 * NW, 0, a.stream>>>(a, stats, partial, groups, n_qtiles, total, a.scale * kLog2e);
+  const int split_keys = diff_split_keys(a.Nq, a.Nk);
+  if (split_keys == 0) {
+    diff_dq_kernel<DQ, QS, DV, 4, NW, false>
+        <<<total, 64 * NW, 0, a.stream>>>(a, stats, partial, groups, n_qtiles, 1, 0, total, a.scale * kLog2e);
+    return hipGetLastError();
+  }
+  const int n_split = (a.Nk + split_keys - 1) / split_keys;
+  diff_dq_kernel<DQ, QS, DV, 4, NW, true><<<total * n_split, 64 * NW, 0, a.stream>>>(
+      a, stats, partial, groups, n_qtiles, n_split, split_keys, total * n_split, a.scale * kLog2e);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  diff_dq_join_kernel<<<(unsigned)((2LL * a.B * a.H * a.Nq + 3) / 4), 256, 0, a.stream>>>(a, n_split);
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t diff_bwd_workspace_floats(int B, int H, int Nq) {
+static size_t dq_share_floats(int B, int H, int Nq, int Nk, int d) {
+  const int s = diff_split_keys(Nq, Nk);
+  return s ? (size_t)B * H * ((Nk + s - 1) / s) * 2 * Nq * d : 0;  // (d: a multiple of 8)
+}
+
+size_t diff_bwd_workspace_floats(int B, int H, int Nq, int Nk, int d) {
   const size_t bh = (size_t)B * H;
-  return bh * query_blocks(Nq) * kStat + bh * row_groups(Nq);
+  return dq_share_floats(B, H, Nq, Nk, d) + bh * query_blocks(Nq) * kStat + bh * row_groups(Nq);
 }
 
 hipError_t launch_diff_bwd(const DiffArgs& a) {
-  float* const stats = a.work;
+  float* const stats = a.work + dq_share_floats(a.B, a.H, a.Nq, a.Nk, a.d);
   float* const partial = stats + (size_t)a.B * a.H * query_blocks(a.Nq) * kStat;
   const int groups = row_groups(a.Nq);
   const unsigned grid = (unsigned)(a.B * a.H) * groups;

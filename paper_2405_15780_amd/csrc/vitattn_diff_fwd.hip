@@ -346,12 +346,12 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
   }
 }
 
-// Joins the splits of one query row (bh, query), a workgroup per row: waves
-// 0 .. 7 take map 1 and 8 .. 15 map 2, each an eighth of the splits. A lane
-// weighs split s; the outputs are added in split order, eight in flight, then
-// the eighths in order.
-__global__ __launch_bounds__(1024) void diff_join_kernel(const DiffArgs a, int n_split) {
-  constexpr int Q = 8, U = 8;
+// Joins the splits of one query row (bh, query), a workgroup per row: Q waves for
+// each map, each of which takes a Q-th of the splits. A lane weighs split s; the
+// outputs are added in split order, eight in flight, then the waves' in order.
+template <int Q>
+__global__ __launch_bounds__(128 * Q) void diff_join_kernel(const DiffArgs a, int n_split) {
+  constexpr int U = 8;
   __shared__ float tops[2 * Q], sums[2 * Q], acc[2][Q][192];
   debug_poison_lds(tops, sums, acc);
   const long long row = blockIdx.x, rows = (long long)a.B * a.H * a.Nq;
@@ -407,21 +407,21 @@ __global__ __launch_bounds__(1024) void diff_join_kernel(const DiffArgs a, int n
   }
   if (lane == 0 && share == 0 && a.lse)
     a.lse[(bh * 2 + m) * a.Nq + i] = top == -INFINITY ? -INFINITY : ref + logf(m ? l[1] : l[0]);
-  const int col = threadIdx.x;
-  if (col >= a.e) return;
-  float y[2];
-#pragma unroll
-  for (int mm = 0; mm < 2; ++mm) {
-    const float inv = l[mm] > 0.f || l[mm] != l[mm] ? 1.f / l[mm] : 0.f;
-    y[mm] = 0.f;
-#pragma unroll
-    for (int w = 0; w < Q; ++w) y[mm] += acc[mm][w][col];
-    y[mm] *= inv;
-    if (a.maps) a.maps[((bh * 2 + mm) * a.Nq + i) * a.e + col] = y[mm];
-  }
   const float lam = lam_of(a.lam, a.lam_bf16, head);
-  a.o[b * a.mo.sb + head * a.mo.sh + (long long)i * a.mo.ld + col] =
-      __builtin_bit_cast(uint16_t, (__bf16)(y[0] - lam * y[1]));
+  for (int col = threadIdx.x; col < a.e; col += 128 * Q) {
+    float y[2];
+#pragma unroll
+    for (int mm = 0; mm < 2; ++mm) {
+      const float inv = l[mm] > 0.f || l[mm] != l[mm] ? 1.f / l[mm] : 0.f;
+      y[mm] = 0.f;
+#pragma unroll
+      for (int w = 0; w < Q; ++w) y[mm] += acc[mm][w][col];
+      y[mm] *= inv;
+      if (a.maps) a.maps[((bh * 2 + mm) * a.Nq + i) * a.e + col] = y[mm];
+    }
+    a.o[b * a.mo.sb + head * a.mo.sh + (long long)i * a.mo.ld + col] =
+        __builtin_bit_cast(uint16_t, (__bf16)(y[0] - lam * y[1]));
+  }
 }
 
 template <int DQ, int QS, int DV, int KB, int QW, bool SPLIT>
@@ -462,16 +462,25 @@ hipError_t go_tile(const DiffArgs& a) {
   const int n_split = (a.Nk + split_keys - 1) / split_keys;
   const hipError_t err = go<DQ, QS, DV, KB, 2, true>(a, split_keys, n_split);
   if (err != hipSuccess) return err;
-  diff_join_kernel<<<(unsigned)(a.B * a.H * a.Nq), 1024, 0, a.stream>>>(a, n_split);
+  // (a row of 128 splits takes 13 us with eight waves per map; of few splits there are many rows)
+  const unsigned rows = (unsigned)(a.B * a.H * a.Nq);
+  if (n_split > 32) diff_join_kernel<8><<<rows, 1024, 0, a.stream>>>(a, n_split);
+  else diff_join_kernel<1><<<rows, 128, 0, a.stream>>>(a, n_split);
   return hipGetLastError();
 }
 
 }  // namespace
 
+// Up to 128 splits of 512 keys or more for one workgroup's queries, up to 32 of
+// 4,096 or more for four of them. (Splits write and read 8 e bytes per query: 256
+// heads of 256 queries over 4,096 keys in two splits took 384 us against 239, so
+// these wait for longer keys; 8 heads of 128 queries over 32,768 took 51 against
+// 417 in 16.)
 int diff_split_keys(int Nq, int Nk) {
-  if (Nq > 64 || Nk < 1024) return 0;
-  const int keys = (Nk / 128 + 63) / 64 * 64;
-  return keys > 512 ? keys : 512;
+  if (Nq > 256 || Nk < (Nq > 64 ? 8192 : 1024)) return 0;
+  const int least = Nq > 64 ? 4096 : 512, most = Nq > 64 ? 32 : 128;
+  const int keys = (Nk / most + 63) / 64 * 64;
+  return keys > least ? keys : least;
 }
 
 size_t diff_fwd_workspace_floats(int B, int H, int Nq, int Nk, int e) {

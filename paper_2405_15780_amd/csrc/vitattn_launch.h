@@ -258,10 +258,10 @@ struct DiffArgs {
   bool lam_bf16;
   hipStream_t stream;
 };
-// Keys per split of a forward call over few queries; 0: not split.
+// Keys per split of a call over few queries; 0: not split.
 int diff_split_keys(int Nq, int Nk);
 size_t diff_fwd_workspace_floats(int B, int H, int Nq, int Nk, int e);
-size_t diff_bwd_workspace_floats(int B, int H, int Nq);
+size_t diff_bwd_workspace_floats(int B, int H, int Nq, int Nk, int d);
 hipError_t launch_diff_fwd(const DiffArgs& a);
 hipError_t launch_diff_bwd(const DiffArgs& a);
 

@@ -72,7 +72,8 @@ def test_lengths_around_tiles(d, e, N):
 
 
 @pytest.mark.parametrize("d,e", [(32, 64), (64, 64), (64, 128), (80, 160)])
-@pytest.mark.parametrize("Nq,Nk", [(1, 1024), (1, 5000), (3, 1023), (33, 3111), (64, 2048), (65, 2048)])
+@pytest.mark.parametrize("Nq,Nk", [(1, 1024), (1, 5000), (3, 1023), (33, 3111), (64, 2048), (65, 2048), (65, 8192), (200, 9001), (256, 8192),
+                                   (257, 8192)])
 def test_few_queries_over_many_keys(d, e, Nq, Nk):
     print(f"case diff few queries Nq={Nq} Nk={Nk} d={d} e={e}", flush=True)
     check(*inputs(2, 1, Nq, Nk, d, e, seed=Nk + Nq))
