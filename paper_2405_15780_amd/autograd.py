@@ -179,9 +179,10 @@ def diff_attention(q, k, v, lam, scale=None, key_lens=None):
     and 2h + 1 are the two maps of head h), v [B,H,Nk,e], lam [H] or one value for
     all heads (fp32 or bf16); scale defaults to 1/sqrt(d). key_lens (int32 [B]):
     sample b attends to its first key_lens[b] keys. Returns o, bf16 [B,H,Nq,e]."""
-    if lam.dim() != 1 or lam.numel() != v.shape[1]:
-        if lam.numel() == 1:
-            lam = lam.reshape(1).expand(v.shape[1])
+    if not isinstance(lam, _torch().Tensor):
+        raise TypeError("lam must be a tensor: [H], or one value for all heads")
+    if lam.numel() == 1 and lam.shape != v.shape[1:2]:
+        lam = lam.reshape(1).expand(v.shape[1])
     lam = lam.contiguous()
     if not _wants_grad(q, k, v, lam):
         return _b.diff_fwd(q, k, v, lam, scale, key_lens, save=False)[0]

@@ -236,6 +236,7 @@ int vitattn_rotary(const void* q, vitattn_strides sq, void* q_out, vitattn_strid
     if (pos_batch < 0 || pos_row < 0 || pos_axis < 0 ||
         (double)(B - 1) * pos_batch + (double)(N - 1) * pos_row + (double)(n_axes - 1) * pos_axis > 1.0e18)
       return VITATTN_E_INVAL;
+    if (Hk > 0 && q_out == k_out) return VITATTN_E_INVAL;
     const void* in[2] = {q, k};
     void* out[2] = {q_out, k_out};
     const vitattn_strides si[2] = {sq, sk}, so[2] = {sq_out, sk_out};

@@ -155,7 +155,7 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
           if (key0 + kb * 32 + acc_row(r, h) >= Nk) s[kb][r] = -INFINITY;
     }
   };
-  auto max_share = [&](const f32x16 (&s)[KB], int q) {
+  auto max_quarter = [&](const f32x16 (&s)[KB], int q) {
     float m = -INFINITY;
 #pragma unroll
     for (int e = q * NE / 4; e < (q + 1) * NE / 4; ++e) m = fmaxf(m, s[e / 16][e % 16]);
@@ -182,7 +182,9 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
     sa[i / QS] = mfma32(lds_frag_row(kbuf[0] + koff, (i / QS) * 32 * 2 * DQ + kfrag.at(i % QS)), qf[i % QS], sa[i / QS]);
   }
   if (n_kt == 1) mask_ragged(sa, 0);
-  m_run = max_halves(fmaxf(fmaxf(max_share(sa, 0), max_share(sa, 1)), fmaxf(max_share(sa, 2), max_share(sa, 3)))) * c;
+  // (finite, so that a first tile of scores -inf leaves zeros and not NaN)
+  m_run = fmaxf(max_halves(fmaxf(fmaxf(max_quarter(sa, 0), max_quarter(sa, 1)), fmaxf(max_quarter(sa, 2), max_quarter(sa, 3)))) * c,
+                -3.0e38f);
   __syncthreads();  // kbuf[0] is refilled by the first stage
 
   auto stage = [&](auto parity, auto has_next, f32x16 (&s)[KB], f32x16 (&sn)[KB], int j) {
@@ -254,7 +256,7 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
         exp_slice(IC, std::integral_constant<int, W>{});
         if constexpr (i >= W && i < W + 4) {
           if constexpr (i == W) mask_ragged(sn, j + 1);
-          mq[i - W] = max_share(sn, i - W);
+          mq[i - W] = max_quarter(sn, i - W);
           pin(mq[i - W]);
         }
         sched_fence();
@@ -474,8 +476,8 @@ hipError_t go_tile(const DiffArgs& a) {
 // Up to 128 splits of 512 keys or more for one workgroup's queries, up to 32 of
 // 4,096 or more for four of them. (Splits write and read 8 e bytes per query: 256
 // heads of 256 queries over 4,096 keys in two splits took 384 us against 239, so
-// these wait for longer keys; 8 heads of 128 queries over 32,768 took 51 against
-// 417 in 16.)
+// these wait for longer keys: 8 heads of 128 queries over 32,768 took 72 us in
+// eight splits against 417, 256 heads of 256 over 8,192 in two 593 against 460.)
 int diff_split_keys(int Nq, int Nk) {
   if (Nq > 256 || Nk < (Nq > 64 ? 8192 : 1024)) return 0;
   const int least = Nq > 64 ? 4096 : 512, most = Nq > 64 ? 32 : 128;

@@ -124,6 +124,7 @@ def test_rotary_more_pairs_than_supported_and_overlaps():
     rotary(b, INVAL, q2=b[2])  # q' over k
     rotary(b, INVAL, q2=b[0], sq2=S(640, 32, 128))  # in place, with other strides
     rotary(b, INVAL, q2=b[2], k2=b[0])
+    rotary(b, INVAL, k2=b[1])  # both outputs at one address
 
 
 def diff_fwd(b, want, **o):

@@ -161,6 +161,20 @@ def test_all_scores_far_below_zero():
     assert all(x.isfinite().all() for x in got.values()) and got["lse"].max() < -200
 
 
+def test_first_tile_of_infinite_scores():
+    """Keys whose score is -inf weigh nothing, also where a whole first tile is such."""
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    q, k, v, lam, _ = inputs(1, 1, 40, 300, 64, 128, seed=25)
+    q = q.abs() + 0.1
+    k[:, :, :100, 0] = -float("inf")
+    o, o2, lse = va.diff_fwd(q, k, v, lam)
+    ref = va.diff_fwd(q, k[:, :, 100:].contiguous(), v[:, :, 100:].contiguous(), lam)
+    for a, b, off in zip((o, o2, lse), ref, (2 ** -6, 2 ** -6, 1e-5)):  # other tiles, so other roundings of P
+        assert a.isfinite().all() and ((a.float() - b.float()).abs() <= off * (1 + b.float().abs())).all()
+
+
 def test_broadcast_heads_and_batches():
     t = torch()
     q, k, v, lam, do = inputs(2, 3, 60, 80, 32, 64, seed=15)
@@ -297,5 +311,7 @@ def test_refusals():
             va.diff_bwd(q, k, v, lam, *bad)
     with pytest.raises(va.VitattnError):
         va.diff_bwd(q, k, v, lam, o, o2, lse, do, workspace=t.empty(8, device="cuda"))
+    with pytest.raises(TypeError):
+        va.diff_attention(q, k, v, 0.5)
     with pytest.raises(va.VitattnError):  # rows that are not 16-byte aligned
         va.diff_fwd(make((2, 4, 10, 36), "bfloat16", 1)[..., :32], k, v, lam)
