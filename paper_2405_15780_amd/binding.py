@@ -158,14 +158,13 @@ def _expect(t, name, dtype, shape, device, dense=False):
     """Raise TypeError unless t is a CUDA tensor of this dtype and exact shape
     on `device`, with unit stride along its last dim (contiguous if dense).
     A mismatch would otherwise become an out-of-bounds access on the GPU."""
-    torch = _torch()
-    shape = tuple(int(n) for n in shape)
-    ok = (isinstance(t, torch.Tensor) and t.is_cuda and t.device == device and t.dtype == dtype
-          and tuple(t.shape) == shape)
+    ok = (isinstance(t, _torch().Tensor) and t.is_cuda and t.device == device and t.dtype == dtype
+          and t.shape == shape)
     if ok:
         ok = t.is_contiguous() if dense else (shape[-1] == 1 or t.stride(-1) == 1)
     if not ok:
         layout = "contiguous" if dense else "unit stride along the last dim"
+        shape = tuple(int(n) for n in shape)
         raise TypeError(f"{name} must be a {dtype} CUDA tensor of shape {shape} on {device} ({layout})")
     return t
 
@@ -661,12 +660,12 @@ def layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, out=None, stats=True):
     order, n = _norm_rows(x4, y4)
     mean = rstd = None
     if stats:
-        mean, rstd = (torch.empty(n, dtype=torch.float32, device=x.device) for _ in range(2))
+        mean, rstd = torch.empty((2, *n), dtype=torch.float32, device=x.device).unbind(0)
     _call(x, library().vitattn_layer_norm_fwd, x4.data_ptr(), _norm_strides(x4, order, D), _ptr(weight), _ptr(bias),
           y.data_ptr(), _norm_strides(y4, order, D), _ptr(mean), _ptr(rstd), *n, D, eps, code,
           VITATTN_FP32 if wt == torch.float32 else code)
     if stats:
-        mean, rstd = (_norm_stat_out(t, order, x4, x.shape) for t in (mean, rstd))
+        mean, rstd = _norm_stat_out(mean, order, x4, x.shape), _norm_stat_out(rstd, order, x4, x.shape)
     return y, mean, rstd
 
 
@@ -684,13 +683,12 @@ def layer_norm_bwd(x, weight, mean, rstd, dy, want_dweight=True, want_dbias=True
     torch = _torch()
     code = _type_code(x, "x")
     x4 = _norm_view(x, "x")
-    shape = tuple(x.shape)
-    D = shape[-1]
-    _expect(dy, "dy", x.dtype, shape, x.device)
+    shape, device = x.shape, x.device
+    D, rows = shape[-1], shape[:-1]
+    _expect(dy, "dy", x.dtype, shape, device)
     for t, n in ((mean, "mean"), (rstd, "rstd")):
-        if not (isinstance(t, torch.Tensor) and t.device == x.device and t.dtype == torch.float32
-                and tuple(t.shape) == shape[:-1]):
-            raise TypeError(f"{n} must be a torch.float32 CUDA tensor of shape {shape[:-1]} on {x.device}")
+        if not (isinstance(t, torch.Tensor) and t.device == device and t.dtype == torch.float32 and t.shape == rows):
+            raise TypeError(f"{n} must be a torch.float32 CUDA tensor of shape {tuple(rows)} on {device}")
     wt = _norm_weights(x, D, weight, None)
     if weight is None and bias_dtype is not None:
         if bias_dtype not in (x.dtype, torch.float32):
@@ -704,13 +702,14 @@ def layer_norm_bwd(x, weight, mean, rstd, dy, want_dweight=True, want_dbias=True
     if order is not None:
         mean, rstd = (t.reshape(x4.shape[:-1]).permute(order) for t in (mean, rstd))
     mean, rstd = mean.contiguous(), rstd.contiguous()
-    dw = torch.empty(D, dtype=wt, device=x.device) if want_dweight and weight is not None else None
-    db = torch.empty(D, dtype=wt, device=x.device) if want_dbias else None
+    dw = torch.empty(D, dtype=wt, device=device) if want_dweight and weight is not None else None
+    db = torch.empty(D, dtype=wt, device=device) if want_dbias else None
     lib = library()
-    need = int(lib.vitattn_layer_norm_bwd_workspace_bytes(*n, D, code)) if dw is not None or db is not None else 0
     if workspace is None:
-        workspace = torch.empty(max(need, 4) // 4, dtype=torch.float32, device=x.device)
-    _expect_workspace(workspace, x.device)
+        need = lib.vitattn_layer_norm_bwd_workspace_bytes(*n, D, code) if dw is not None or db is not None else 0
+        workspace = torch.empty(max(need, 4) // 4, dtype=torch.float32, device=device)
+    else:
+        _expect_workspace(workspace, device)
     _call(x, lib.vitattn_layer_norm_bwd, x4.data_ptr(), _norm_strides(x4, order, D), _ptr(weight), mean.data_ptr(),
           rstd.data_ptr(), dy4.data_ptr(), _norm_strides(dy4, order, D), dx4.data_ptr(), _norm_strides(dx4, order, D),
           _ptr(dw), _ptr(db), *n, D, code, VITATTN_FP32 if wt == torch.float32 else code, workspace.data_ptr(),
@@ -822,7 +821,7 @@ def _like_layout(t, shape):
 def _diff_workspace(workspace, need, device):
     torch = _torch()
     if workspace is None:
-        workspace = torch.empty(max(need, 4) // 4, dtype=torch.float32, device=device)
+        return torch.empty(max(need, 4) // 4, dtype=torch.float32, device=device)
     return _expect_workspace(workspace, device)
 
 
