@@ -14,6 +14,12 @@
 // four waves of a workgroup for long ones. Rows too long for registers (over
 // 256 * 8 pieces) are read once per pass instead, from L2.
 //
+// Measured (a large copy reaches 5.1 TB/s): 32,768 rows of 1,024 bf16 forward
+// 26 us (134 MB, 5.1 TB/s), backward 42 us (201 MB, 4.8 TB/s) and its sums of
+// partials 4; 3,125,000 rows of 64 bf16 171 and 239 us (4.7 and 5.0 TB/s); 3,062
+// rows of 5,001 fp32 27 and 39 us (4.5 and 4.7 TB/s); one row of 768 5.5 us,
+// nearly all of it the launch.
+//
 // The backward's workgroups each take a fixed run of row groups and keep their
 // share of dw and db in registers; at the end the workgroup adds its lanes'
 // and waves' shares in a fixed order and writes one row of partial sums, and a
@@ -460,31 +466,40 @@ __global__ __launch_bounds__(64 * kWeightWaves) void norm_weights_kernel(const N
   else static_cast<T*>(out)[at] = (T)s;
 }
 
-// Lanes that share a row and pieces per lane (lanes = 0: too long for
-// registers). For short rows the fewest pieces per lane that keep three
-// quarters of a wave's lanes at work, or else the most lanes at work.
+// Lanes that share a row and pieces per lane (lanes = 0: too long for registers).
+// With a piece per lane a wave sums over up to 64 lanes for 16 bytes of each; more
+// pieces need fewer lanes, hence fewer steps, and are as many loads. The forward
+// takes two from 4 pieces on (D = 64, 46 MB 17.6 -> 15.8 us, 400 MB 165 -> 171; 72
+// 22.4 -> 19.8 and 178 -> 185; 128 19.8 -> 17.3 and 164 -> 157) and from 16 pieces on
+// two or three, whichever keeps more lanes at work (D = 192 25.3 -> 17.3 and 195 ->
+// 157, 768 21.3 -> 17.4 and 161 -> 152). The backward keeps dw's and db's share of
+// each piece as well: one below 16 pieces (two: D = 64 35 -> 43 us), then two, or
+// three where two leave a fifth of the lanes idle (D = 192 42 -> 37 and 313 -> 235,
+// 384 42 -> 37 and 320 -> 230, 768, against two, 40 -> 35 and 269 -> 228). Four are
+// for rows of more. These are rules on D alone: a row's bits do not depend on the
+// call it is part of.
 struct Shape {
   int lanes, np;
 };
-Shape shape_of(int D, int V) {
+Shape shape_of(int D, int V, bool fwd) {
   const int pieces = (D + V - 1) / V;
-  if (pieces <= 256) {
-    Shape best = {0, 0};
-    int most = -1;
-    for (int np = 1; np <= 4; ++np) {
-      const int L = (pieces + np - 1) / np;
-      if (L > 64) continue;
-      const int used = pieces * (64 / L) * 12 / np;  // of 64 * 12
-      if (used >= 64 * 9) return {L, np};
-      if (used > most) {
-        most = used;
-        best = {L, np};
-      }
-    }
-    return best;
+  if (pieces > 256) {
+    const int np = (pieces + kThreads - 1) / kThreads;
+    return np > 8 ? Shape{0, 0} : Shape{kThreads, np == 7 ? 8 : np};
   }
-  const int np = (pieces + kThreads - 1) / kThreads;
-  return np > 8 ? Shape{0, 0} : Shape{kThreads, np == 7 ? 8 : np};
+  if (pieces < (fwd ? 4 : 16)) return {pieces, 1};
+  if (pieces < 16) return {(pieces + 1) / 2, 2};
+  Shape best = {(pieces + 3) / 4, 4};
+  int most = 0;
+  for (int np = 2; np <= 3; ++np) {
+    const int L = (pieces + np - 1) / np;
+    const int used = L > 64 ? 0 : pieces * (64 / L) * 60 / np;  // of 64 * 60
+    if (used <= most) continue;
+    most = used;
+    best = {L, np};
+    if (!fwd && used >= 64 * 48) break;
+  }
+  return best;
 }
 
 // Workgroups of the backward that a CU holds, from the registers of a lane:
@@ -542,7 +557,7 @@ hipError_t go_shape(const NormArgs& a, const Shape& s, int n) {
 
 template <typename T>
 hipError_t fwd_t(NormArgs a) {
-  const Shape s = shape_of(a.D, Piece<T>::V);
+  const Shape s = shape_of(a.D, Piece<T>::V, true);
   if (s.lanes == 0) {
     norm_fwd_long_kernel<T><<<min(a.rows, 2048), kThreads, 0, a.stream>>>(a);
     return hipGetLastError();
@@ -553,7 +568,7 @@ hipError_t fwd_t(NormArgs a) {
 
 template <typename T>
 hipError_t bwd_t(NormArgs a) {
-  const Shape s = shape_of(a.D, Piece<T>::V);
+  const Shape s = shape_of(a.D, Piece<T>::V, false);
   const int n = norm_partials(a.rows, a.D, (int)sizeof(T));
   hipError_t err;
   if (s.lanes == 0) {
@@ -573,7 +588,7 @@ hipError_t bwd_t(NormArgs a) {
 }  // namespace
 
 int norm_partials(int rows, int D, int elem_bytes) {
-  const Shape s = shape_of(D, 16 / elem_bytes);
+  const Shape s = shape_of(D, 16 / elem_bytes, false);
   if (s.lanes == 0) return rows < 64 ? rows : 64;
   return min(groups_of(s, rows, false), 256 * bwd_resident(s.np, 16 / elem_bytes, s.lanes > 64));
 }
