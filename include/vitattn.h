@@ -410,14 +410,15 @@ enum vitattn_type { VITATTN_BF16 = 0, VITATTN_FP16 = 1, VITATTN_FP32 = 2 };
  *                 contiguous, no alignment beyond the element's); all of
  *                 `type`. y and dx must not overlap themselves. y may be x (the
  *                 same strides); dx may be dy (the same strides), except where
- *                 dw or db is wanted and D is above 16,384 (fp32: 8,192); any
- *                 other output whose address range meets an input's is rejected.
+ *                 dw or db is wanted and D is above 16,384 (fp32: 8,192). An output
+ *                 (or workspace) whose address range meets that of any other
+ *                 operand is rejected.
  *   w, b, dw, db: [D], contiguous, of `weight_type` (x's type or fp32). w and b
  *                 may be null (ones, zeros); so may dw and db (not wanted).
  *   mean, rstd  : fp32, one per row in the order [B][H][N]; the forward takes
  *                 null for both (not wanted).
  *   eps         : finite, >= 0.
- *   D           : 1 .. 2^24, else VITATTN_E_UNSUPPORTED; B*H*N below 2^31 - 2^20.
+ *   D           : 1 .. 2^24, else VITATTN_E_UNSUPPORTED; B*H*N below 2^31 - 2^22.
  *   workspace   : vitattn_layer_norm_bwd_workspace_bytes() bytes, 16-byte
  *                 aligned, if dw or db is wanted (partial sums; overwritten).
  * Sums and statistics are fp32; y and dx are rounded once, to their type. dw
@@ -455,7 +456,7 @@ enum vitattn_pos_type { VITATTN_POS_I32 = 0, VITATTN_POS_I64 = 1, VITATTN_POS_F3
  *              or share elements (the same address is rejected).
  *              Each may be its input (the same strides); if both are, q and k
  *              may be interleaved heads of one tensor. Any other output whose
- *              address range meets an input's is rejected.
+ *              address range meets an input's or the positions' is rejected.
  *   positions: [B or 1][N][n_axes] of pos_type at element strides pos_batch (0:
  *              shared by the samples), pos_row and pos_axis.
  *   d        : 2 R <= d <= 65,536; R <= 128, n_axes <= 8 (VITATTN_E_UNSUPPORTED
@@ -507,8 +508,9 @@ int vitattn_rotary(const void* q, vitattn_strides sq, void* q_out, vitattn_strid
  *              0 unless up to 256 queries meet many keys; then both passes split
  *              the keys over workgroups whose results are joined), 16-byte aligned.
  * Scores, statistics, sums and the difference are fp32; P and dS are rounded
- * to bf16 as operands of the matrix cores, o and the gradients once at the end. Results are bitwise deterministic, and a head's results do not depend
- * on the call it is part of. No atomics.
+ * to bf16 as operands of the matrix cores, o and the gradients once at the end. Results are
+ * bitwise deterministic, and a head's results do not depend on the call it is
+ * part of. No atomics.
  */
 size_t vitattn_diff_fwd_workspace_bytes(int B, int H, int Nq, int Nk, int d, int e);
 int vitattn_diff_fwd(const void* q, vitattn_strides sq, const void* k, vitattn_strides sk, const void* v,

@@ -13,6 +13,17 @@ bool ranges_overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return a != nullptr && b != nullptr && x < y + nb && y < x + na;
 }
+struct Range {
+  const void* p;  // null: absent
+  size_t bytes;
+};
+// whether one of the first n_out ranges meets any other
+bool outputs_meet(const Range* r, int n_out, int n) {
+  for (int o = 0; o < n_out; ++o)
+    for (int i = o + 1; i < n; ++i)
+      if (ranges_overlap(r[o].p, r[o].bytes, r[i].p, r[i].bytes)) return true;
+  return false;
+}
 
 // ------------------------------------------------------------ row kernels
 
@@ -61,7 +72,8 @@ constexpr int kNormMaxWidth = 1 << 24;
 
 int check_norm(int B, int H, int N, int D, int type, int weight_type) {
   if (B < 1 || H < 1 || N < 1 || D < 1) return VITATTN_E_INVAL;
-  if ((double)B * H * N > 0x7fffffff - (1 << 20)) return VITATTN_E_INVAL;  // row indexes of the last round stay below 2^31
+  // a row's index plus the rows of one round of workgroups (up to 2^21, at one piece a row) stays below 2^31
+  if ((double)B * H * N > 0x7fffffff - (1 << 22)) return VITATTN_E_INVAL;
   if (D > kNormMaxWidth || elem_bytes(type) == 0) return VITATTN_E_UNSUPPORTED;
   return weight_type == type || weight_type == VITATTN_FP32 ? VITATTN_OK : VITATTN_E_UNSUPPORTED;
 }
@@ -131,9 +143,11 @@ int vitattn_layer_norm_fwd(const void* x, vitattn_strides sx, const void* w, con
       return VITATTN_E_INVAL;
     if (!isfinite(eps) || eps < 0.f) return VITATTN_E_INVAL;
     if (check_rows_map(sx, B, H, N, D, false) || check_rows_map(sy, B, H, N, D, true)) return VITATTN_E_INVAL;
-    if (x == y ? !same_strides(sx, sy, B, H, N)
-               : ranges_overlap(x, span_of(sx, B, H, N, D) * size, y, span_of(sy, B, H, N, D) * size))
-      return VITATTN_E_INVAL;
+    if (x == y && !same_strides(sx, sy, B, H, N)) return VITATTN_E_INVAL;
+    const size_t stats = sizeof(float) * B * H * N, wbytes = (size_t)D * wsize;
+    const Range ranges[] = {{y, span_of(sy, B, H, N, D) * size}, {mean, stats}, {rstd, stats},
+                            {x == y ? nullptr : x, span_of(sx, B, H, N, D) * size}, {w, wbytes}, {b, wbytes}};
+    if (outputs_meet(ranges, 3, 6)) return VITATTN_E_INVAL;
     vitattn::NormArgs a = {};
     a.x = x;
     a.w = w;
@@ -176,15 +190,18 @@ int vitattn_layer_norm_bwd(const void* x, vitattn_strides sx, const void* w, con
         check_rows_map(sdx, B, H, N, D, true))
       return VITATTN_E_INVAL;
     // dx may replace dy; x is still read by rows too long for registers
-    const size_t out = span_of(sdx, B, H, N, D) * size;
-    if (ranges_overlap(x, span_of(sx, B, H, N, D) * size, dx, out) ||
-        (dy == dx ? !same_strides(sdy, sdx, B, H, N) : ranges_overlap(dy, span_of(sdy, B, H, N, D) * size, dx, out)))
-      return VITATTN_E_INVAL;
+    if (dy == dx && !same_strides(sdy, sdx, B, H, N)) return VITATTN_E_INVAL;
     const bool sums = dw != nullptr || db != nullptr;
+    const size_t need = sums ? vitattn_layer_norm_bwd_workspace_bytes(B, H, N, D, type) : 0;
+    const size_t stats = sizeof(float) * B * H * N, wbytes = (size_t)D * wsize;
+    const Range ranges[] = {{dx, span_of(sdx, B, H, N, D) * size}, {dw, wbytes}, {db, wbytes},
+                            {sums ? workspace : nullptr, need}, {x, span_of(sx, B, H, N, D) * size},
+                            {dy == dx ? nullptr : dy, span_of(sdy, B, H, N, D) * size}, {mean, stats}, {rstd, stats},
+                            {w, wbytes}};
+    if (outputs_meet(ranges, 4, 9)) return VITATTN_E_INVAL;
     // the column sums of rows too long for registers read dy after dx is written
     if (dy == dx && sums && D > 256 * 8 * (16 / size)) return VITATTN_E_INVAL;
-    if (sums && (!aligned16(workspace) || workspace_bytes < vitattn_layer_norm_bwd_workspace_bytes(B, H, N, D, type)))
-      return VITATTN_E_WORKSPACE;
+    if (sums && (!aligned16(workspace) || workspace_bytes < need)) return VITATTN_E_WORKSPACE;
     vitattn::NormArgs a = {};
     a.x = x;
     a.dy = dy;
@@ -241,11 +258,14 @@ int vitattn_rotary(const void* q, vitattn_strides sq, void* q_out, vitattn_strid
     void* out[2] = {q_out, k_out};
     const vitattn_strides si[2] = {sq, sk}, so[2] = {sq_out, sk_out};
     const int heads[2] = {Hq, Hk};
+    const size_t pos_bytes = (size_t)((B - 1) * pos_batch + (N - 1) * pos_row + (n_axes - 1) * pos_axis + 1) *
+                             (pos_type == VITATTN_POS_I64 ? 8 : 4);
     for (int o = 0; o < 2; ++o) {
       if (heads[o] == 0) continue;
       if (check_rows_map(si[o], B, heads[o], N, d, false) || check_rows_map(so[o], B, heads[o], N, d, true))
         return VITATTN_E_INVAL;
       const size_t bytes = span_of(so[o], B, heads[o], N, d) * size;
+      if (ranges_overlap(positions, pos_bytes, out[o], bytes)) return VITATTN_E_INVAL;
       for (int i = 0; i < 2; ++i) {
         if (heads[i] == 0 || (i == o && in[i] == out[o])) continue;
         if (ranges_overlap(in[i], span_of(si[i], B, heads[i], N, d) * size, out[o], bytes)) {

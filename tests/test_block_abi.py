@@ -85,6 +85,31 @@ def test_norm_backward_overlaps():
     norm_bwd(b, INVAL, dx=b[4], **rows)  # dw would be summed from an overwritten dy
 
 
+def test_norm_outputs_over_other_operands():
+    """An output over an operand that is not its row's input: the weights, the statistics, another output."""
+    b = Bufs()
+    norm_fwd(b, INVAL, y=b[1])
+    norm_fwd(b, INVAL, mean=b[0])
+    norm_fwd(b, INVAL, rstd=b[4])  # mean's
+    norm_fwd(b, INVAL, rstd=b[3] + 1016)  # y's last bytes
+    norm_fwd(b, INVAL, mean=b[2] + 60)  # the bias's
+    norm_bwd(b, INVAL, dx=b[1])
+    norm_bwd(b, INVAL, dx=b[2])
+    norm_bwd(b, INVAL, dw=b[0] + 64)
+    norm_bwd(b, INVAL, dw=b[7] + 62)  # db's
+    norm_bwd(b, INVAL, ws=b[0])
+    norm_bwd(b, INVAL, ws=b[5])
+
+
+def test_norm_most_rows():
+    """A row's index and one round's rows beyond it stay below 2^31."""
+    for n in (2 ** 31 - 1, 2 ** 31 - 2 ** 21, 2 ** 31 - 2 ** 22):
+        one = dict(B=1, H=1, N=n, D=8, sx=S(0, 0, 0))
+        norm_fwd(Bufs(), INVAL, sy=S(0, 0, 8), y=2 ** 40, mean=2 ** 41, rstd=2 ** 42, **one)
+        assert lib().vitattn_layer_norm_bwd_workspace_bytes(1, 1, n, 8, BF16) == 0
+    assert lib().vitattn_layer_norm_bwd_workspace_bytes(1, 1, 2 ** 31 - 2 ** 22 - 1, 8, BF16) > 0
+
+
 def test_norm_workspace_bytes():
     f = lib().vitattn_layer_norm_bwd_workspace_bytes
     assert f(1, 1, 1, 64, BF16) == 2 * 64 * 4
@@ -125,6 +150,12 @@ def test_rotary_more_pairs_than_supported_and_overlaps():
     rotary(b, INVAL, q2=b[0], sq2=S(640, 32, 128))  # in place, with other strides
     rotary(b, INVAL, q2=b[2], k2=b[0])
     rotary(b, INVAL, k2=b[1])  # both outputs at one address
+
+
+def test_rotary_output_over_the_positions():
+    b = Bufs()
+    rotary(b, INVAL, q2=b[4])
+    rotary(b, INVAL, k2=b[4] + 72)  # the last position's
 
 
 def diff_fwd(b, want, **o):
