@@ -100,11 +100,12 @@ def open_library(path):
 def library():
     """Load libvitattn.so once. Raises if it has not been built."""
     global _lib
-    with _lock:
-        if _lib is None:
-            if not os.path.exists(LIB_PATH):
-                raise ImportError(f"{LIB_PATH} is missing: build it with paper_2405_15780_amd._build.build()")
-            _lib = open_library(LIB_PATH)
+    if _lib is None:
+        with _lock:
+            if _lib is None:
+                if not os.path.exists(LIB_PATH):
+                    raise ImportError(f"{LIB_PATH} is missing: build it with paper_2405_15780_amd._build.build()")
+                _lib = open_library(LIB_PATH)
     return _lib
 
 
@@ -614,10 +615,16 @@ def _norm_rows(*ts):
     return order, (1,) * (3 - lead) + tuple(x.shape[i] for i in order)
 
 
+@functools.lru_cache(maxsize=1024)
+def _strides(batch, head, row):
+    """Strides(batch, head, row), which nobody writes."""
+    return Strides(batch, head, row)
+
+
 def _norm_strides(t, order, D):
     if order is None:
-        return Strides(0, 0, D)
-    return Strides(*[0] * (3 - len(order)), *(0 if t.shape[i] == 1 else t.stride(i) for i in order))
+        return _strides(0, 0, D)
+    return _strides(*[0] * (3 - len(order)), *(0 if t.shape[i] == 1 else t.stride(i) for i in order))
 
 
 def _norm_weights(x, D, weight, bias):
@@ -719,8 +726,8 @@ def layer_norm_bwd(x, weight, mean, rstd, dy, want_dweight=True, want_dbias=True
 
 def _strides_any(t):
     """Strides of a [B, H, N, d] view, zeros for dims of size one."""
-    s, n = t.stride(), t.shape
-    return Strides(s[0] if n[0] != 1 else 0, s[1] if n[1] != 1 else 0, s[2] if n[2] != 1 else 0)
+    (b, h, r, _), (B, H, N, _) = t.stride(), t.shape
+    return _strides(b if B != 1 else 0, h if H != 1 else 0, r if N != 1 else 0)
 
 
 @functools.lru_cache(maxsize=None)
@@ -744,9 +751,12 @@ def rotary_fwd(q, k, positions, sections, base=10000.0, interleaved=False, joint
     into, which may be q and k. Returns q', or (q', k') if there is a k."""
     torch = _torch()
     code = _type_code(q, "q")
+    device, dtype = q.device, q.dtype
     for t, n in ((q, "q"), (k, "k")):
-        if t is not None and not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == q.dtype and t.dim() == 4
-                                  and t.device == q.device and (t.stride(3) == 1 or t.shape[3] == 1)):
+        if t is None:
+            continue
+        if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == device and t.dim() == 4
+                and (t.stride(3) == 1 or t.shape[3] == 1)):
             raise TypeError(f"{n} must be a 4-D CUDA tensor [B, H, N, d] of q's type and device with unit stride along d")
     B, Hq, N, d = q.shape
     Hk = 0
@@ -757,8 +767,8 @@ def rotary_fwd(q, k, positions, sections, base=10000.0, interleaved=False, joint
     sections = tuple(map(int, sections))
     A = len(sections)
     pos_code = _pos_codes().get(positions.dtype) if isinstance(positions, torch.Tensor) else None
-    if pos_code is None or positions.device != q.device or tuple(positions.shape) not in ((N, A), (B, N, A)):
-        raise TypeError(f"positions must be an int32, int64 or float32 tensor [{N}, {A}] or [{B}, {N}, {A}] on {q.device}")
+    if pos_code is None or positions.device != device or positions.shape not in ((N, A), (B, N, A)):
+        raise TypeError(f"positions must be an int32, int64 or float32 tensor [{N}, {A}] or [{B}, {N}, {A}] on {device}")
     k_out, sk, sk_out = None, _NO_STRIDES, _NO_STRIDES
     if out is None:
         q_out = torch.empty_like(q)
@@ -768,7 +778,7 @@ def rotary_fwd(q, k, positions, sections, base=10000.0, interleaved=False, joint
         q_out, k_out = out if k is not None else ((out[0] if isinstance(out, (tuple, list)) else out), None)
         for t, like, n in ((q_out, q, "out q"), (k_out, k, "out k")):
             if like is not None:
-                _expect(t, n, q.dtype, like.shape, q.device)
+                _expect(t, n, dtype, like.shape, device)
     if k is not None:
         sk, sk_out = _strides_any(k), _strides_any(k_out)
     sp = positions.stride()
@@ -788,8 +798,8 @@ _NO_STRIDES = Strides(0, 0, 0)
 def _diff_strides(t):
     """Strides of a [B, H, N, d] view as the attention takes them; those of dims
     of size one do not matter and are replaced."""
-    s, n = t.stride(), t.shape
-    return Strides(s[0] if n[0] != 1 else 0, s[1] if n[1] != 1 else 0, s[2] if n[2] != 1 else n[3])
+    (b, h, r, _), (B, H, N, d) = t.stride(), t.shape
+    return _strides(b if B != 1 else 0, h if H != 1 else 0, r if N != 1 else d)
 
 
 def _diff_args(q, k, v, lam, key_lens):
