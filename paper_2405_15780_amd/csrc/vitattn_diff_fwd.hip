@@ -10,8 +10,8 @@
 // the tiles of V (and both maps' K) are fetched once for the two maps and both
 // land on the same SIMD (QW = 4), where one wave's exponentials run beside the
 // other's matrix ops. K_1, K_2 and V stream through LDS in tiles of 32 KB keys
-// (two slots each, K one tile ahead of V), rows past the sample's keys read
-// as zeros. The pipeline within a tile is vitattn_fwd.hip's: one stream of
+// (R slots each, K one tile ahead of V), rows past the sample's keys read as
+// zeros. The pipeline within a tile is vitattn_fwd.hip's: one stream of
 // score ops (tile j + 1) then PV ops (tile j), operands read two ops ahead,
 // exponentials, tile requests and the next maximum spread over it.
 //
@@ -26,6 +26,13 @@
 // a second kernel joins them, O_m = sum_s exp(LSE_s - LSE) O_s. The split
 // depends on Nq and Nk alone, so a head's bits do not depend on the call it is
 // part of.
+//
+// Bound by the vector work beside the matrix cores and the power limit for long
+// sequences: 4 heads, 32,768 keys, d = 64, e = 128 3.1 ms, 3.3 TFLOP at 1.06
+// PFLOP/s, where a large matrix product runs at 1.35; by one and a third rounds of
+// workgroups at 64 heads of 1,024, d = 32 (48 us); by HBM for one query: 8 heads
+// over 131,072 keys 106 us with the join (537 MB, 5.1 TB/s), 256 heads over 32,768
+// 722 us (5.9 TB/s).
 #include "vitattn_diff.h"
 
 namespace vitattn {
@@ -45,8 +52,8 @@ constexpr int exp_window(int NS, int CPB, int KB, int NOPS) {
   return w;
 }
 
-template <int DQ, int QS, int DV, int KB, int QW, bool SPLIT>
-__global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a, int n_qtiles, int n_split,
+template <int DQ, int QS, int DV, int KB, int QW, int R, bool SPLIT>
+__global__ __launch_bounds__(128 * QW, QW == 1 && R == 4 ? 1 : 2) void diff_fwd_kernel(const DiffArgs a, int n_qtiles, int n_split,
                                                                int split_keys, int total, float c) {
   constexpr int NW = 2 * QW;
   constexpr int BM = 32 * QW, BN = 32 * KB;
@@ -56,16 +63,34 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
   constexpr int NV = 2 * KB * CPB;                   // PV ops per tile
   __shared__ __attribute__((aligned(1024))) char kbuf0[2 * KT];  // K_1, then K_2
   __shared__ __attribute__((aligned(1024))) char kbuf1[2 * KT];
+  __shared__ __attribute__((aligned(1024))) char kbuf2[R > 2 ? 2 * KT : 1];
+  __shared__ __attribute__((aligned(1024))) char kbuf3[R > 2 ? 2 * KT : 1];
   __shared__ __attribute__((aligned(1024))) char vbuf0[VT];
   __shared__ __attribute__((aligned(1024))) char vbuf1[VT];
+  __shared__ __attribute__((aligned(1024))) char vbuf2[R > 2 ? VT : 1];
+  __shared__ __attribute__((aligned(1024))) char vbuf3[R > 2 ? VT : 1];
   // The second map's outputs, 32 columns at a time: over the K tiles where these
   // are large enough (no wave reads K in the last stage), which leaves a CU room
   // for another workgroup.
   constexpr bool OVER_K = 2 * KT >= QW * 4096;
   __shared__ float xown[OVER_K ? 1 : QW][16][64];
-  char* const kbuf[2] = {kbuf0, kbuf1};
-  char* const vbuf[2] = {vbuf0, vbuf1};
-  debug_poison_lds(kbuf0, kbuf1, vbuf0, vbuf1, xown);
+  static_assert(R == 2 || R == 4, "slots, a multiple of the two score buffers");
+  // (selected at compile time: a table of them would be one of generic addresses)
+  auto kbuf = [&](auto I) __attribute__((always_inline)) -> char* {
+    constexpr int i = decltype(I)::value % R;
+    if constexpr (i == 0) return kbuf0;
+    else if constexpr (i == 1) return kbuf1;
+    else if constexpr (i == 2) return kbuf2;
+    else return kbuf3;
+  };
+  auto vbuf = [&](auto I) __attribute__((always_inline)) -> char* {
+    constexpr int i = decltype(I)::value % R;
+    if constexpr (i == 0) return vbuf0;
+    else if constexpr (i == 1) return vbuf1;
+    else if constexpr (i == 2) return vbuf2;
+    else return vbuf3;
+  };
+  debug_poison_lds(kbuf0, kbuf1, kbuf2, kbuf3, vbuf0, vbuf1, vbuf2, vbuf3, xown);
   float(*const xbuf)[16][64] = OVER_K ? reinterpret_cast<float(*)[16][64]>(kbuf0) : xown;
 
   const int work = work_item(a.key_lens, total);
@@ -126,7 +151,7 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
   kfrag.init(lane);
   TrFrag<DV> vfrag;
   vfrag.init(lane);
-  // a tile's requests: K_1, K_2 (tile j + 2), V (tile j + 1)
+  // a stage's requests: K_1, K_2 (tile j + R), V (tile j + R - 1)
   constexpr int PK = decltype(dma)::PER_WAVE, PV = decltype(dmv)::PER_WAVE, NDMA = 2 * PK + PV;
 
   f32x16 oacc[CPB];
@@ -135,14 +160,18 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
   float m_run = -INFINITY;  // running max of scaled logits, log2 units
   float l_part = 0.f;
 
-  const int n_kt = (Nk + BN - 1) / BN;
-  dma.issue(rk1, 0, ldk, kbuf[0]);
-  dma.issue(rk2, 0, ldk, kbuf[0] + KT);
-  dmv.issue(rv, 0, ldv, vbuf[0]);
-  dma.issue(rk1, BN, ldk, kbuf[1]);
-  dma.issue(rk2, BN, ldk, kbuf[1] + KT);
-  wait_vmem();
-  __syncthreads();
+  // (tiles past the last are zeros whose scores are masked)
+  const int tiles = (Nk + BN - 1) / BN, n_kt = R == 2 ? tiles : (tiles + R - 1) / R * R;
+  dma.issue(rk1, 0, ldk, kbuf0);
+  dma.issue(rk2, 0, ldk, kbuf0 + KT);
+  static_for<1, R>([&](auto T) __attribute__((always_inline)) {
+    constexpr int t = decltype(T)::value;
+    dma.issue(rk1, t * BN, ldk, kbuf(T));
+    dma.issue(rk2, t * BN, ldk, kbuf(T) + KT);
+    dmv.issue(rv, (t - 1) * BN, ldv, vbuf(std::integral_constant<int, t - 1>{}));
+  });
+  wait_vmem_leave<(R - 2) * NDMA>();
+  barrier_lds();
 
   constexpr int NE = 16 * KB;
   auto mask_ragged = [&](f32x16 (&s)[KB], int tile) {
@@ -179,19 +208,19 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
 #pragma unroll
   for (int i = 0; i < NS; ++i) {
     if (i % QS == 0) sa[i / QS] = zero16();
-    sa[i / QS] = mfma32(lds_frag_row(kbuf[0] + koff, (i / QS) * 32 * 2 * DQ + kfrag.at(i % QS)), qf[i % QS], sa[i / QS]);
+    sa[i / QS] = mfma32(lds_frag_row(kbuf0 + koff, (i / QS) * 32 * 2 * DQ + kfrag.at(i % QS)), qf[i % QS], sa[i / QS]);
   }
-  if (n_kt == 1) mask_ragged(sa, 0);
+  mask_ragged(sa, 0);
   // (finite, so that a first tile of scores -inf leaves zeros and not NaN)
   m_run = fmaxf(max_halves(fmaxf(fmaxf(max_quarter(sa, 0), max_quarter(sa, 1)), fmaxf(max_quarter(sa, 2), max_quarter(sa, 3)))) * c,
                 -3.0e38f);
-  __syncthreads();  // kbuf[0] is refilled by the first stage
+  barrier_lds();  // kbuf0 is refilled by the first stage
 
-  auto stage = [&](auto parity, auto has_next, f32x16 (&s)[KB], f32x16 (&sn)[KB], int j) {
+  auto stage = [&](auto parity, auto has_next, f32x16 (&s)[KB], f32x16 (&sn)[KB], int j) __attribute__((always_inline)) {
     constexpr int P = decltype(parity)::value;
     constexpr bool NEXT = decltype(has_next)::value;
-    const char* ks = kbuf[1 - P] + koff;
-    const char* vs = vbuf[P];
+    const char* ks = kbuf(std::integral_constant<int, P + 1>{}) + koff;
+    const char* vs = vbuf(parity);
     const float m_cur = m_run;
     float ls0 = 0.f, ls1 = 0.f;
     u32x4 pq[2 * KB];
@@ -249,9 +278,9 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
         }
         if constexpr (i % STEP == STEP - 1 && i / STEP < NDMA) {
           constexpr int q = i / STEP;
-          if constexpr (q < PK) dma.issue_one(rk1, (j + 2) * BN, ldk, kbuf[P], q);
-          else if constexpr (q < 2 * PK) dma.issue_one(rk2, (j + 2) * BN, ldk, kbuf[P] + KT, q - PK);
-          else dmv.issue_one(rv, (j + 1) * BN, ldv, vbuf[1 - P], q - 2 * PK);
+          if constexpr (q < PK) dma.issue_one(rk1, (j + R) * BN, ldk, kbuf(parity), q);
+          else if constexpr (q < 2 * PK) dma.issue_one(rk2, (j + R) * BN, ldk, kbuf(parity) + KT, q - PK);
+          else dmv.issue_one(rv, (j + R - 1) * BN, ldv, vbuf(std::integral_constant<int, P + R - 1>{}), q - 2 * PK);
         }
         exp_slice(IC, std::integral_constant<int, W>{});
         if constexpr (i >= W && i < W + 4) {
@@ -263,8 +292,8 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
       });
       l_part += ls0 + ls1;
       fold_max(fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])));
-      wait_vmem();
-      __syncthreads();
+      wait_vmem_leave<(R - 2) * NDMA>();
+      barrier_lds();
     } else {
       exp_slice(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
       bf16x8 vq[3];
@@ -281,19 +310,24 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
     }
   };
 
-  using P0 = std::integral_constant<int, 0>;
-  using P1 = std::integral_constant<int, 1>;
   int j = 0;
-  for (; j + 2 < n_kt; j += 2) {
-    stage(P0{}, std::true_type{}, sa, sb, j);
-    stage(P1{}, std::true_type{}, sb, sa, j + 1);
+  for (; j + R < n_kt; j += R) {
+    static_for<0, R / 2>([&](auto IC) __attribute__((always_inline)) {
+      constexpr int p = 2 * decltype(IC)::value;
+      stage(std::integral_constant<int, p>{}, std::true_type{}, sa, sb, j + p);
+      stage(std::integral_constant<int, p + 1>{}, std::true_type{}, sb, sa, j + p + 1);
+    });
   }
-  if (j + 1 < n_kt) {
-    stage(P0{}, std::true_type{}, sa, sb, j);
-    stage(P1{}, std::false_type{}, sb, sa, j + 1);
+  if (R > 2 || j + 1 < n_kt) {
+    static_for<0, R / 2>([&](auto IC) __attribute__((always_inline)) {
+      constexpr int p = 2 * decltype(IC)::value;
+      stage(std::integral_constant<int, p>{}, std::true_type{}, sa, sb, j + p);
+      stage(std::integral_constant<int, p + 1>{}, std::bool_constant<(p + 2 < R)>{}, sb, sa, j + p + 1);
+    });
   } else {
-    stage(P0{}, std::false_type{}, sa, sb, j);
+    stage(std::integral_constant<int, 0>{}, std::false_type{}, sa, sb, j);
   }
+  wait_vmem();  // requests past the last tile still write LDS
 
   const float l = sum_halves(l_part);
   const float inv = 1.0f / l;
@@ -348,57 +382,63 @@ __global__ __launch_bounds__(128 * QW, 2) void diff_fwd_kernel(const DiffArgs a,
   }
 }
 
-// Joins the splits of one query row (bh, query), a workgroup per row: Q waves for
-// each map, each of which takes a Q-th of the splits. A lane weighs split s; the
-// outputs are added in split order, eight in flight, then the waves' in order.
+// Joins the splits of one query row (bh, query), a workgroup per row and 64
+// columns: Q waves for each map, each of which takes a Q-th of the splits. The
+// outputs of U splits are requested beside their LSE, the first U before the
+// maximum is known, and added in split order, then the waves' in order.
 template <int Q>
 __global__ __launch_bounds__(128 * Q) void diff_join_kernel(const DiffArgs a, int n_split) {
-  constexpr int U = 8;
-  __shared__ float tops[2 * Q], sums[2 * Q], acc[2][Q][192];
+  constexpr int U = 16;
+  __shared__ float tops[2 * Q], sums[2 * Q], acc[2][Q][64];
   debug_poison_lds(tops, sums, acc);
   const long long row = blockIdx.x, rows = (long long)a.B * a.H * a.Nq;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = wave / Q, share = wave % Q;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m = wave / Q, share = wave % Q, col = 64 * blockIdx.y + lane;
   const long long bh = row / a.Nq;
   const int i = (int)(row - bh * a.Nq);
   const int b = (int)(bh / a.H), head = (int)(bh - (long long)b * a.H);
   const long long base = (bh * n_split * 2 + m) * a.Nq + i, step = 2LL * a.Nq;
   const float* lses = a.work + rows * n_split * 2 * a.e + base;
   const float* outs = a.work + base * a.e;
-  float top = -INFINITY, sum = 0.f;
-  for (int s = share * 64 + lane; s < n_split; s += 64 * Q) top = fmaxf(top, lses[s * step]);
+  // this wave's splits
+  const int s0 = (int)((long long)n_split * share / Q), s1 = (int)((long long)n_split * (share + 1) / Q);
+  float lse[U], x[U];
+  auto load = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
-  for (int x = 32; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+    for (int u = 0; u < U; ++u) {
+      lse[u] = -INFINITY;
+      x[u] = 0.f;
+      if (s + u < s1) {
+        lse[u] = lses[(s + u) * step];
+        if (col < a.e) x[u] = outs[(s + u) * step * a.e + col];
+      }
+    }
+  };
+  load(s0);
+  float top = -INFINITY;
+  for (int s = s0 + lane; s < s1; s += 64) top = fmaxf(top, lses[s * step]);
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
   if (lane == 0) tops[wave] = top;
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < Q; ++w) top = fmaxf(top, tops[m * Q + w]);
   const float ref = top == -INFINITY ? 0.f : top;  // no keys at all
-  for (int s = share * 64 + lane; s < n_split; s += 64 * Q) sum += expf(lses[s * step] - ref);
-#pragma unroll
-  for (int x = 32; x >= 1; x >>= 1) sum += __shfl_xor(sum, x, 64);
-  if (lane == 0) sums[wave] = sum;
-  // columns lane, lane + 64, lane + 128 of this wave's splits
-  float o[3] = {0.f, 0.f, 0.f};
-  const int s0 = (int)((long long)n_split * share / Q), s1 = (int)((long long)n_split * (share + 1) / Q);
-  for (int s = s0; s < s1; s += U) {
-    float w[U], x[U][3];
+  float o = 0.f, sum = 0.f;
+  for (int s = s0;;) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const bool on = s + u < s1;
-      const float l = on ? lses[(s + u) * step] : -INFINITY;
-      const bool any = l != -INFINITY;  // an empty split wrote no outputs
-      w[u] = any ? expf(l - ref) : 0.f;
-#pragma unroll
-      for (int t = 0; t < 3; ++t)
-        x[u][t] = any && lane + 64 * t < a.e ? outs[(s + u) * step * a.e + lane + 64 * t] : 0.f;
+      const bool any = lse[u] != -INFINITY;  // an empty split wrote no outputs
+      const float w = any ? expf(lse[u] - ref) : 0.f;
+      sum += w;
+      o += any ? w * x[u] : 0.f;
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int t = 0; t < 3; ++t) o[t] += w[u] * x[u][t];
+    s += U;
+    if (s >= s1) break;
+    load(s);
   }
-#pragma unroll
-  for (int t = 0; t < 3; ++t) acc[m][share][lane + 64 * t] = o[t];
+  if (lane == 0) sums[wave] = sum;
+  acc[m][share][lane] = o;
   __syncthreads();
   float l[2];
 #pragma unroll
@@ -407,17 +447,17 @@ __global__ __launch_bounds__(128 * Q) void diff_join_kernel(const DiffArgs a, in
 #pragma unroll
     for (int w = 0; w < Q; ++w) l[mm] += sums[mm * Q + w];
   }
-  if (lane == 0 && share == 0 && a.lse)
+  if (lane == 0 && share == 0 && blockIdx.y == 0 && a.lse)
     a.lse[(bh * 2 + m) * a.Nq + i] = top == -INFINITY ? -INFINITY : ref + logf(m ? l[1] : l[0]);
   const float lam = lam_of(a.lam, a.lam_bf16, head);
-  for (int col = threadIdx.x; col < a.e; col += 128 * Q) {
+  if (wave == 0 && col < a.e) {
     float y[2];
 #pragma unroll
     for (int mm = 0; mm < 2; ++mm) {
       const float inv = l[mm] > 0.f || l[mm] != l[mm] ? 1.f / l[mm] : 0.f;
       y[mm] = 0.f;
 #pragma unroll
-      for (int w = 0; w < Q; ++w) y[mm] += acc[mm][w][col];
+      for (int w = 0; w < Q; ++w) y[mm] += acc[mm][w][lane];
       y[mm] *= inv;
       if (a.maps) a.maps[((bh * 2 + mm) * a.Nq + i) * a.e + col] = y[mm];
     }
@@ -426,11 +466,11 @@ __global__ __launch_bounds__(128 * Q) void diff_join_kernel(const DiffArgs a, in
   }
 }
 
-template <int DQ, int QS, int DV, int KB, int QW, bool SPLIT>
+template <int DQ, int QS, int DV, int KB, int QW, int R, bool SPLIT>
 hipError_t go(const DiffArgs& a, int split_keys, int n_split) {
   const int n_qtiles = (a.Nq + 32 * QW - 1) / (32 * QW);
   const int total = a.B * a.H * n_split * n_qtiles;
-  diff_fwd_kernel<DQ, QS, DV, KB, QW, SPLIT>
+  diff_fwd_kernel<DQ, QS, DV, KB, QW, R, SPLIT>
       <<<total, 128 * QW, 0, a.stream>>>(a, n_qtiles, n_split, split_keys, total, a.scale * kLog2e);
   return hipGetLastError();
 }
@@ -445,7 +485,7 @@ template <int DQ, int QS, int DV, int KB>
 bool two_query_waves(const DiffArgs& a) {
   if (a.Nq <= 64) return true;
   static ResidentCache cache;
-  const int cus = cache.get(reinterpret_cast<const void*>(diff_fwd_kernel<DQ, QS, DV, KB, 4, false>), 512).cus;
+  const int cus = cache.get(reinterpret_cast<const void*>(diff_fwd_kernel<DQ, QS, DV, KB, 4, 2, false>), 512).cus;
   if (cus <= 0) return false;
   const long long wide = (long long)a.B * a.H * ((a.Nq + 127) / 128), narrow = (long long)a.B * a.H * ((a.Nq + 63) / 64);
   const long long left = narrow % (2 * cus);
@@ -453,21 +493,45 @@ bool two_query_waves(const DiffArgs& a) {
   return two < (double)((wide + cus - 1) / cus);
 }
 
+// Split keys, each workgroup a few KB of its own: bound by the latency of the tile
+// requests. Up to 32 queries take one wave per map, tiles of 32 keys and four slots,
+// three tiles ahead (d = 64, e = 128, one query, against two waves, 64 keys and two
+// slots: 131,072 keys 1 head 33.2 -> 28.8 us, 32,768 keys 4 heads 26.0 -> 23.3, 32
+// heads 103 -> 101). Of two slots twice as many workgroups fit: taken where all of
+// the grid is resident then and would not be with four (8 heads, 131,072 keys 115 ->
+// 106 us; twice the grid 101 -> 109). The bits are the same. The 96-wide tile keeps
+// its shape (its four slots leave one workgroup per CU: 115.2 us against 115.7).
+template <int DQ, int QS, int DV, int KB>
+hipError_t go_split(const DiffArgs& a, int split_keys, int n_split) {
+  if constexpr (DQ < 96) {
+    if (a.Nq <= 32) {
+      static ResidentCache two, four;
+      const int n2 = two.get(reinterpret_cast<const void*>(diff_fwd_kernel<DQ, QS, DV, 1, 1, 2, true>), 128).workgroups;
+      const int n4 = four.get(reinterpret_cast<const void*>(diff_fwd_kernel<DQ, QS, DV, 1, 1, 4, true>), 128).workgroups;
+      const long long grid = (long long)a.B * a.H * n_split;
+      if (grid > n4 && grid <= n2) return go<DQ, QS, DV, 1, 1, 2, true>(a, split_keys, n_split);
+      return go<DQ, QS, DV, 1, 1, 4, true>(a, split_keys, n_split);
+    }
+  }
+  return go<DQ, QS, DV, KB, 2, 2, true>(a, split_keys, n_split);
+}
+
 template <int DQ, int QS, int DV, int KB>
 hipError_t go_tile(const DiffArgs& a) {
   const int split_keys = diff_split_keys(a.Nq, a.Nk);
   if (split_keys == 0) {
     if constexpr (DV > 64)
-      if (!two_query_waves<DQ, QS, DV, KB>(a)) return go<DQ, QS, DV, KB, 4, false>(a, 0, 1);
-    return go<DQ, QS, DV, KB, 2, false>(a, 0, 1);
+      if (!two_query_waves<DQ, QS, DV, KB>(a)) return go<DQ, QS, DV, KB, 4, 2, false>(a, 0, 1);
+    return go<DQ, QS, DV, KB, 2, 2, false>(a, 0, 1);
   }
   const int n_split = (a.Nk + split_keys - 1) / split_keys;
-  const hipError_t err = go<DQ, QS, DV, KB, 2, true>(a, split_keys, n_split);
+  const hipError_t err = go_split<DQ, QS, DV, KB>(a, split_keys, n_split);
   if (err != hipSuccess) return err;
-  // (a row of 128 splits takes 13 us with eight waves per map; of few splits there are many rows)
-  const unsigned rows = (unsigned)(a.B * a.H * a.Nq);
-  if (n_split > 32) diff_join_kernel<8><<<rows, 1024, 0, a.stream>>>(a, n_split);
-  else diff_join_kernel<1><<<rows, 128, 0, a.stream>>>(a, n_split);
+  // (one query of 8 heads in 128 splits: eight waves per map 117 us for both kernels,
+  // one 123; 64 queries 161 and 151)
+  const dim3 grid(a.B * a.H * a.Nq, (a.e + 63) / 64);
+  if (n_split > 32 && a.Nq <= 16) diff_join_kernel<8><<<grid, 1024, 0, a.stream>>>(a, n_split);
+  else diff_join_kernel<1><<<grid, 128, 0, a.stream>>>(a, n_split);
   return hipGetLastError();
 }
 
