@@ -12,6 +12,12 @@
 // whole number of turns. In fp32 a coordinate of 1e6 would leave 0.06 of a
 // radian. What remains is at most half a turn, and fp32 holds its sine and
 // cosine to about an ulp.
+//
+// Measured: 188,416 tokens of 16 query and 16 key heads of 64, bf16, three axes
+// 321 us (1.55 GB, 4.8 TB/s; a large copy reaches 5.1); 2 x 5,003 tokens of 12 and
+// 4 heads of 80, fp32, adjacent pairs 22 us (102 MB, 4.6 TB/s); one token 5.7 us,
+// nearly all of it the launch. Requesting the next heads' pieces before these are
+// written (U of them) took the first from 376 us to 328.
 #include "vitattn_rows.h"
 
 namespace vitattn {
@@ -131,7 +137,8 @@ hipError_t go(const RotaryArgs& a) {
   const int pieces = turned + rest;
   const int heads = a.heads[0] + a.heads[1];
   const long long blocks = ((long long)a.N * pieces + kThreads - 1) / kThreads;
-  // heads per thread: as many as leave eight workgroups per CU
+  // heads per thread: as many as leave eight workgroups per CU, so that long
+  // sequences form their angles once per 16 heads and short ones still fill the card
   int group = 16;
   while (group > 1 && blocks * a.B * ((heads + group - 1) / group) < 2048) group /= 2;
   const dim3 grid((unsigned)blocks, (heads + group - 1) / group, a.B);
