@@ -79,6 +79,29 @@ def test_few_queries_over_many_keys(d, e, Nq, Nk):
     check(*inputs(2, 1, Nq, Nk, d, e, seed=Nk + Nq))
 
 
+@pytest.mark.parametrize("d,e", [(32, 64), (64, 128)])
+@pytest.mark.parametrize("Nq,Nk", [(1, 1090), (2, 16385), (1, 20000), (16, 17409), (17, 20000), (32, 33500), (33, 17000), (5, 66001)])
+def test_joins_of_few_and_many_splits(d, e, Nq, Nk):
+    """3 to 128 splits of 512 keys and more, the last one short; one wave per map joins them, or eight."""
+    print(f"case diff joins Nq={Nq} Nk={Nk} d={d} e={e}", flush=True)
+    check(*inputs(1, 2, Nq, Nk, d, e, seed=Nk + Nq), None, [Nk])
+
+
+@pytest.mark.parametrize("d,e", [(32, 64), (64, 64), (64, 128), (72, 144)])
+def test_split_keys_of_many_heads_are_those_of_one(d, e):
+    """The same bits whatever form the grid takes: 1,024 workgroups against 128."""
+    import paper_2405_15780_amd as va
+
+    print(f"case diff split forms d={d} e={e}", flush=True)
+    q, k, v, lam, _ = inputs(1, 8, 2, 65536, d, e, seed=d + e)
+    o, o2, lse = va.diff_fwd(q, k, v, lam)
+    for h in (0, 5, 7):
+        m = slice(2 * h, 2 * h + 2)
+        one = va.diff_fwd(q[:, m], k[:, m], v[:, h:h + 1], lam[h:h + 1])
+        for got, ref in zip((o[:, h:h + 1], o2[:, m], lse[:, m]), one):
+            assert torch().equal(got, ref)
+
+
 @pytest.mark.parametrize("lens", [[300, 0, 1], [64, 65, 299], [0, 0, 0], [128, 300, 31]])
 @pytest.mark.parametrize("d,e", [(32, 64), (64, 128), (72, 144)])
 def test_key_lens(lens, d, e):
