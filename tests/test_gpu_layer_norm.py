@@ -93,6 +93,17 @@ def test_widths(D, dtype):
     check(x, w, b, dy, *run(x, w, b, dy), dtype, dtype)
 
 
+@pytest.mark.parametrize("D", [4, 13, 25, 31, 33, 57, 100, 121, 125, 160, 185, 191, 193, 255, 380, 384, 500, 601, 640, 768, 1001, 1025, 1400,
+                               1537, 2047])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_widths_by_lanes_and_pieces(D, dtype):
+    """One to four pieces per lane, lanes of a row that divide a wave and that do not, a last piece of a few elements."""
+    print(f"case layer norm D={D} {dtype} by lanes", flush=True)
+    x, dy = make((301, D), dtype, D), make((301, D), dtype, D + 1)
+    w, b = make((D,), "float32", D + 2, 1.0), make((D,), "float32", D + 3)
+    check(x, w, b, dy, *run(x, w, b, dy), dtype, "float32")
+
+
 @pytest.mark.parametrize("rows", [1, 2, 63, 64, 65, 1000, 20011])
 @pytest.mark.parametrize("D", [8, 72, 768])
 def test_row_counts(rows, D):
