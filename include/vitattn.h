@@ -521,8 +521,8 @@ size_t vitattn_diff_bwd_workspace_bytes(int B, int H, int Nq, int Nk, int d, int
 int vitattn_diff_bwd(const void* q, vitattn_strides sq, const void* k, vitattn_strides sk, const void* v,
                      vitattn_strides sv, const void* lam, int lam_type, const int* key_lens, const float* maps,
                      const float* lse, const void* dout, vitattn_strides sdo, void* dq, vitattn_strides sdq, void* dk,
-                     vitattn_strides sdk, void* dv, vitattn_strides sdv, void* dlam, int B, int H, int Nq, int Nk, int d, int e, float scale, void* workspace,
-                     size_t workspace_bytes, void* stream);
+                     vitattn_strides sdk, void* dv, vitattn_strides sdv, void* dlam, int B, int H, int Nq, int Nk, int d,
+                     int e, float scale, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Human-readable name of a status code (static storage, never NULL). */
 const char* vitattn_status_str(int status);

@@ -373,12 +373,13 @@ size_t vitattn_diff_bwd_workspace_bytes(int B, int H, int Nq, int Nk, int d, int
 int vitattn_diff_bwd(const void* q, vitattn_strides sq, const void* k, vitattn_strides sk, const void* v,
                      vitattn_strides sv, const void* lam, int lam_type, const int* key_lens, const float* maps,
                      const float* lse, const void* dout, vitattn_strides sdo, void* dq, vitattn_strides sdq, void* dk,
-                     vitattn_strides sdk, void* dv, vitattn_strides sdv, void* dlam, int B, int H, int Nq, int Nk, int d, int e, float scale, void* workspace,
-                     size_t workspace_bytes, void* stream) {
+                     vitattn_strides sdk, void* dv, vitattn_strides sdv, void* dlam, int B, int H, int Nq, int Nk, int d,
+                     int e, float scale, void* workspace, size_t workspace_bytes, void* stream) {
   try {
     int st = check_diff_sizes(B, H, Nq, Nk, d, e);
     if (st != VITATTN_OK) return st;
-    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(maps) || !aligned16(lse) || !aligned16(dout) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || (key_lens && !aligned_to(key_lens, 4)))
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(maps) || !aligned16(lse) || !aligned16(dout) ||
+        !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || (key_lens && !aligned_to(key_lens, 4)))
       return VITATTN_E_INVAL;
     if (!scale_ok(scale)) return VITATTN_E_INVAL;
     if ((st = check_lam(lam, lam_type)) != VITATTN_OK) return st;

@@ -25,8 +25,8 @@
 // ones are off by at most 2^-39, nothing beside the row's others. Everything else
 // is fp32 until the outputs are rounded once. One of the two differences dP - D
 // comes from the matrix cores, whose accumulator starts at -D_1; the other is that
-// plus D_1 - D_2. No atomics: the sums of dlam's partials
-// are added in a fixed order, and each output row by one workgroup.
+// plus D_1 - D_2. No atomics: the sums of dlam's partials are added in a fixed
+// order, and each output row by one workgroup.
 //
 // Bound as the forward is. 4 heads of 32,768 tokens, d = 64, e = 128: dK/dV 4.3 ms
 // (4.4 TFLOP, 1.02 PFLOP/s), dQ 3.0 (3.3 TFLOP, 1.1), rows 0.03, the board at its
