@@ -608,7 +608,10 @@ def _norm_rows(*ts):
     which the first tensor's memory has them (None: one dimension, all of them
     contiguous) and their sizes padded to three."""
     x = ts[0]
-    if all(t.is_contiguous() for t in ts):
+    for t in ts:
+        if not t.is_contiguous():
+            break
+    else:
         return None, (1, 1, x.numel() // x.shape[-1])
     lead = x.dim() - 1
     order = sorted(range(lead), key=lambda i: (-x.stride(i), i))
@@ -629,18 +632,17 @@ def _norm_strides(t, order, D):
 
 def _norm_weights(x, D, weight, bias):
     """The type of weight and bias, checked (x's without any)."""
-    wt = None
+    wt, dtype, device, torch = None, x.dtype, x.device, _torch()
     for t, n in ((weight, "weight"), (bias, "bias")):
         if t is None:
             continue
-        torch = _torch()
-        if not (isinstance(t, torch.Tensor) and (t.dtype == x.dtype or t.dtype == torch.float32) and t.dim() == 1
-                and t.numel() == D and t.device == x.device and t.is_contiguous()):
-            raise TypeError(f"{n} must be a contiguous {x.dtype} or torch.float32 CUDA tensor of shape ({D},) on {x.device}")
+        if not (isinstance(t, torch.Tensor) and (t.dtype == dtype or t.dtype == torch.float32) and t.shape == (D,)
+                and t.device == device and t.is_contiguous()):
+            raise TypeError(f"{n} must be a contiguous {dtype} or torch.float32 CUDA tensor of shape ({D},) on {device}")
         if wt is not None and t.dtype != wt:
             raise TypeError("weight and bias must be of one type")
         wt = t.dtype
-    return x.dtype if wt is None else wt
+    return dtype if wt is None else wt
 
 
 def _ptr(t):
@@ -667,19 +669,19 @@ def layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, out=None, stats=True):
     order, n = _norm_rows(x4, y4)
     mean = rstd = None
     if stats:
-        mean, rstd = torch.empty((2, *n), dtype=torch.float32, device=x.device).unbind(0)
+        mean = torch.empty(x.shape[:-1] if order is None else n, dtype=torch.float32, device=x.device)
+        rstd = torch.empty_like(mean)
     _call(x, library().vitattn_layer_norm_fwd, x4.data_ptr(), _norm_strides(x4, order, D), _ptr(weight), _ptr(bias),
           y.data_ptr(), _norm_strides(y4, order, D), _ptr(mean), _ptr(rstd), *n, D, eps, code,
           VITATTN_FP32 if wt == torch.float32 else code)
-    if stats:
+    if order is not None and stats:
         mean, rstd = _norm_stat_out(mean, order, x4, x.shape), _norm_stat_out(rstd, order, x4, x.shape)
     return y, mean, rstd
 
 
 def _norm_stat_out(t, order, x4, shape):
     """A statistic in the kernel's order of rows, as x.shape[:-1]."""
-    if order is not None:
-        t = t.view([x4.shape[i] for i in order]).permute(sorted(range(len(order)), key=lambda i: order[i]))
+    t = t.view([x4.shape[i] for i in order]).permute(sorted(range(len(order)), key=lambda i: order[i]))
     return t.reshape(shape[:-1])
 
 
@@ -708,19 +710,18 @@ def layer_norm_bwd(x, weight, mean, rstd, dy, want_dweight=True, want_dbias=True
     order, n = _norm_rows(x4, dy4, dx4)
     if order is not None:
         mean, rstd = (t.reshape(x4.shape[:-1]).permute(order) for t in (mean, rstd))
-    mean, rstd = mean.contiguous(), rstd.contiguous()
+    mean, rstd = mean.contiguous(), rstd.contiguous()  # (rows of x in memory order)
     dw = torch.empty(D, dtype=wt, device=device) if want_dweight and weight is not None else None
     db = torch.empty(D, dtype=wt, device=device) if want_dbias else None
-    lib = library()
-    if workspace is None:
-        need = lib.vitattn_layer_norm_bwd_workspace_bytes(*n, D, code) if dw is not None or db is not None else 0
-        workspace = torch.empty(max(need, 4) // 4, dtype=torch.float32, device=device)
-    else:
-        _expect_workspace(workspace, device)
+    lib, size = library(), 0
+    if workspace is not None:
+        size = _expect_workspace(workspace, device).numel() * workspace.element_size()
+    elif dw is not None or db is not None:
+        size = lib.vitattn_layer_norm_bwd_workspace_bytes(*n, D, code)
+        workspace = torch.empty(size // 4, dtype=torch.float32, device=device)
     _call(x, lib.vitattn_layer_norm_bwd, x4.data_ptr(), _norm_strides(x4, order, D), _ptr(weight), mean.data_ptr(),
           rstd.data_ptr(), dy4.data_ptr(), _norm_strides(dy4, order, D), dx4.data_ptr(), _norm_strides(dx4, order, D),
-          _ptr(dw), _ptr(db), *n, D, code, VITATTN_FP32 if wt == torch.float32 else code, workspace.data_ptr(),
-          workspace.numel() * workspace.element_size())
+          _ptr(dw), _ptr(db), *n, D, code, VITATTN_FP32 if wt == torch.float32 else code, _ptr(workspace), size)
     return dx, dw, db
 
 
