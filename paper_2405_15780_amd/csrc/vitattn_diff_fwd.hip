@@ -330,7 +330,9 @@ __global__ __launch_bounds__(128 * QW, QW == 1 && R == 4 ? 1 : 2) void diff_fwd_
   wait_vmem();  // requests past the last tile still write LDS
 
   const float l = sum_halves(l_part);
-  const float inv = 1.0f / l;
+  // (l is at least 1 but for a query whose scores are all -inf, which has zeros and an
+  // LSE of -inf, as a sample without keys has and as the join makes of such splits)
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
   const float lse = (m_run + __log2f(l)) * kLn2;
   if constexpr (SPLIT) {
     if (qrow < a.Nq) {

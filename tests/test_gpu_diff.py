@@ -198,6 +198,38 @@ def test_first_tile_of_infinite_scores():
         assert a.isfinite().all() and ((a.float() - b.float()).abs() <= off * (1 + b.float().abs())).all()
 
 
+@pytest.mark.parametrize("maps", ["both", "second"])
+@pytest.mark.parametrize("d,e", [(32, 64), (64, 64), (64, 128), (72, 144)])
+@pytest.mark.parametrize("Nq,Nk", [(40, 300), (300, 300), (3, 5000), (40, 2000), (100, 9000)])
+def test_rows_whose_scores_are_all_infinite(Nq, Nk, d, e, maps):
+    """A query that scores -inf against every key (a product past fp32's range) is one without keys, whether the
+    keys are split or not: zeros, an LSE of -inf and no part in any gradient. The others do not see it."""
+    print(f"case diff all -inf Nq={Nq} Nk={Nk} d={d} e={e} {maps}", flush=True)
+    t = torch()
+    q, k, v, lam, do = inputs(1, 2, Nq, Nk, d, e, seed=26)
+    q[..., 0], k[..., 0] = 0, -2.0 ** 70
+    bad, good = [0, 2, Nq - 1], [i for i in range(Nq) if i not in (0, 2, Nq - 1)]
+    do0 = do.clone()
+    do0[:, :, bad] = 0
+    ref = run(q, k, v, lam, do0)
+    m = slice(0 if maps == "both" else 1, None, 1 if maps == "both" else 2)
+    q[:, m, bad, 0] = 2.0 ** 70
+    got = run(q, k, v, lam, do)
+    for n in ("o", "o2", "lse", "dq"):
+        assert t.equal(got[n][:, :, good], ref[n][:, :, good]), n
+    for n in ("o2", "dq"):
+        assert not got[n][:, m, bad].any(), n
+    assert (got["lse"][:, m, bad] == -float("inf")).all()
+    if maps == "both":
+        assert not got["o"][:, :, bad].any()
+        for n in ("dk", "dv", "dlam"):
+            assert t.equal(got[n], ref[n]), n
+    else:
+        assert t.equal(got["o"][:, :, bad], got["o2"][:, 0::2, bad].bfloat16())
+        assert t.equal(got["dk"][:, 1::2], ref["dk"][:, 1::2]) and t.equal(got["dlam"], ref["dlam"])
+        assert all(got[n].isfinite().all() for n in ("dq", "dk", "dv"))
+
+
 def test_broadcast_heads_and_batches():
     t = torch()
     q, k, v, lam, do = inputs(2, 3, 60, 80, 32, 64, seed=15)
