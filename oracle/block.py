@@ -81,8 +81,8 @@ def diff_attention(q, k, v, lam, scale, key_lens=None, dout=None):
     """q (B, 2H, Nq, d), k (B, 2H, Nk, d), v (B, H, Nk, e), lam (H): a dict of o,
     o2 (B, 2H, Nq, e: each map's output) and lse (B, 2H, Nq), and with dout of dq,
     dk, dv and dlam. Under the same names with "_off" stands a bound of what the
-    rounding to 16 bits of P and dS (as operands) and of the outputs can change, half
-    a step of bf16 (2^-8) each, with fp32 sums."""
+    rounding to bf16 of P and dS (as operands) and of the outputs can change, half a
+    step (2^-8) each, with fp32 sums."""
     q, k, v = (np.asarray(x, dtype=np.float64) for x in (q, k, v))
     B, H, Nk, e = v.shape
     Nq, d = q.shape[2], q.shape[3]
@@ -133,9 +133,6 @@ def diff_attention(q, k, v, lam, scale, key_lens=None, dout=None):
                 ds = P[m] * (dP - D[:, None])
                 grow = fp32 * P[m] * (np.abs(g) @ np.abs(vv).T + np.abs(D)[:, None])
                 ds_off = (2 * u + u * u) * np.abs(ds) + (1 + 2 * u) * P[m] * off[:, None] + grow
-                # P may be held in fp16 times 2^14: below that type's normal numbers
-                # (2^-14) its steps are 2^-24, so P is off by at most half of 2^-38
-                ds_off += 2.0 ** -39 * np.abs(dP - D[:, None])
                 c = scale * f
                 for name, x, xo in (("dq", c * ds @ k[b, 2 * h + m, :n], abs(c) * ds_off @ np.abs(k[b, 2 * h + m, :n])),
                                     ("dk", c * ds.T @ q[b, 2 * h + m], abs(c) * ds_off.T @ np.abs(q[b, 2 * h + m]))):

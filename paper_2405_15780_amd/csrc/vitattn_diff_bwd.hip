@@ -18,12 +18,11 @@
 //      workgroups as in the forward, and a fourth kernel adds the shares in order.
 //
 // P_1 - lam P_2 and dS are rounded to bf16 as matrix-core operands, and P to
-// fp16 where role V hands it over: 10 bits of fraction against bf16's 7 (dK is
-// 2.4e-3 off in norm and not 2.9e-3), and products with it need no unpacking.
-// Every P carries a factor 2^14 (in the LSE that is subtracted; it leaves with the
-// outputs' scale), so that fp16 holds P from 2^-28 to 1 to all its bits; smaller
-// ones are off by at most 2^-39, nothing beside the row's others. Everything else
-// is fp32 until the outputs are rounded once. One of the two differences dP - D
+// bf16 where role V hands it over: with fp32's range of exponents, since dK of a
+// key that every query gives little weight is a sum of small P alone (fp16 has
+// three bits more, dK 2.4e-3 off in norm and not 2.9e-3, and even with a factor
+// 2^14 made such rows coarse below P = 2^-28 and zero below 2^-39). Everything
+// else is fp32 until the outputs are rounded once. One of the two differences dP - D
 // comes from the matrix cores, whose accumulator starts at -D_1; the other is that
 // plus D_1 - D_2. No atomics: the sums of dlam's partials are added in a fixed
 // order, and each output row by one workgroup.
@@ -42,11 +41,10 @@ namespace {
 
 // Workspace: the shares of dQ where the keys are split, fp32 [bh][split][map]
 // [query][d]; then per (b, h) and block of 32 queries 128 floats, [-D_1 | D_1 - D_2 |
-// LSE_1 log2 e - 14 | LSE_2 log2 e - 14] of 32 each; then the partial sums of D_2,
+// LSE_1 log2 e | LSE_2 log2 e] of 32 each; then the partial sums of D_2,
 // [bh][row-pass workgroup]. Rows past the last query hold zeros and an LSE of
 // +inf, which makes their P zero; so do rows without keys.
 constexpr int kStat = 128;
-constexpr float kShift = 14.f, kUnshift = 1.f / 16384.f;  // the factor of P
 constexpr int kRowBlock = 64;  // query rows of a row-pass workgroup
 constexpr int kKeyBlock = 128;  // keys of a wide dK/dV workgroup, or of two narrow ones
 
@@ -91,8 +89,8 @@ __global__ __launch_bounds__(256) void diff_rowdot_kernel(const DiffArgs a, floa
     if (col == 0 && row < 32 * query_blocks(a.Nq)) {
       float l1 = INFINITY, l2 = INFINITY;
       if (row < a.Nq) {
-        l1 = a.lse[(2LL * bh) * a.Nq + row] * kLog2e - kShift;
-        l2 = a.lse[(2LL * bh + 1) * a.Nq + row] * kLog2e - kShift;
+        l1 = a.lse[(2LL * bh) * a.Nq + row] * kLog2e;
+        l2 = a.lse[(2LL * bh + 1) * a.Nq + row] * kLog2e;
         if (l1 == -INFINITY) l1 = INFINITY;
         if (l2 == -INFINITY) l2 = INFINITY;
       }
@@ -108,15 +106,6 @@ __global__ __launch_bounds__(256) void diff_rowdot_kernel(const DiffArgs a, floa
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = total;
   __syncthreads();
   if (threadIdx.x == 0) partial[blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-}
-
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-// accumulator registers 8*ks .. 8*ks+7 as fp16
-__device__ __forceinline__ uint4 to_half8(const f32x16& a, int ks) {
-  half8 r;
-#pragma unroll
-  for (int t = 0; t < 8; ++t) r[t] = (_Float16)a[8 * ks + t];
-  return __builtin_bit_cast(uint4, r);
 }
 
 // Widest window of ops that a block's 16 rows of vector work may ride on (row r
@@ -315,8 +304,8 @@ __global__ __launch_bounds__(128 * KBW, KBW == 2 && DV > 64 ? 1 : 2) void diff_d
           cur[1][r] = p2;
           wv[r] = w;
           if constexpr ((r & 7) == 7) {
-            xb[0][r >> 3][lane] = to_half8(cur[0], r >> 3);
-            xb[1][r >> 3][lane] = to_half8(cur[1], r >> 3);
+            xb[0][r >> 3][lane] = __builtin_bit_cast(uint4, acc_to_operand(cur[0], r >> 3));
+            xb[1][r >> 3][lane] = __builtin_bit_cast(uint4, acc_to_operand(cur[1], r >> 3));
             on[r >> 3] = acc_to_operand(wv, r >> 3);
           }
         };
@@ -393,9 +382,12 @@ __global__ __launch_bounds__(128 * KBW, KBW == 2 && DV > 64 ? 1 : 2) void diff_d
         f32x16 s1, s2;
         auto row = [&](auto RC) __attribute__((always_inline)) {
           constexpr int r = decltype(RC)::value;
-          // (the sum with zero is the form that takes a 16-bit factor)
-          float x1 = __builtin_fmaf((float)__builtin_bit_cast(half8, pm[0][r >> 3])[r & 7], cur[r], 0.f);
-          float x2 = __builtin_fmaf((float)__builtin_bit_cast(half8, pm[1][r >> 3])[r & 7], cur[r] + dd[r >> 2][r & 3], 0.f);
+          auto p_of = [&](int m) {
+            const uint32_t w = __builtin_bit_cast(u32x4, pm[m][r >> 3])[(r & 7) >> 1];
+            return __uint_as_float((r & 1) ? (w & 0xffff0000u) : (w << 16));
+          };
+          float x1 = p_of(0) * cur[r];
+          float x2 = p_of(1) * (cur[r] + dd[r >> 2][r & 3]);
           pin(x1);
           pin(x2);
           s1[r] = x1;
@@ -476,13 +468,13 @@ __global__ __launch_bounds__(128 * KBW, KBW == 2 && DV > 64 ? 1 : 2) void diff_d
       for (int g = 0; g < 4; ++g) {
         const int col = 32 * cb + 8 * g + 4 * h;
         if (col < a.e)
-          put4_bf16(out + col, real ? acc[cb][4 * g] * kUnshift : 0.f, real ? acc[cb][4 * g + 1] * kUnshift : 0.f,
-                    real ? acc[cb][4 * g + 2] * kUnshift : 0.f, real ? acc[cb][4 * g + 3] * kUnshift : 0.f);
+          put4_bf16(out + col, real ? acc[cb][4 * g] : 0.f, real ? acc[cb][4 * g + 1] : 0.f,
+                    real ? acc[cb][4 * g + 2] : 0.f, real ? acc[cb][4 * g + 3] : 0.f);
       }
   } else {
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      const float f = (m ? -lam * a.scale : a.scale) * kUnshift;
+      const float f = m ? -lam * a.scale : a.scale;
       uint16_t* out = a.dk + map_head(a.mdk, b, head, m) + (long long)key * a.mdk.ld;
 #pragma unroll
       for (int cb = 0; cb < NCQ; ++cb)
@@ -714,7 +706,7 @@ __global__ __launch_bounds__(64 * NW, DV > 128 ? 1 : 2) void diff_dq_kernel(cons
   if (qrow >= a.Nq) return;
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
-    const float f = (m ? -lam * a.scale : a.scale) * kUnshift;
+    const float f = m ? -lam * a.scale : a.scale;
     uint16_t* out = a.dq + map_head(a.mdq, b, head, m) + (long long)qrow * a.mdq.ld;
     float* share = a.work + ((((long long)bh * n_split + sp) * 2 + m) * a.Nq + qrow) * a.d;
 #pragma unroll

@@ -230,6 +230,20 @@ def test_rows_whose_scores_are_all_infinite(Nq, Nk, d, e, maps):
         assert all(got[n].isfinite().all() for n in ("dq", "dk", "dv"))
 
 
+@pytest.mark.parametrize("d,e", [(32, 64), (64, 64), (64, 128), (72, 144)])
+@pytest.mark.parametrize("Nq", [130, 3])
+def test_keys_that_every_query_scores_low(Nq, d, e):
+    """A key's gradient is a sum over its column of P. Where that is small throughout (2^-20 to 2^-86), each row of
+    dK and dV still has the accuracy of the others, relative to its own size: the bounds below are P's multiples."""
+    print(f"case diff low keys Nq={Nq} d={d} e={e}", flush=True)
+    q, k, v, lam, do = inputs(1, 2, Nq, 200, d, e, seed=27)
+    q[..., 0] = 4.0
+    for j in range(16):
+        k[:, :, 7 * j, 0] = -(14 + 3 * j) * d ** 0.5 / 4
+    got = check(q, k, v, lam, do)
+    assert got["dk"][:, :, :112:7].any(-1).all() and got["dv"][:, :, :112:7].any(-1).all()
+
+
 def test_broadcast_heads_and_batches():
     t = torch()
     q, k, v, lam, do = inputs(2, 3, 60, 80, 32, 64, seed=15)
