@@ -5,8 +5,14 @@
 //
 // Bound by HBM: the forward reads x and writes y, the backward reads x and dy
 // and writes dx, so a row is read once and kept in registers: the mean, then
-// the sum of squared deviations from it (no cancellation of large squares).
-// Statistics, products and sums are fp32; x, y, dy and dx are rounded once, to
+// the sum of squared deviations from it (no cancellation of large squares). A
+// mean is off by the roundings of its sum, which matters where a row's spread is
+// small beside it (constant rows): from a quarter on (is_far) the deviations'
+// own mean corrects it, and the squares are summed again about the corrected one. (32,768
+// rows of 1,024 bf16 forward 26 us, about a mean of 100 sigma 35; the wave or
+// workgroup whose rows are none such skips it.)
+// Statistics, products and sums are fp32 (a lane's sums over a row too long for
+// registers, up to 65,536 values, fp64); x, y, dy and dx are rounded once, to
 // their type.
 //
 // L lanes share a row, each holding NP pieces of 16 bytes (pieces lane, lane +
@@ -18,7 +24,9 @@
 // 26 us (134 MB, 5.1 TB/s), backward 42 us (201 MB, 4.8 TB/s) and its sums of
 // partials 4; 3,125,000 rows of 64 bf16 171 and 239 us (4.7 and 5.0 TB/s); 3,062
 // rows of 5,001 fp32 27 and 39 us (4.5 and 4.7 TB/s); one row of 768 5.5 us,
-// nearly all of it the launch.
+// nearly all of it the launch. Too long for registers: 67 million bf16 elements in
+// rows of 16,392 167 us forward, 491 backward (268 and 402 MB, 1.6 and 0.8 TB/s), in
+// rows of 2^24, a workgroup each, 13.5 and 17.2 ms.
 //
 // The backward's workgroups each take a fixed run of row groups and keep their
 // share of dw and db in registers; at the end the workgroup adds its lanes'
@@ -101,7 +109,19 @@ struct Place {
     }
     return x;
   }
+  // whether it holds anywhere in the wave (BLOCK: all of which agree)
+  __device__ __forceinline__ static bool any(bool x) { return BLOCK ? x : __any(x); }
 };
+
+// A mean that a row's spread (var about it) is small beside. Below this bound the
+// mean's error of n 2^-24 |mean|, n the length of a lane's sum and the lanes' tree,
+// is at most 4 n 2^-24 of a standard deviation. (Infinite and NaN ones are far.)
+__device__ __forceinline__ bool is_far(float mean, float var) { return mean != 0.f && !(mean * mean < 16.f * var); }
+// variance from the mean of squares q and of deviations c (NaN stays NaN)
+__device__ __forceinline__ float var_of(float q, float c) {
+  const float v = q - c * c;
+  return v < 0.f ? 0.f : v;
+}
 
 // A row's pieces in this lane's registers.
 template <typename T, int NP>
@@ -168,26 +188,46 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_kernel(const NormArgs a) {
       for (int i = 0; i < NP; ++i)
 #pragma unroll
         for (int e = 0; e < V; ++e) s += x[u].p[i].get(e);
-      const float mean = at.sum(s, lds) * inv;
-      float q = 0.f;
+      float mean = at.sum(s, lds) * inv;
+      // this lane's sums of the deviations from m and of their squares
+      auto deviations = [&](float m, float& c, float& q) __attribute__((always_inline)) {
+        c = q = 0.f;
 #pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const int n = a.D - (lane + i * L) * V;
-        if (n >= V) {
+        for (int i = 0; i < NP; ++i) {
+          const int n = a.D - (lane + i * L) * V;
+          if (n >= V) {
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const float d = x[u].p[i].get(e) - mean;
-            q = __builtin_fmaf(d, d, q);
-          }
-        } else if (n > 0) {
+            for (int e = 0; e < V; ++e) {
+              const float d = x[u].p[i].get(e) - m;
+              c += d;
+              q = __builtin_fmaf(d, d, q);
+            }
+          } else if (n > 0) {
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const float d = e < n ? x[u].p[i].get(e) - mean : 0.f;
-            q = __builtin_fmaf(d, d, q);
+            for (int e = 0; e < V; ++e) {
+              const float d = e < n ? x[u].p[i].get(e) - m : 0.f;
+              c += d;
+              q = __builtin_fmaf(d, d, q);
+            }
           }
         }
+      };
+      float c, q;
+      deviations(mean, c, q);
+      float var = at.sum(q, lds) * inv;
+      const bool far = is_far(mean, var);
+      if (at.any(far)) {
+        deviations(mean, c, q);
+        const float m = mean + at.sum(c, lds) * inv;
+        deviations(m, c, q);
+        c = at.sum(c, lds) * inv;
+        q = at.sum(q, lds) * inv;
+        if (far) {
+          mean = m;
+          var = var_of(q, c);
+        }
       }
-      const float rstd = rsqrtf(at.sum(q, lds) * inv + a.eps);
+      const float rstd = rsqrtf(var + a.eps);
       if (at.row < 0 || r >= a.rows) continue;
       T* y = static_cast<T*>(a.y) + row_at(a, a.my, r);
 #pragma unroll
@@ -208,7 +248,7 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_kernel(const NormArgs a) {
   }
 }
 
-// Rows too long for registers: three passes over the row.
+// Rows too long for registers: three passes over the row (four about a far mean).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void norm_fwd_long_kernel(const NormArgs a) {
   constexpr int V = Piece<T>::V;
@@ -218,24 +258,37 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_long_kernel(const NormArgs 
   for (int r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T* x = static_cast<const T*>(a.x) + row_at(a, a.mx, r);
     T* y = static_cast<T*>(a.y) + row_at(a, a.my, r);
-    float s = 0.f, q = 0.f;
+    const Place<true> at(kThreads);
+    double s = 0.;
     for (int c = threadIdx.x * V; c < a.D; c += kThreads * V) {
       Piece<T> p;
       p.load(x + c, min(a.D - c, V));
 #pragma unroll
       for (int e = 0; e < V; ++e) s += p.get(e);
     }
-    const float mean = Place<true>(kThreads).sum(s, lds) * inv;
-    for (int c = threadIdx.x * V; c < a.D; c += kThreads * V) {
-      Piece<T> p;
-      p.load(x + c, min(a.D - c, V));
+    float mean = at.sum((float)s, lds) * inv, var, c;
+    auto about_mean = [&]() {  // mean deviation and mean square from `mean`
+      double sd = 0., sq = 0.;
+      for (int k = threadIdx.x * V; k < a.D; k += kThreads * V) {
+        Piece<T> p;
+        p.load(x + k, min(a.D - k, V));
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float d = p.get(e) - mean;
-        q += e < a.D - c ? d * d : 0.f;
+        for (int e = 0; e < V; ++e) {
+          const float d = e < a.D - k ? p.get(e) - mean : 0.f;
+          sd += d;
+          sq += (double)d * d;
+        }
       }
+      c = at.sum((float)sd, lds) * inv;
+      var = at.sum((float)sq, lds) * inv;
+    };
+    about_mean();
+    if (is_far(mean, var)) {
+      mean += c;
+      about_mean();
+      var = var_of(var, c);
     }
-    const float rstd = rsqrtf(Place<true>(kThreads).sum(q, lds) * inv + a.eps);
+    const float rstd = rsqrtf(var + a.eps);
     for (int c = threadIdx.x * V; c < a.D; c += kThreads * V) {
       const int n = min(a.D - c, V);
       Piece<T> p;
@@ -382,7 +435,8 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_long_kernel(const NormArgs 
     const T* dy = static_cast<const T*>(a.dy) + row_at(a, a.mdy, r);
     T* dx = static_cast<T*>(a.y) + row_at(a, a.my, r);
     const float mean = a.mean[r], rstd = a.rstd[r];
-    float s1 = 0.f, s2 = 0.f, m1 = 0.f, m2 = 0.f;
+    double s1 = 0., s2 = 0.;
+    float m1 = 0.f, m2 = 0.f;
     for (int pass = 0; pass < 2; ++pass) {
       for (int c = threadIdx.x * V; c < a.D; c += kThreads * V) {
         const int n = min(a.D - c, V);
@@ -397,7 +451,7 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_long_kernel(const NormArgs 
         for (int e = 0; e < V; ++e) {
           const float h = (p.get(e) - mean) * rstd, gw = g.get(e) * w[e];
           s1 += gw;
-          s2 += gw * h;
+          s2 += (double)gw * h;
           v[e] = rstd * (gw - m1 - h * m2);
         }
         if (pass) {
@@ -406,8 +460,8 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_long_kernel(const NormArgs 
         }
       }
       if (!pass) {
-        m1 = Place<true>(kThreads).sum(s1, lds) * inv;
-        m2 = Place<true>(kThreads).sum(s2, lds) * inv;
+        m1 = Place<true>(kThreads).sum((float)s1, lds) * inv;
+        m2 = Place<true>(kThreads).sum((float)s2, lds) * inv;
       }
     }
   }

@@ -170,6 +170,46 @@ def test_mean_far_from_zero_and_constant_rows():
     assert np.allclose(np64(rstd), 1 / np.sqrt(EPS), rtol=1e-6)
 
 
+@pytest.mark.parametrize("value", [1000.0, 1000.1, -3.3e6, 1e30])
+@pytest.mark.parametrize("D", [5, 100, 777, 1000, 3000, 5001, 8192, 8193, 40003, 1000003])
+def test_constant_rows(D, value):
+    """Deviations from the mean of equal values are zeros at any width: y is the bias and dx, dw see h = 0."""
+    print(f"case layer norm constant rows D={D} value={value}", flush=True)
+    t = torch()
+    rows = 5 if D < 10000 else 2
+    for dtype in ("float32", "bfloat16"):
+        x = t.full((rows, D), value, device="cuda").to(getattr(t, dtype))
+        w, b = make((D,), dtype, 34, mean=1.0), make((D,), dtype, 35)
+        dy = make((rows, D), dtype, 36)
+        y, mean, rstd, dx, dw, db = run(x, w, b, dy)
+        assert (mean == x[:, 0].float()).all()
+        assert np.allclose(np64(rstd), 1 / np.sqrt(EPS), rtol=1e-6)
+        assert t.equal(y, b.expand(rows, D)) and not dw.any()
+
+
+@pytest.mark.parametrize("D", [64, 100, 1000, 5001, 8193, 40003])
+@pytest.mark.parametrize("sigma", [3e-4, 1e-2])
+def test_rows_of_little_spread_about_a_far_mean(D, sigma):
+    """The mean is the fp32 number next to the true one (2^-24 of it, and as much again for the rounding of the
+    correction), the deviations x - mean are exact where x is within a factor of two of it, and the variance is
+    about the true mean. So h is off by r * 2^-23 |mean| and the usual relative part (n fp32 additions)."""
+    print(f"case layer norm little spread D={D} sigma={sigma}", flush=True)
+    t = torch()
+    g = t.Generator(device="cuda").manual_seed(D)
+    x = (1000.1 + sigma * t.randn((6, D), generator=g, device="cuda", dtype=t.float64)).float()
+    dy = make((6, D), "float32", 37)
+    y, mean, rstd, dx, dw, db = run(x, None, None, dy)
+    X = np64(x)
+    Y, M, R = ob.layer_norm(X, None, None, EPS)
+    f, n = 2.0 ** -24, 96 + D // 256
+    close(mean, M, 2 * f * np.abs(M), "mean")
+    h_off = R * 2 * f * np.abs(M)
+    # r: the variance's sum, its root, and the square of the deviation of the mean that was subtracted
+    r_off = R * f * (n + 8)
+    close(rstd, R, r_off + 1e-30, "rstd")
+    close(y, Y, h_off[:, None] * (1 + 2.0 ** -20) + (n + 12) * f * np.abs(Y), "y")
+
+
 def test_other_rows_do_not_see_a_bad_one():
     t = torch()
     x, dy = make((40, 72), "float32", 40), make((40, 72), "float32", 41)
