@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import math
+import operator
 import os
 import threading
 
@@ -34,47 +35,62 @@ class Forms(ctypes.Structure):
 
 _S = Strides
 
+
+class Int:
+    """A C int argument. ctypes would keep the low 32 bits of a larger value and
+    the entry would compute a part of the call; it gets the lowest int instead,
+    which every entry refuses (a workspace size is then 0)."""
+
+    @staticmethod
+    def from_param(x):
+        if isinstance(x, int):
+            return x if -0x80000000 <= x <= 0x7fffffff else -0x80000000
+        return c_int.from_param(x) if isinstance(x, c_int) else Int.from_param(operator.index(x))
+
+
+_I = Int
+
 _SIGNATURES = {
-    "vitattn_fwd": (c_int, [c_void_p] * 5 + [c_int] * 4 + [c_float, c_void_p]),
-    "vitattn_bwd_workspace_bytes": (c_size_t, [c_int] * 4),
-    "vitattn_bwd": (c_int, [c_void_p] * 9 + [c_int] * 4 + [c_float, c_void_p, c_size_t, c_void_p]),
-    "vitattn_bwd_rowdot": (c_int, [c_void_p] * 3 + [c_int] * 4 + [c_void_p, c_size_t, c_void_p]),
-    "vitattn_bwd_dkdv": (c_int, [c_void_p] * 7 + [c_int] * 4 + [c_float, c_void_p, c_size_t, c_void_p]),
-    "vitattn_bwd_dq": (c_int, [c_void_p] * 6 + [c_int] * 4 + [c_float, c_void_p, c_size_t, c_void_p]),
-    "vitattn_fwd_kv": (c_int, [c_void_p] * 5 + [c_int] * 5 + [c_float, c_void_p]),
-    "vitattn_bwd_kv": (c_int, [c_void_p] * 9 + [c_int] * 5 + [c_float, c_int, c_void_p, c_size_t, c_void_p]),
-    "vitattn_bwd_workspace_bytes_kv": (c_size_t, [c_int] * 6),
-    "vitattn_bwd_dkdv_ds": (c_int, [c_void_p] * 7 + [c_int] * 4 + [c_float, c_void_p, c_size_t, c_void_p]),
-    "vitattn_bwd_dq_from_ds": (c_int, [c_void_p] * 2 + [c_int] * 4 + [c_float, c_void_p, c_size_t, c_void_p]),
-    "vitattn_fwd_strided": (c_int, [c_void_p, _S] * 4 + [c_void_p] + [c_int] * 5 + [c_float, c_void_p]),
-    "vitattn_bwd_strided": (c_int, [c_void_p, _S] * 5 + [c_void_p] + [c_void_p, _S] * 3 + [c_int] * 5
-                            + [c_float, c_int, c_void_p, c_size_t, c_void_p]),
-    "vitattn_bwd_train_bf16_kv": (c_int, [c_int]),
-    "vitattn_bwd_train": (c_int, [c_void_p, _S] * 5 + [c_void_p] * 5 + [c_int] * 5
+    "vitattn_fwd": (c_int, [c_void_p] * 5 + [_I] * 4 + [c_float, c_void_p]),
+    "vitattn_bwd_workspace_bytes": (c_size_t, [_I] * 4),
+    "vitattn_bwd": (c_int, [c_void_p] * 9 + [_I] * 4 + [c_float, c_void_p, c_size_t, c_void_p]),
+    "vitattn_bwd_rowdot": (c_int, [c_void_p] * 3 + [_I] * 4 + [c_void_p, c_size_t, c_void_p]),
+    "vitattn_bwd_dkdv": (c_int, [c_void_p] * 7 + [_I] * 4 + [c_float, c_void_p, c_size_t, c_void_p]),
+    "vitattn_bwd_dq": (c_int, [c_void_p] * 6 + [_I] * 4 + [c_float, c_void_p, c_size_t, c_void_p]),
+    "vitattn_fwd_kv": (c_int, [c_void_p] * 5 + [_I] * 5 + [c_float, c_void_p]),
+    "vitattn_bwd_kv": (c_int, [c_void_p] * 9 + [_I] * 5 + [c_float, _I, c_void_p, c_size_t, c_void_p]),
+    "vitattn_bwd_workspace_bytes_kv": (c_size_t, [_I] * 6),
+    "vitattn_bwd_dkdv_ds": (c_int, [c_void_p] * 7 + [_I] * 4 + [c_float, c_void_p, c_size_t, c_void_p]),
+    "vitattn_bwd_dq_from_ds": (c_int, [c_void_p] * 2 + [_I] * 4 + [c_float, c_void_p, c_size_t, c_void_p]),
+    "vitattn_fwd_strided": (c_int, [c_void_p, _S] * 4 + [c_void_p] + [_I] * 5 + [c_float, c_void_p]),
+    "vitattn_bwd_strided": (c_int, [c_void_p, _S] * 5 + [c_void_p] + [c_void_p, _S] * 3 + [_I] * 5
+                            + [c_float, _I, c_void_p, c_size_t, c_void_p]),
+    "vitattn_bwd_train_bf16_kv": (c_int, [_I]),
+    "vitattn_bwd_train": (c_int, [c_void_p, _S] * 5 + [c_void_p] * 5 + [_I] * 5
                           + [c_float, c_void_p, c_size_t, c_void_p]),
-    "vitattn_launch_forms": (c_int, [c_int] * 6 + [ctypes.POINTER(Forms)]),
-    "vitattn_merge": (c_int, [c_void_p] * 2 + [c_int] + [c_void_p] * 2 + [c_int] * 4 + [c_void_p]),
-    "vitattn_agg_fwd": (c_int, [c_void_p] * 5 + [c_int] * 4 + [c_float, c_void_p]),
-    "vitattn_agg_bwd_workspace_bytes": (c_size_t, [c_int] * 4),
-    "vitattn_agg_bwd": (c_int, [c_void_p] * 9 + [c_int] * 4 + [c_float, c_void_p, c_size_t, c_void_p]),
-    "vitattn_ulysses_pack": (c_int, [c_void_p] * 2 + [c_int] * 5 + [c_void_p]),
-    "vitattn_ulysses_unpack": (c_int, [c_void_p] * 2 + [c_int] * 5 + [c_void_p]),
-    "vitattn_ulysses_pack_out": (c_int, [c_void_p] * 2 + [c_int] * 5 + [c_void_p]),
-    "vitattn_ulysses_unpack_out": (c_int, [c_void_p] * 2 + [c_int] * 5 + [c_void_p]),
-    "vitattn_bwd_noalloc": (c_int, [c_void_p] * 9 + [c_int] * 4 + [c_float, c_void_p]),
-    "vitattn_layer_norm_fwd": (c_int, [c_void_p, _S] + [c_void_p] * 3 + [_S] + [c_void_p] * 2 + [c_int] * 4
-                               + [c_float, c_int, c_int, c_void_p]),
-    "vitattn_layer_norm_bwd_workspace_bytes": (c_size_t, [c_int] * 5),
+    "vitattn_launch_forms": (c_int, [_I] * 6 + [ctypes.POINTER(Forms)]),
+    "vitattn_merge": (c_int, [c_void_p] * 2 + [_I] + [c_void_p] * 2 + [_I] * 4 + [c_void_p]),
+    "vitattn_agg_fwd": (c_int, [c_void_p] * 5 + [_I] * 4 + [c_float, c_void_p]),
+    "vitattn_agg_bwd_workspace_bytes": (c_size_t, [_I] * 4),
+    "vitattn_agg_bwd": (c_int, [c_void_p] * 9 + [_I] * 4 + [c_float, c_void_p, c_size_t, c_void_p]),
+    "vitattn_ulysses_pack": (c_int, [c_void_p] * 2 + [_I] * 5 + [c_void_p]),
+    "vitattn_ulysses_unpack": (c_int, [c_void_p] * 2 + [_I] * 5 + [c_void_p]),
+    "vitattn_ulysses_pack_out": (c_int, [c_void_p] * 2 + [_I] * 5 + [c_void_p]),
+    "vitattn_ulysses_unpack_out": (c_int, [c_void_p] * 2 + [_I] * 5 + [c_void_p]),
+    "vitattn_bwd_noalloc": (c_int, [c_void_p] * 9 + [_I] * 4 + [c_float, c_void_p]),
+    "vitattn_layer_norm_fwd": (c_int, [c_void_p, _S] + [c_void_p] * 3 + [_S] + [c_void_p] * 2 + [_I] * 4
+                               + [c_float, _I, _I, c_void_p]),
+    "vitattn_layer_norm_bwd_workspace_bytes": (c_size_t, [_I] * 5),
     "vitattn_layer_norm_bwd": (c_int, [c_void_p, _S] + [c_void_p] * 4 + [_S, c_void_p, _S] + [c_void_p] * 2
-                               + [c_int] * 6 + [c_void_p, c_size_t, c_void_p]),
-    "vitattn_rotary": (c_int, ([c_void_p, _S] * 2 + [c_int]) * 2 + [c_void_p] + [ctypes.c_longlong] * 3 + [c_int]
-                       + [ctypes.POINTER(c_int), c_int, ctypes.c_double] + [c_int] * 5 + [c_void_p]),
-    "vitattn_diff_fwd_workspace_bytes": (c_size_t, [c_int] * 6),
-    "vitattn_diff_fwd": (c_int, [c_void_p, _S] * 3 + [c_void_p, c_int, c_void_p] + [c_void_p, _S] + [c_void_p] * 2
-                         + [c_int] * 6 + [c_float, c_void_p, c_size_t, c_void_p]),
-    "vitattn_diff_bwd_workspace_bytes": (c_size_t, [c_int] * 6),
-    "vitattn_diff_bwd": (c_int, [c_void_p, _S] * 3 + [c_void_p, c_int] + [c_void_p] * 3
-                         + [c_void_p, _S] * 4 + [c_void_p] + [c_int] * 6 + [c_float, c_void_p, c_size_t, c_void_p]),
+                               + [_I] * 6 + [c_void_p, c_size_t, c_void_p]),
+    "vitattn_rotary": (c_int, ([c_void_p, _S] * 2 + [_I]) * 2 + [c_void_p] + [ctypes.c_longlong] * 3 + [_I]
+                       + [ctypes.POINTER(c_int), _I, ctypes.c_double] + [_I] * 5 + [c_void_p]),
+    "vitattn_diff_fwd_workspace_bytes": (c_size_t, [_I] * 6),
+    "vitattn_diff_fwd": (c_int, [c_void_p, _S] * 3 + [c_void_p, _I, c_void_p] + [c_void_p, _S] + [c_void_p] * 2
+                         + [_I] * 6 + [c_float, c_void_p, c_size_t, c_void_p]),
+    "vitattn_diff_bwd_workspace_bytes": (c_size_t, [_I] * 6),
+    "vitattn_diff_bwd": (c_int, [c_void_p, _S] * 3 + [c_void_p, _I] + [c_void_p] * 3
+                         + [c_void_p, _S] * 4 + [c_void_p] + [_I] * 6 + [c_float, c_void_p, c_size_t, c_void_p]),
     "vitattn_status_str": (ctypes.c_char_p, [c_int]),
     "vitattn_version": (ctypes.c_char_p, []),
 }
@@ -740,7 +756,7 @@ def _pos_codes():
 @functools.lru_cache(maxsize=256)
 def _c_ints(values):
     """A C array of these ints, which nobody writes."""
-    return (c_int * max(len(values), 1))(*values)
+    return (c_int * max(len(values), 1))(*map(Int.from_param, values))
 
 
 def rotary_fwd(q, k, positions, sections, base=10000.0, interleaved=False, joint=False, inverse=False, out=None):
@@ -765,7 +781,10 @@ def rotary_fwd(q, k, positions, sections, base=10000.0, interleaved=False, joint
         Bk, Hk, Nk, dk = k.shape
         if (Bk, Nk, dk) != (B, N, d):
             raise ValueError("k must be [B, Hk, N, d] with the B, N and d of q")
-    sections = tuple(map(int, sections))
+    pairs = tuple(sections)
+    sections = tuple(map(int, pairs))
+    if sections != pairs:
+        raise ValueError("sections must be whole numbers")
     A = len(sections)
     pos_code = _pos_codes().get(positions.dtype) if isinstance(positions, torch.Tensor) else None
     if pos_code is None or positions.device != device or positions.shape not in ((N, A), (B, N, A)):

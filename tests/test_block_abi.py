@@ -219,3 +219,47 @@ def test_diff_backward_workspace():
     diff_bwd(b, WS, wsb=f(2, 2, 10, 7, 32, 64) - 1)
     diff_bwd(b, INVAL, dlam=b[11] + 2)
     assert f(1, 1, 0, 7, 32, 64) == 0 and f(1, 1, 10, 7, 82, 64) == 0
+
+
+BIG = 2 ** 32  # an int of this and a valid size has the valid size's low 32 bits
+
+
+def test_sizes_past_a_c_int_are_refused_and_not_cut_off():
+    """No entry may compute the part of a call that a size's low 32 bits name."""
+    b = Bufs()
+    for o in (dict(N=BIG + 4), dict(B=BIG + 2), dict(H=BIG + 2), dict(D=BIG + 32), dict(type=BIG), dict(wtype=BIG), dict(N=-BIG + 4)):
+        norm_fwd(b, INVAL if not {"type", "wtype"} & o.keys() else UNSUP, **o)
+        norm_bwd(b, INVAL if not {"type", "wtype"} & o.keys() else UNSUP, **o)
+    f = lib().vitattn_layer_norm_bwd_workspace_bytes
+    assert f(1, 1, BIG + 5, 8, BF16) == f(1, 1, 5, BIG + 8, BF16) == f(BIG + 1, 1, 5, 8, BF16) == 0
+    for o in (dict(N=BIG + 5), dict(B=BIG + 2), dict(Hq=BIG + 4), dict(Hk=BIG + 2), dict(d=BIG + 32), dict(axes=BIG + 2), dict(pt=BIG + 1),
+              dict(flags=BIG)):
+        rotary(b, INVAL, **o)
+    rotary(b, UNSUP, type=BIG)
+    for o in (dict(B=BIG + 2), dict(H=BIG + 2), dict(Nq=BIG + 10), dict(Nk=BIG + 7)):
+        diff_fwd(b, INVAL, **o)
+        diff_bwd(b, INVAL, **o)
+    for o in (dict(d=BIG + 32), dict(e=BIG + 64), dict(lt=BIG + FP32)):
+        diff_fwd(b, UNSUP, **o)
+        diff_bwd(b, UNSUP, **o)
+    for f in (lib().vitattn_diff_fwd_workspace_bytes, lib().vitattn_diff_bwd_workspace_bytes):
+        ok = (1, 1, 3, 5000, 64, 128)
+        assert f(*ok) > 0
+        for i in range(6):
+            assert f(*(n + BIG * (i == j) for j, n in enumerate(ok))) == 0
+
+
+def test_int_arguments():
+    from paper_2405_15780_amd import binding
+
+    conv = binding.Int.from_param
+    for n in (0, 1, -1, 2 ** 31 - 1, -2 ** 31, True, np.int64(7)):
+        assert conv(n) == n
+    for n in (2 ** 31, -2 ** 31 - 1, BIG, BIG + 5, np.int64(BIG + 5)):
+        assert conv(n) == -2 ** 31
+    for bad in (1.0, "1", None):
+        with pytest.raises(TypeError):
+            conv(bad)
+    assert list(binding._c_ints((BIG + 8, 8))) == [-2 ** 31, 8]  # a section of so many pairs
+    for name, (_, args) in binding._SIGNATURES.items():
+        assert ctypes.c_int not in args or name == "vitattn_status_str"

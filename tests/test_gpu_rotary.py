@@ -177,3 +177,18 @@ def test_refusals():
         va.rotary_fwd(q, None, pos, ok, out=t.empty((1, 1, 5, 16), dtype=q.dtype, device="cuda").expand(1, 2, 5, 16))
     with pytest.raises(TypeError):
         va.rotary_fwd(q, None, pos, ok, out=t.empty((1, 2, 5, 8), dtype=q.dtype, device="cuda"))
+
+
+def test_sections_are_whole_numbers_in_range():
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    q, pos = make((1, 2, 5, 16), "bfloat16", 34), positions(5, 2, "int64", 35)
+    want = va.rotary_fwd(q, None, pos, (5, 3))
+    for same in ([5, 3], (n for n in (5, 3)), np.array([5, 3]), t.tensor([5, 3]), (5.0, 3.0)):
+        assert t.equal(va.rotary_fwd(q, None, pos, same), want)
+    with pytest.raises(ValueError):
+        va.rotary_fwd(q, None, pos, (5.5, 2.5))
+    for bad in ((2 ** 32 + 5, 3), (2 ** 31, 0)):
+        with pytest.raises(va.VitattnError):
+            va.rotary_fwd(q, None, pos, bad)
