@@ -214,8 +214,9 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_kernel(const NormArgs a) {
       };
       float c, q;
       deviations(mean, c, q);
-      float var = at.sum(q, lds) * inv;
-      const bool far = is_far(mean, var);
+      q = at.sum(q, lds);
+      float rstd = rsqrtf(__builtin_fmaf(q, inv, a.eps));
+      const bool far = is_far(mean, q * inv);
       if (at.any(far)) {
         deviations(mean, c, q);
         const float m = mean + at.sum(c, lds) * inv;
@@ -224,10 +225,9 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_kernel(const NormArgs a) {
         q = at.sum(q, lds) * inv;
         if (far) {
           mean = m;
-          var = var_of(q, c);
+          rstd = rsqrtf(var_of(q, c) + a.eps);
         }
       }
-      const float rstd = rsqrtf(var + a.eps);
       if (at.row < 0 || r >= a.rows) continue;
       T* y = static_cast<T*>(a.y) + row_at(a, a.my, r);
 #pragma unroll
@@ -266,8 +266,8 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_long_kernel(const NormArgs 
 #pragma unroll
       for (int e = 0; e < V; ++e) s += p.get(e);
     }
-    float mean = at.sum((float)s, lds) * inv, var, c;
-    auto about_mean = [&]() {  // mean deviation and mean square from `mean`
+    float mean = at.sum((float)s, lds) * inv, c, q;
+    auto about_mean = [&]() {  // mean deviation from, and sum of squares about, `mean`
       double sd = 0., sq = 0.;
       for (int k = threadIdx.x * V; k < a.D; k += kThreads * V) {
         Piece<T> p;
@@ -280,15 +280,15 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_long_kernel(const NormArgs 
         }
       }
       c = at.sum((float)sd, lds) * inv;
-      var = at.sum((float)sq, lds) * inv;
+      q = at.sum((float)sq, lds);
     };
     about_mean();
-    if (is_far(mean, var)) {
+    float rstd = rsqrtf(__builtin_fmaf(q, inv, a.eps));
+    if (is_far(mean, q * inv)) {
       mean += c;
       about_mean();
-      var = var_of(var, c);
+      rstd = rsqrtf(var_of(q * inv, c) + a.eps);
     }
-    const float rstd = rsqrtf(var + a.eps);
     for (int c = threadIdx.x * V; c < a.D; c += kThreads * V) {
       const int n = min(a.D - c, V);
       Piece<T> p;
