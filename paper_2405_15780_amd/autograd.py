@@ -85,7 +85,14 @@ class _LayerNorm:
 
 
 def _wants_grad(*ts):
-    if not _torch().is_grad_enabled():
+    """Whether a call goes through its autograd function: if any of its tensors
+    wants a gradient, and wherever one could carry a forward-mode tangent (that
+    does not set requires_grad, nor does no_grad end it), which the function
+    refuses like `attention` does."""
+    torch = _torch()
+    if torch.autograd.forward_ad._current_level >= 0:
+        return True
+    if not torch.is_grad_enabled():
         return False
     for t in ts:
         if t is not None and t.requires_grad:
