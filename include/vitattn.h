@@ -452,8 +452,8 @@ enum vitattn_pos_type { VITATTN_POS_I32 = 0, VITATTN_POS_I64 = 1, VITATTN_POS_F3
  *   q, k     : [B][Hq][N][d] and [B][Hk][N][d] (Hk = 0: no k), of `type`, at
  *              any element strides >= 0, the d elements of a row contiguous, no
  *              alignment beyond the element's.
- *   q_out, k_out: written, of the same type; they must not overlap themselves
- *              or share elements (the same address is rejected).
+ *   q_out, k_out: written, of the same type; they must not overlap themselves,
+ *              nor each other (interleaved heads of one tensor do not).
  *              Each may be its input (the same strides); if both are, q and k
  *              may be interleaved heads of one tensor. Any other output whose
  *              address range meets an input's or the positions' is rejected.

@@ -25,6 +25,80 @@ bool outputs_meet(const Range* r, int n_out, int n) {
   return false;
 }
 
+// Memory of an operand: rows of `row` bytes in up to three dimensions at byte
+// strides (sizes of one: their strides do not matter).
+typedef __int128 wide;
+struct Memory {
+  const void* p;  // null: absent
+  long long row;
+  int n[3];
+  wide stride[3];
+};
+Memory strided_memory(const void* p, const vitattn_strides& s, int n0, int n1, int n2, int D, int elem_bytes) {
+  return Memory{p, (long long)D * elem_bytes, {n0, n1, n2},
+                {(wide)s.batch * elem_bytes, (wide)s.head * elem_bytes, (wide)s.row * elem_bytes}};
+}
+
+// A step that na of the first operand's indexes and nb of the second's take.
+struct Step {
+  wide stride;
+  long long na, nb;
+};
+// Whether rows of wa bytes at i_0 s_0 + .. and rows of wb at delta + j_0 s_0 + .. meet
+// (0 <= i < na, 0 <= j < nb, steps from the longest to the shortest): the two parts
+// under a step can meet for few differences i_0 - j_0 alone, each of which is a
+// question of the same kind about the steps that are left. Interleaved views of one
+// tensor have the same steps and are settled in a few of these; out of budget
+// counts as meeting.
+bool steps_meet(const Step* s, int n, wide wa, wide wb, wide delta, int& budget) {
+  if (--budget < 0) return true;
+  wide la = wa, lb = wb;  // spans
+  for (int i = 0; i < n; ++i) {
+    la += (s[i].na - 1) * s[i].stride;
+    lb += (s[i].nb - 1) * s[i].stride;
+  }
+  if (delta >= la || -delta >= lb) return false;
+  if (n == 0) return true;
+  const wide S = s[0].stride;
+  la -= (s[0].na - 1) * S;
+  lb -= (s[0].nb - 1) * S;
+  // differences t with -lb < delta - t S < la
+  auto floor_div = [](wide x, wide y) { return x >= 0 ? x / y : -((-x + y - 1) / y); };
+  wide lo = floor_div(delta - la, S) + 1, hi = -floor_div(-(delta + lb), S) - 1;
+  if (lo < -(s[0].nb - 1)) lo = -(s[0].nb - 1);
+  if (hi > s[0].na - 1) hi = s[0].na - 1;
+  for (wide t = lo; t <= hi; ++t)
+    if (steps_meet(s + 1, n - 1, wa, wb, delta - t * S, budget)) return true;
+  return false;
+}
+bool memories_meet(const Memory& a, const Memory& b) {
+  if (a.p == nullptr || b.p == nullptr) return false;
+  const wide delta = (wide) reinterpret_cast<uintptr_t>(b.p) - (wide) reinterpret_cast<uintptr_t>(a.p);
+  wide la = a.row, lb = b.row;
+  for (int i = 0; i < 3; ++i) {
+    la += (a.n[i] - 1) * a.stride[i];
+    lb += (b.n[i] - 1) * b.stride[i];
+  }
+  if (delta >= la || -delta >= lb) return false;  // (the usual end)
+  Step s[6];
+  int n = 0;
+  for (int i = 0; i < 6; ++i) {
+    const Memory& m = i < 3 ? a : b;
+    const int size = m.n[i % 3];
+    const wide stride = m.stride[i % 3];
+    if (size == 1 || stride == 0) continue;
+    int at = 0;
+    while (at < n && s[at].stride > stride) ++at;
+    if (at == n || s[at].stride != stride) {
+      for (int k = n++; k > at; --k) s[k] = s[k - 1];
+      s[at] = Step{stride, 1, 1};
+    }
+    (i < 3 ? s[at].na : s[at].nb) += size - 1;
+  }
+  int budget = 4096;
+  return steps_meet(s, n, a.row, b.row, delta, budget);
+}
+
 // ------------------------------------------------------------ row kernels
 
 int elem_bytes(int type) { return type == VITATTN_FP32 ? 4 : type == VITATTN_BF16 || type == VITATTN_FP16 ? 2 : 0; }
@@ -253,7 +327,6 @@ int vitattn_rotary(const void* q, vitattn_strides sq, void* q_out, vitattn_strid
     if (pos_batch < 0 || pos_row < 0 || pos_axis < 0 ||
         (double)(B - 1) * pos_batch + (double)(N - 1) * pos_row + (double)(n_axes - 1) * pos_axis > 1.0e18)
       return VITATTN_E_INVAL;
-    if (Hk > 0 && q_out == k_out) return VITATTN_E_INVAL;
     const void* in[2] = {q, k};
     void* out[2] = {q_out, k_out};
     const vitattn_strides si[2] = {sq, sk}, so[2] = {sq_out, sk_out};
@@ -276,6 +349,8 @@ int vitattn_rotary(const void* q, vitattn_strides sq, void* q_out, vitattn_strid
       }
       if (in[o] == out[o] && !same_strides(si[o], so[o], B, heads[o], N)) return VITATTN_E_INVAL;
     }
+    if (Hk > 0 && memories_meet(strided_memory(q_out, sq_out, B, Hq, N, d, size), strided_memory(k_out, sk_out, B, Hk, N, d, size)))
+      return VITATTN_E_INVAL;
     vitattn::RotaryArgs a = {};
     for (int o = 0; o < 2; ++o) {
       if (heads[o] == 0) continue;

@@ -263,3 +263,20 @@ def test_int_arguments():
     assert list(binding._c_ints((BIG + 8, 8))) == [-2 ** 31, 8]  # a section of so many pairs
     for name, (_, args) in binding._SIGNATURES.items():
         assert ctypes.c_int not in args or name == "vitattn_status_str"
+
+
+def test_rotary_outputs_that_share_elements():
+    """Also where both operands are turned in place, which interleaved heads of one tensor may be."""
+    b = Bufs()
+    x = b[0]  # [2][N = 5][6 heads][32]: q the first four heads, k from head `h` on
+    fused = dict(sq=S(960, 32, 192), sq2=S(960, 32, 192), sk=S(960, 32, 192), sk2=S(960, 32, 192), q=x, q2=x)
+    for h in (0, 1, 3):
+        rotary(b, INVAL, k=x + 64 * h, k2=x + 64 * h, **fused)
+    rotary(b, INVAL, k=x + 64 * 4 + 2, k2=x + 64 * 4 + 2, **fused)  # its last element is the next row's first
+    rotary(b, INVAL, k=x + 64 * 4 - 2, k2=x + 64 * 4 - 2, **fused)
+    # one row apart: q's and k's heads one after the other, rows shared
+    rotary(b, INVAL, q=x, q2=x, k=x + 64, k2=x + 64, **dict.fromkeys(("sq", "sq2"), S(640, 160, 32)), **dict.fromkeys(("sk", "sk2"), S(640, 160, 32)))
+    # new outputs
+    rotary(b, INVAL, k2=b[1] + 320)
+    rotary(b, INVAL, k2=b[1] - 2)
+    rotary(b, INVAL, q2=b[1], sq2=S(960, 32, 192), k2=b[1] + 64 * 3, sk2=S(960, 32, 192))
