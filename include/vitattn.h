@@ -502,7 +502,9 @@ int vitattn_rotary(const void* q, vitattn_strides sq, void* q_out, vitattn_strid
  *              kernels compute in tiles of width (d, e) = (32, 64), (64, 64),
  *              (64, 128) or (96, 160), columns past d and e zero.
  *   strides  : as for vitattn_fwd_strided (2H heads for q, k, dq and dk), with
- *              (rows + 512) * row * 2 < 2^31. Outputs must not alias inputs.
+ *              (rows + 512) * row * 2 < 2^31.
+ *   overlaps : an output (or the workspace) that shares memory with any other
+ *              operand is rejected; interleaved views of one tensor do not.
  *   sizes    : B*H*(max(Nq, Nk) + 512) below 2^30.
  *   workspace: at least the bytes the matching function gives (the forward's is
  *              0 unless up to 256 queries meet many keys; then both passes split

@@ -34,6 +34,7 @@ struct Memory {
   int n[3];
   wide stride[3];
 };
+Memory dense_memory(const void* p, size_t bytes) { return Memory{p, (long long)bytes, {1, 1, 1}, {0, 0, 0}}; }
 Memory strided_memory(const void* p, const vitattn_strides& s, int n0, int n1, int n2, int D, int elem_bytes) {
   return Memory{p, (long long)D * elem_bytes, {n0, n1, n2},
                 {(wide)s.batch * elem_bytes, (wide)s.head * elem_bytes, (wide)s.row * elem_bytes}};
@@ -97,6 +98,13 @@ bool memories_meet(const Memory& a, const Memory& b) {
   }
   int budget = 4096;
   return steps_meet(s, n, a.row, b.row, delta, budget);
+}
+// whether one of the first n_out operands meets any other
+bool outputs_meet(const Memory* m, int n_out, int n) {
+  for (int o = 0; o < n_out; ++o)
+    for (int i = o + 1; i < n; ++i)
+      if (memories_meet(m[o], m[i])) return true;
+  return false;
 }
 
 // ------------------------------------------------------------ row kernels
@@ -411,6 +419,12 @@ int vitattn_diff_fwd(const void* q, vitattn_strides sq, const void* k, vitattn_s
       return VITATTN_E_INVAL;
     const size_t need = vitattn_diff_fwd_workspace_bytes(B, H, Nq, Nk, d, e);
     if (need > 0 && (!aligned16(workspace) || workspace_bytes < need)) return VITATTN_E_WORKSPACE;
+    const size_t rows = (size_t)2 * B * H * Nq;
+    const Memory used[] = {strided_memory(o, so, B, H, Nq, e, 2), dense_memory(maps, rows * e * 4), dense_memory(lse, rows * 4),
+                           dense_memory(need > 0 ? workspace : nullptr, need), strided_memory(q, sq, B, 2 * H, Nq, d, 2),
+                           strided_memory(k, sk, B, 2 * H, Nk, d, 2), strided_memory(v, sv, B, H, Nk, e, 2),
+                           dense_memory(lam, (size_t)H * elem_bytes(lam_type)), dense_memory(key_lens, (size_t)B * 4)};
+    if (outputs_meet(used, 4, 9)) return VITATTN_E_INVAL;
     vitattn::DiffArgs a = {};
     a.q = static_cast<const uint16_t*>(q);
     a.k = static_cast<const uint16_t*>(k);
@@ -464,8 +478,16 @@ int vitattn_diff_bwd(const void* q, vitattn_strides sq, const void* k, vitattn_s
         check_diff_map(sdo, B, H, Nq, e, false) || check_diff_map(sdq, B, 2 * H, Nq, d, true) ||
         check_diff_map(sdk, B, 2 * H, Nk, d, true) || check_diff_map(sdv, B, H, Nk, e, true))
       return VITATTN_E_INVAL;
-    if (!aligned16(workspace) || workspace_bytes < vitattn_diff_bwd_workspace_bytes(B, H, Nq, Nk, d, e))
-      return VITATTN_E_WORKSPACE;
+    const size_t need = vitattn_diff_bwd_workspace_bytes(B, H, Nq, Nk, d, e), rows = (size_t)2 * B * H * Nq;
+    if (!aligned16(workspace) || workspace_bytes < need) return VITATTN_E_WORKSPACE;
+    const size_t lam_bytes = (size_t)H * elem_bytes(lam_type);
+    const Memory used[] = {strided_memory(dq, sdq, B, 2 * H, Nq, d, 2), strided_memory(dk, sdk, B, 2 * H, Nk, d, 2),
+                           strided_memory(dv, sdv, B, H, Nk, e, 2), dense_memory(dlam, lam_bytes),
+                           dense_memory(workspace, need), strided_memory(q, sq, B, 2 * H, Nq, d, 2),
+                           strided_memory(k, sk, B, 2 * H, Nk, d, 2), strided_memory(v, sv, B, H, Nk, e, 2),
+                           strided_memory(dout, sdo, B, H, Nq, e, 2), dense_memory(maps, rows * e * 4),
+                           dense_memory(lse, rows * 4), dense_memory(lam, lam_bytes), dense_memory(key_lens, (size_t)B * 4)};
+    if (outputs_meet(used, 5, 13)) return VITATTN_E_INVAL;
     vitattn::DiffArgs a = {};
     a.q = static_cast<const uint16_t*>(q);
     a.k = static_cast<const uint16_t*>(k);

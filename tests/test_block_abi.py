@@ -280,3 +280,32 @@ def test_rotary_outputs_that_share_elements():
     rotary(b, INVAL, k2=b[1] + 320)
     rotary(b, INVAL, k2=b[1] - 2)
     rotary(b, INVAL, q2=b[1], sq2=S(960, 32, 192), k2=b[1] + 64 * 3, sk2=S(960, 32, 192))
+
+
+def test_diff_outputs_that_share_memory():
+    b = Bufs()
+    for n in range(8):
+        if n != 4:  # on every other operand
+            diff_fwd(b, INVAL, o=b[n], lens=b[7])
+    diff_fwd(b, INVAL, o=b[0] + 5040)  # q's last 80 bytes
+    diff_fwd(b, INVAL, maps=b[6] - 16)
+    for i in (0, 1, 2, 3, 4, 6, 7):
+        diff_fwd(b, INVAL, maps=b[i], lens=b[7])
+    for i in (0, 1, 2, 3, 4, 5, 7):
+        diff_fwd(b, INVAL, lse=b[i], lens=b[7])
+    # an output among q's heads: rows of 4 * 32 + 2 * 64 columns, q's first, o one head early
+    fused = dict(q=b[0], sq=S(2560, 32, 256), so=S(2560, 64, 256))
+    diff_fwd(b, INVAL, o=b[0] + 2 * 96, **fused)
+    diff_fwd(b, INVAL, o=b[0] + 2 * 136, **fused)
+    one = dict(B=1, H=1, Nq=1, Nk=1024, sq=S(64, 32, 32), sk=S(0, 32768, 32), sv=S(0, 0, 64), so=S(64, 64, 64), wsb=1 << 20)
+    for i in (0, 1, 2, 3, 4, 5, 6):
+        diff_fwd(b, INVAL, ws=b[i], **one)
+
+
+@pytest.mark.parametrize("out", ["dq", "dk", "dv", "dlam", "ws"])
+def test_diff_gradients_that_share_memory(out):
+    b = Bufs()
+    base = dict(q=0, k=1, v=2, lam=3, maps=5, lse=6, dout=7, dq=8, dk=9, dv=10, dlam=11, ws=12, lens=13)
+    for n, i in base.items():
+        if n != out:
+            diff_bwd(b, INVAL, **{"lens": b[13], out: b[i]})

@@ -251,3 +251,36 @@ def test_offsets_past_32_bits():
         assert t.equal(a[:, -n:], b)
 
 
+
+
+def test_outputs_among_other_operands():
+    """Outputs interleaved with other operands in one tensor share no memory with them; those that do are refused."""
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    B, H, N, d, e = 2, 2, 70, 32, 64
+    q, k, v, lam, _ = inputs(B, H, N, N, d, e, seed=90, layout=[0, 2, 1, 3])
+    want = va.diff_fwd(q, k, v, lam)[0]
+    buf = t.full((B, N, 2 * H * d + H * e + 8), 7.0, dtype=t.bfloat16, device="cuda")
+    qi = buf[..., :2 * H * d].view(B, N, 2 * H, d).transpose(1, 2)
+    oi = buf[..., 2 * H * d:-8].view(B, N, H, e).transpose(1, 2)
+    qi.copy_(q)
+    va.diff_fwd(qi, k, v, lam, out=oi)
+    assert t.equal(oi, want) and t.equal(qi, q) and (buf[..., -8:] == 7).all()
+    shifted = buf[..., 2 * H * d - 8:-16].view(B, N, H, e).transpose(1, 2)  # from q's last columns on
+    for inputs_, out in (((qi, k, v), shifted), ((q, k, v), v)):
+        with pytest.raises(va.VitattnError):
+            va.diff_fwd(*inputs_, lam, out=out)
+    # rotary: outputs interleaved in a new tensor, and operands in place that share a head
+    pos, both = positions(t, N), t.empty((B, N, 5, d), dtype=t.bfloat16, device="cuda")
+    q1, k1 = va.rotary_fwd(q[:, :3], k[:, :2], pos, SECTIONS)
+    va.rotary_fwd(q[:, :3], k[:, :2], pos, SECTIONS, out=(both[:, :, :3].transpose(1, 2), both[:, :, 3:].transpose(1, 2)))
+    assert t.equal(both[:, :, :3].transpose(1, 2), q1) and t.equal(both[:, :, 3:].transpose(1, 2), k1)
+    x = both.transpose(1, 2)
+    before = both.clone()
+    for a, c in ((x, x[:, 1:]), (x[:, :3], x[:, 2:]), (x, x)):
+        with pytest.raises(va.VitattnError):
+            va.rotary_fwd(a, c, pos, SECTIONS, out=(a, c))
+    with pytest.raises(va.VitattnError):
+        va.rotary_fwd(q[:, :3], k[:, :3], pos, SECTIONS, out=(x[:, :3], x[:, 2:]))
+    assert t.equal(both, before)
