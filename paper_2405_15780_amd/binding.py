@@ -602,6 +602,21 @@ def _call(t, fn, *args):
         raise VitattnError(status)
 
 
+def _expect_out(t, name, dtype, shape, device, dense=False):
+    """_expect for a tensor that a call writes: as in torch, one that requires a
+    gradient is refused where gradients are recorded."""
+    _expect(t, name, dtype, shape, device, dense)
+    if t.requires_grad and _torch().is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient: it is written outside autograd (detach it, or call under no_grad)")
+    return t
+
+
+def _written(*ts):
+    """Tells autograd that these were written, as torch's own in-place operations do: the backward of an operation that
+    saved one raises instead of reading what it has become."""
+    _torch().autograd.graph.increment_version(ts)
+
+
 def plain_memory(t):
     """t, or a copy where its memory does not hold its values as they are: a
     lazily negated view, zeros without memory, a last dim that is not contiguous."""
@@ -680,7 +695,7 @@ def layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, out=None, stats=True):
     if out is None:
         y = torch.empty_like(x) if x4 is x else torch.empty(x.shape, dtype=x.dtype, device=x.device)
     else:
-        y = _expect(out, "out", x.dtype, x.shape, x.device, dense=x4 is not x)
+        y = _expect_out(out, "out", x.dtype, x.shape, x.device, dense=x4 is not x)
     y4 = y if x4 is x else y.view(x4.shape)
     order, n = _norm_rows(x4, y4)
     mean = rstd = None
@@ -690,6 +705,8 @@ def layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, out=None, stats=True):
     _call(x, library().vitattn_layer_norm_fwd, x4.data_ptr(), _norm_strides(x4, order, D), _ptr(weight), _ptr(bias),
           y.data_ptr(), _norm_strides(y4, order, D), _ptr(mean), _ptr(rstd), *n, D, eps, code,
           VITATTN_FP32 if wt == torch.float32 else code)
+    if out is not None:
+        _written(out)
     if order is not None and stats:
         mean, rstd = _norm_stat_out(mean, order, x4, x.shape), _norm_stat_out(rstd, order, x4, x.shape)
     return y, mean, rstd
@@ -798,7 +815,7 @@ def rotary_fwd(q, k, positions, sections, base=10000.0, interleaved=False, joint
         q_out, k_out = out if k is not None else ((out[0] if isinstance(out, (tuple, list)) else out), None)
         for t, like, n in ((q_out, q, "out q"), (k_out, k, "out k")):
             if like is not None:
-                _expect(t, n, dtype, like.shape, device)
+                _expect_out(t, n, dtype, like.shape, device)
     if k is not None:
         sk, sk_out = _strides_any(k), _strides_any(k_out)
     sp = positions.stride()
@@ -807,6 +824,8 @@ def rotary_fwd(q, k, positions, sections, base=10000.0, interleaved=False, joint
     _call(q, library().vitattn_rotary, q.data_ptr(), _strides_any(q), q_out.data_ptr(), _strides_any(q_out), Hq,
           _ptr(k), sk, _ptr(k_out), sk_out, Hk, positions.data_ptr(), sp[0] if len(sp) == 3 else 0, sp[-2], sp[-1],
           pos_code, _c_ints(sections), A, float(base), B, N, d, code, flags)
+    if out is not None:
+        _written(q_out) if k is None else _written(q_out, k_out)
     return q_out if k is None else (q_out, k_out)
 
 
@@ -866,7 +885,8 @@ def diff_fwd(q, k, v, lam, scale=None, key_lens=None, out=None, save=True, works
     torch = _torch()
     sizes, lam_code = _diff_args(q, k, v, lam, key_lens)
     B, H, Nq, Nk, d, e = sizes
-    o = _like_layout(q, (B, H, Nq, e)) if out is None else _expect(out, "out", torch.bfloat16, (B, H, Nq, e), q.device)
+    o = (_like_layout(q, (B, H, Nq, e)) if out is None
+         else _expect_out(out, "out", torch.bfloat16, (B, H, Nq, e), q.device))
     o2 = lse = None
     if save:
         o2 = torch.empty((B, 2 * H, Nq, e), dtype=torch.float32, device=q.device)
@@ -877,6 +897,8 @@ def diff_fwd(q, k, v, lam, scale=None, key_lens=None, out=None, save=True, works
     _call(q, lib.vitattn_diff_fwd, q.data_ptr(), _diff_strides(q), k.data_ptr(), _diff_strides(k), v.data_ptr(),
           _diff_strides(v), lam.data_ptr(), lam_code, _ptr(key_lens), o.data_ptr(), _diff_strides(o), _ptr(o2), _ptr(lse),
           *sizes, _default_scale(d, scale), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+    if out is not None:
+        _written(out)
     return o, o2, lse
 
 

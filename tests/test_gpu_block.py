@@ -284,3 +284,34 @@ def test_outputs_among_other_operands():
     with pytest.raises(va.VitattnError):
         va.rotary_fwd(q[:, :3], k[:, :3], pos, SECTIONS, out=(x[:, :3], x[:, 2:]))
     assert t.equal(both, before)
+
+
+def test_outputs_written_in_place_are_known_to_autograd():
+    """out= is refused where it requires a gradient, and a tensor that was saved before it was written is not read as if
+    it had not been."""
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    q, k, v, lam, _ = inputs(1, 2, 20, 20, 32, 64, seed=91)
+    pos = positions(t, 20)
+    writes = {"norm": (q, lambda x: va.layer_norm_fwd(x, out=x)), "rotary": (q, lambda x: va.rotary_fwd(x, None, pos, SECTIONS, out=x)),
+              "rotary k": (k, lambda x: va.rotary_fwd(q, x, pos, SECTIONS, out=(q.clone(), x))),
+              "diff": (v, lambda x: va.diff_fwd(q, k, v, lam, out=x))}
+    for n, (like, write) in writes.items():
+        leaf = like.clone().requires_grad_()
+        x = leaf * 1.0
+        y = x * x  # saves x
+        before = x.detach().clone()
+        with pytest.raises(ValueError):
+            write(x)
+        assert t.equal(x.detach(), before), n
+        with t.no_grad():
+            write(x)
+        assert not t.equal(x.detach(), before), n
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+        # a leaf that is not in a graph, and one whose value autograd has no use for
+        x = leaf * 1.0
+        write(x.detach())
+        x.sum().backward()
+        assert t.equal(leaf.grad, t.ones_like(leaf)), n
