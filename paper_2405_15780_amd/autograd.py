@@ -158,21 +158,21 @@ class _DiffAttention:
                 @staticmethod
                 def forward(ctx, q, k, v, lam, scale, key_lens):
                     o, o2, lse = _b.diff_fwd(q, k, v, lam, scale, key_lens)
-                    ctx.save_for_backward(q, k, v, lam, o, o2, lse, key_lens)
+                    ctx.save_for_backward(q, k, v, lam, o2, lse, key_lens)
                     ctx.scale = scale
                     return o
 
                 @staticmethod
                 @torch.autograd.function.once_differentiable
                 def backward(ctx, grad_o):
-                    q, k, v, lam, o, o2, lse, key_lens = ctx.saved_tensors
+                    q, k, v, lam, o2, lse, key_lens = ctx.saved_tensors
                     g = _b.plain_memory(grad_o)
                     s = _b._diff_strides(g)
                     # shared or misaligned rows are laid out anew
                     if s.row < g.shape[3] or s.row % 8 or s.head % 8 or s.batch % 8 or g.data_ptr() % 16 \
                             or (g.shape[2] + 512) * s.row * 2 > 0x7fffffff:
                         g = torch.empty(g.shape, dtype=g.dtype, device=g.device).copy_(g)
-                    dq, dk, dv, dlam = _b.diff_bwd(q, k, v, lam, o, o2, lse, g, ctx.scale, key_lens,
+                    dq, dk, dv, dlam = _b.diff_bwd(q, k, v, lam, None, o2, lse, g, ctx.scale, key_lens,
                                                    want_dlam=ctx.needs_input_grad[3])
                     return dq, dk, dv, dlam, None, None
 

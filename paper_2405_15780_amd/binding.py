@@ -905,11 +905,13 @@ def diff_fwd(q, k, v, lam, scale=None, key_lens=None, out=None, save=True, works
 def diff_bwd(q, k, v, lam, o, o2, lse, dout, scale=None, key_lens=None, want_dlam=True, workspace=None):
     """dq, dk, dv (bf16, like q, k and v) and dlam (lam's type, or None) of
     diff_fwd for the upstream gradient dout (bf16 [B,H,Nq,e]). The kernels read
-    the unrounded outputs in o2; o is checked to belong to the same call's sizes."""
+    the unrounded outputs in o2; o (or None) is only checked to belong to the same
+    call's sizes."""
     torch = _torch()
     sizes, lam_code = _diff_args(q, k, v, lam, key_lens)
     B, H, Nq, Nk, d, e = sizes
-    _expect(o, "o", torch.bfloat16, (B, H, Nq, e), q.device)
+    if o is not None:
+        _expect(o, "o", torch.bfloat16, (B, H, Nq, e), q.device)
     _expect(o2, "o2", torch.float32, (B, 2 * H, Nq, e), q.device, dense=True)
     _expect(lse, "lse", torch.float32, (B, 2 * H, Nq), q.device, dense=True)
     _expect(dout, "dout", torch.bfloat16, (B, H, Nq, e), q.device)

@@ -83,3 +83,23 @@ def test_functional_derivatives_are_refused(stand_ins, fn, shapes):
     first = next(iter(shapes))
     with pytest.raises(Exception):
         torch.func.jvp(lambda x: fn({**ts, first: x}), (ts[first],), (torch.ones(shapes[first]),))
+
+
+def test_the_output_of_diff_attention_is_free(stand_ins, monkeypatch):
+    """The backward reads the unrounded maps' outputs, so o is neither kept alive nor held against in-place operations."""
+    seen = []
+
+    def diff_bwd(q, k, v, lam, o, o2, lse, dout, scale=None, key_lens=None, want_dlam=True, workspace=None, **wants):
+        seen.append((o, dout))
+        return torch.ones_like(q), torch.ones_like(k), torch.ones_like(v), torch.ones_like(lam)
+
+    monkeypatch.setattr(binding, "diff_bwd", diff_bwd)
+    ts = {n: torch.randn(s, requires_grad=True) for n, s in QKV.items()}
+    saved = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: saved.append(t.shape) or t, lambda t: t):
+        o = diff(ts)
+    assert o.shape not in saved and ts["q"].shape in saved
+    o.mul_(3.0)
+    o.sum().backward()
+    assert seen[0][0] is None and (seen[0][1] == 3).all()
+    assert all((t.grad == 1).all() for t in ts.values())

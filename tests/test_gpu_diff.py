@@ -384,3 +384,20 @@ def test_refusals():
         va.diff_attention(q, k, v, 0.5)
     with pytest.raises(va.VitattnError):  # rows that are not 16-byte aligned
         va.diff_fwd(make((2, 4, 10, 36), "bfloat16", 1)[..., :32], k, v, lam)
+
+
+def test_backward_without_the_rounded_output():
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    q, k, v, lam, do = inputs(1, 2, 33, 40, 32, 64, seed=28)
+    ref = run(q, k, v, lam, do)
+    for got, n in zip(va.diff_bwd(q, k, v, lam, None, ref["o2"], ref["lse"], do), ("dq", "dk", "dv", "dlam")):
+        assert t.equal(got, ref[n]), n
+    leaves = [x.detach().requires_grad_() for x in (q, k, v, lam)]
+    o = va.diff_attention(*leaves)
+    o.mul_(2.0)  # the backward has no use for it
+    o.backward(do)
+    want = run(q, k, v, lam, 2 * do)
+    for x, n in zip(leaves, ("dq", "dk", "dv", "dlam")):
+        assert t.equal(x.grad, want[n]), n
