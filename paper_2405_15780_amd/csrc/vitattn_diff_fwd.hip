@@ -547,7 +547,7 @@ hipError_t go_tile(const DiffArgs& a) {
 int diff_split_keys(int Nq, int Nk) {
   if (Nq > 256 || Nk < (Nq > 64 ? 8192 : 1024)) return 0;
   const int least = Nq > 64 ? 4096 : 512, most = Nq > 64 ? 32 : 128;
-  const int keys = (Nk / most + 63) / 64 * 64;
+  const int keys = ((Nk + most - 1) / most + 63) / 64 * 64;
   return keys > least ? keys : least;
 }
 

@@ -309,3 +309,17 @@ def test_diff_gradients_that_share_memory(out):
     for n, i in base.items():
         if n != out:
             diff_bwd(b, INVAL, **{"lens": b[13], out: b[i]})
+
+
+@pytest.mark.parametrize("Nq,least,most", [(1, 1024, 128), (64, 1024, 128), (65, 8192, 32), (256, 8192, 32)])
+def test_number_of_splits(Nq, least, most):
+    """The forward's workspace holds a row of e outputs and an LSE per split, map and query."""
+    def splits(Nk):
+        n = lib().vitattn_diff_fwd_workspace_bytes(1, 1, Nq, Nk, 64, 128)
+        assert n % (4 * 2 * Nq * 129) == 0
+        return n // (4 * 2 * Nq * 129)
+
+    assert splits(least - 1) == 0 and splits(least) > 1
+    for Nk in {n + i for n in (least, 65536, 65600, 66048, 131072, 131136, 1 << 20) for i in (0, 1, 63, 64, 127, 128, 129)}:
+        assert 1 < splits(Nk) <= most, Nk
+    assert splits(131072) == most and splits(1 << 20) == most

@@ -401,3 +401,9 @@ def test_backward_without_the_rounded_output():
     want = run(q, k, v, lam, 2 * do)
     for x, n in zip(leaves, ("dq", "dk", "dv", "dlam")):
         assert t.equal(x.grad, want[n]), n
+
+
+@pytest.mark.parametrize("Nq,Nk", [(1, 65537), (2, 131073), (128, 131073)])
+def test_one_key_past_whole_splits(Nq, Nk):
+    print(f"case diff Nq={Nq} Nk={Nk} past whole splits", flush=True)
+    check(*inputs(1, 1, Nq, Nk, 32, 64, seed=Nq))
