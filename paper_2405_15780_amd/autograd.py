@@ -122,15 +122,18 @@ class _Rotary:
                 def forward(ctx, q, k, positions, sections, base, interleaved, joint, inverse):
                     ctx.save_for_backward(positions)
                     ctx.args = (sections, base, interleaved, joint)
-                    ctx.inverse, ctx.pair = inverse, k is not None
+                    ctx.inverse = inverse
                     return _b.rotary_fwd(q, k, positions, sections, base, interleaved, joint, inverse)
 
                 @staticmethod
                 def backward(ctx, dq, dk=None):
-                    # the turn by the opposite angles, itself differentiable
-                    dq, dk = (None if g is None else _b.plain_memory(g) for g in (dq, dk))
-                    r = Rotary.apply(dq, dk, ctx.saved_tensors[0], *ctx.args, not ctx.inverse)
-                    dq, dk = r if ctx.pair else (r, None)
+                    # the turn by the opposite angles, itself differentiable, of
+                    # those that are asked for
+                    grads = [_b.plain_memory(g) if need else None for g, need in zip((dq, dk), ctx.needs_input_grad)]
+                    first, *second = [g for g in grads if g is not None]
+                    r = Rotary.apply(first, second[0] if second else None, ctx.saved_tensors[0], *ctx.args, not ctx.inverse)
+                    turned = iter(r if second else (r,))
+                    dq, dk = (None if g is None else next(turned) for g in grads)
                     return dq, dk, None, None, None, None, None, None
 
             cls._fn = Rotary

@@ -25,7 +25,7 @@ def stand_ins(monkeypatch):
         return y, mean, rstd
 
     def rotary_fwd(q, k, positions, sections, base=10000.0, interleaved=False, joint=False, inverse=False, out=None):
-        calls.append("rotary_fwd")
+        calls.append(("rotary_fwd", tuple(q.shape), k is not None, inverse))
         return 2 * q if k is None else (2 * q, 2 * k)
 
     def diff_fwd(q, k, v, lam, scale=None, key_lens=None, out=None, save=True, workspace=None):
@@ -103,3 +103,13 @@ def test_the_output_of_diff_attention_is_free(stand_ins, monkeypatch):
     o.sum().backward()
     assert seen[0][0] is None and (seen[0][1] == 3).all()
     assert all((t.grad == 1).all() for t in ts.values())
+
+
+@pytest.mark.parametrize("need", ["q", "k", "qk"])
+def test_rotary_turns_back_only_what_is_asked_for(stand_ins, need):
+    q, k = torch.randn((1, 4, 5, 8), requires_grad="q" in need), torch.randn((1, 2, 5, 8), requires_grad="k" in need)
+    a, b = va.rotary(q, k, POS, (4,))
+    (a.sum() + b.sum()).backward()
+    assert stand_ins[1:] == [("rotary_fwd", tuple((k if need == "k" else q).shape), need == "qk", True)]
+    for x, n in ((q, "q"), (k, "k")):
+        assert x.grad is None if n not in need else (x.grad == 2).all()

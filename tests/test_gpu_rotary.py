@@ -192,3 +192,18 @@ def test_sections_are_whole_numbers_in_range():
     for bad in ((2 ** 32 + 5, 3), (2 ** 31, 0)):
         with pytest.raises(va.VitattnError):
             va.rotary_fwd(q, None, pos, bad)
+
+
+@pytest.mark.parametrize("need", ["q", "k", "qk"])
+def test_gradient_of_one_operand(need):
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    pos, sections = positions(17, 2, "int64", 36), (8, 7)
+    q, k = make((2, 3, 17, 40), "float32", 37), make((2, 2, 17, 40), "float32", 38)
+    leaves = [x.detach().requires_grad_(n in need) for x, n in ((q, "q"), (k, "k"))]
+    gs = [make(tuple(x.shape), "float32", 39) for x in leaves]
+    out = va.rotary(*leaves, pos, sections)
+    t.autograd.backward(out, gs)
+    for x, g, n in zip(leaves, gs, "qk"):
+        assert x.grad is None if n not in need else t.equal(x.grad, va.rotary_fwd(g, None, pos, sections, inverse=True))
