@@ -625,6 +625,16 @@ def plain_memory(t):
     return t
 
 
+def _new_like(t):
+    """A new tensor in t's order of dims, the last one contiguous: torch's order of
+    a sliding window's (whose rows start one element apart) may put another there."""
+    torch = _torch()
+    y = torch.empty_like(t)
+    if y.stride(-1) != 1 and y.shape[-1] != 1:
+        y = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    return y
+
+
 def _norm_view(t, name):
     """t as the rows of a layer norm; more than three leading dims become one (by
     a copy where t's layout needs it)."""
@@ -693,7 +703,7 @@ def layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, out=None, stats=True):
     if x.numel() == 0:
         raise ValueError("layer_norm needs at least one row and one column")
     if out is None:
-        y = torch.empty_like(x) if x4 is x else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        y = _new_like(x) if x4 is x else torch.empty(x.shape, dtype=x.dtype, device=x.device)
     else:
         y = _expect_out(out, "out", x.dtype, x.shape, x.device, dense=x4 is not x)
     y4 = y if x4 is x else y.view(x4.shape)
@@ -738,7 +748,7 @@ def layer_norm_bwd(x, weight, mean, rstd, dy, want_dweight=True, want_dbias=True
         wt = bias_dtype
     if x.numel() == 0:
         raise ValueError("layer_norm needs at least one row and one column")
-    dx = torch.empty_like(x) if x4 is x else torch.empty(shape, dtype=x.dtype, device=x.device)
+    dx = _new_like(x) if x4 is x else torch.empty(shape, dtype=x.dtype, device=x.device)
     dy4, dx4 = _norm_view(dy, "dy"), dx if x4 is x else dx.view(x4.shape)
     order, n = _norm_rows(x4, dy4, dx4)
     if order is not None:
@@ -808,9 +818,9 @@ def rotary_fwd(q, k, positions, sections, base=10000.0, interleaved=False, joint
         raise TypeError(f"positions must be an int32, int64 or float32 tensor [{N}, {A}] or [{B}, {N}, {A}] on {device}")
     k_out, sk, sk_out = None, _NO_STRIDES, _NO_STRIDES
     if out is None:
-        q_out = torch.empty_like(q)
+        q_out = _new_like(q)
         if k is not None:
-            k_out = torch.empty_like(k)
+            k_out = _new_like(k)
     else:
         q_out, k_out = out if k is not None else ((out[0] if isinstance(out, (tuple, list)) else out), None)
         for t, like, n in ((q_out, q, "out q"), (k_out, k, "out k")):

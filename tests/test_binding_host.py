@@ -60,3 +60,14 @@ def test_missing_library_raises_instead_of_falling_back(monkeypatch):
         binding.workspace_bytes(1, 1, 8, 64)
     with pytest.raises(ImportError, match="is missing"):
         binding.version()
+
+
+def test_new_tensors_have_contiguous_rows():
+    from paper_2405_15780_amd import binding
+
+    x = torch.arange(200.0)
+    for t in (x[:40].unfold(0, 30, 1), x[:80].view(2, 40).unfold(1, 30, 1), x.as_strided((2, 3, 4, 8), (1, 8, 0, 1)), x[:6].view(6, 1).expand(6, 40)):
+        y = binding._new_like(t)
+        assert y.shape == t.shape and y.stride(-1) == 1
+    heads = x[:192].view(2, 4, 3, 8).transpose(1, 2)  # [2, 3, 4, 8], rows before heads in memory
+    assert binding._new_like(heads).stride() == heads.stride()

@@ -312,3 +312,18 @@ def test_refusals():
         va.layer_norm_bwd(x, None, mean[:3], rstd, x)
     with pytest.raises(va.VitattnError):
         va.layer_norm_bwd(x, None, mean, rstd, x, workspace=t.empty(4, device="cuda"))
+
+
+@pytest.mark.parametrize("windows,D,hop", [(11, 30, 1), (31, 10, 1), (9, 72, 1), (6, 30, 2), (3, 700, 1)])
+def test_sliding_windows(windows, D, hop):
+    """Rows that start a few elements apart: the outputs have rows of their own."""
+    for dtype in TYPES:
+        print(f"case layer norm windows {windows} x {D} by {hop} {dtype}", flush=True)
+        long = make((2, D + hop * (windows - 1)), dtype, 93)
+        x, dy = long.unfold(1, D, hop), make((2, D + hop * (windows - 1)), dtype, 94).unfold(1, D, hop)
+        assert x.shape == (2, windows, D) and x.stride() == (long.shape[1], hop, 1)
+        w, b = make((D,), dtype, 95, mean=1.0), make((D,), dtype, 96)
+        got = run(x, w, b, dy)
+        check(x, w, b, dy, *got, dtype, dtype)
+        want = run(x.contiguous(), w, b, dy.contiguous())
+        assert all(torch().equal(a, c) for a, c in zip(got, want))

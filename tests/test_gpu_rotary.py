@@ -207,3 +207,16 @@ def test_gradient_of_one_operand(need):
     t.autograd.backward(out, gs)
     for x, g, n in zip(leaves, gs, "qk"):
         assert x.grad is None if n not in need else t.equal(x.grad, va.rotary_fwd(g, None, pos, sections, inverse=True))
+
+
+def test_sliding_windows():
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    long = make((2, 3, 40), "bfloat16", 40)
+    q, k = long.unfold(2, 32, 1), long[:, :2].unfold(2, 32, 1)  # [2, 3, 9, 32], rows one element apart
+    pos = positions(9, 2, "int64", 41)
+    q1, k1 = va.rotary_fwd(q, k, pos, (8, 8))
+    check(q, q1, pos, (8, 8), "bfloat16")
+    want = va.rotary_fwd(q.contiguous(), k.contiguous(), pos, (8, 8))
+    assert t.equal(q1, want[0]) and t.equal(k1, want[1])
