@@ -586,7 +586,15 @@ def _type_code(t, name, allowed=_ALL_TYPES):
     if code is None or code not in allowed:
         names = ", ".join(str(d) for d, c in _type_codes().items() if c in allowed)
         raise TypeError(f"{name} must be a CUDA tensor of one of {names}")
+    _as_it_is(t, name)
     return code
+
+
+def _as_it_is(t, name):
+    """Raise TypeError where t's memory holds its values negated (the imaginary part
+    of a conjugate, which torch negates when it reads it)."""
+    if t.is_neg():
+        raise TypeError(f"{name} is a lazily negated view: pass {name}.resolve_neg()")
 
 
 def _call(t, fn, *args):
@@ -605,7 +613,7 @@ def _call(t, fn, *args):
 def _expect_out(t, name, dtype, shape, device, dense=False):
     """_expect for a tensor that a call writes: as in torch, one that requires a
     gradient is refused where gradients are recorded."""
-    _expect(t, name, dtype, shape, device, dense)
+    _as_it_is(_expect(t, name, dtype, shape, device, dense), name)
     if t.requires_grad and _torch().is_grad_enabled():
         raise ValueError(f"{name} requires a gradient: it is written outside autograd (detach it, or call under no_grad)")
     return t
@@ -682,6 +690,7 @@ def _norm_weights(x, D, weight, bias):
             raise TypeError(f"{n} must be a contiguous {dtype} or torch.float32 CUDA tensor of shape ({D},) on {device}")
         if wt is not None and t.dtype != wt:
             raise TypeError("weight and bias must be of one type")
+        _as_it_is(t, n)
         wt = t.dtype
     return dtype if wt is None else wt
 
@@ -737,7 +746,7 @@ def layer_norm_bwd(x, weight, mean, rstd, dy, want_dweight=True, want_dbias=True
     x4 = _norm_view(x, "x")
     shape, device = x.shape, x.device
     D, rows = shape[-1], shape[:-1]
-    _expect(dy, "dy", x.dtype, shape, device)
+    _as_it_is(_expect(dy, "dy", x.dtype, shape, device), "dy")
     for t, n in ((mean, "mean"), (rstd, "rstd")):
         if not (isinstance(t, torch.Tensor) and t.device == device and t.dtype == torch.float32 and t.shape == rows):
             raise TypeError(f"{n} must be a torch.float32 CUDA tensor of shape {tuple(rows)} on {device}")
@@ -802,6 +811,7 @@ def rotary_fwd(q, k, positions, sections, base=10000.0, interleaved=False, joint
         if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == device and t.dim() == 4
                 and (t.stride(3) == 1 or t.shape[3] == 1)):
             raise TypeError(f"{n} must be a 4-D CUDA tensor [B, H, N, d] of q's type and device with unit stride along d")
+        _as_it_is(t, n)
     B, Hq, N, d = q.shape
     Hk = 0
     if k is not None:
@@ -816,6 +826,7 @@ def rotary_fwd(q, k, positions, sections, base=10000.0, interleaved=False, joint
     pos_code = _pos_codes().get(positions.dtype) if isinstance(positions, torch.Tensor) else None
     if pos_code is None or positions.device != device or positions.shape not in ((N, A), (B, N, A)):
         raise TypeError(f"positions must be an int32, int64 or float32 tensor [{N}, {A}] or [{B}, {N}, {A}] on {device}")
+    _as_it_is(positions, "positions")
     k_out, sk, sk_out = None, _NO_STRIDES, _NO_STRIDES
     if out is None:
         q_out = _new_like(q)
@@ -856,6 +867,8 @@ def _diff_args(q, k, v, lam, key_lens):
     device = q.device
     _as_input(k, "k", device)
     _as_input(v, "v", device)
+    for t, n in ((q, "q"), (k, "k"), (v, "v")):
+        _as_it_is(t, n)
     B, H2, Nq, d = q.shape
     Bv, H, Nk, e = v.shape
     if H2 != 2 * H or Bv != B or tuple(k.shape) != (B, H2, Nk, d):
@@ -924,7 +937,7 @@ def diff_bwd(q, k, v, lam, o, o2, lse, dout, scale=None, key_lens=None, want_dla
         _expect(o, "o", torch.bfloat16, (B, H, Nq, e), q.device)
     _expect(o2, "o2", torch.float32, (B, 2 * H, Nq, e), q.device, dense=True)
     _expect(lse, "lse", torch.float32, (B, 2 * H, Nq), q.device, dense=True)
-    _expect(dout, "dout", torch.bfloat16, (B, H, Nq, e), q.device)
+    _as_it_is(_expect(dout, "dout", torch.bfloat16, (B, H, Nq, e), q.device), "dout")
     dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
     dlam = torch.empty_like(lam) if want_dlam else None
     lib = library()

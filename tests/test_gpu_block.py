@@ -315,3 +315,30 @@ def test_outputs_written_in_place_are_known_to_autograd():
         write(x.detach())
         x.sum().backward()
         assert t.equal(leaf.grad, t.ones_like(leaf)), n
+
+
+def test_lazily_negated_operands_are_refused():
+    """Their memory holds the opposite values. (Gradients are resolved by the autograd functions.)"""
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    q, k, v, lam, do = inputs(1, 2, 20, 20, 32, 64, seed=92)
+    x, w = make((20, 32), "float32", 93), make((32,), "float32", 94)
+    pos = t.complex(t.zeros(20, 3, device="cuda"), positions(t, 20).float()).conj().imag
+    assert pos.is_neg()
+    n = t._neg_view
+    o, o2, lse = va.diff_fwd(q, k, v, lam)
+    y, mean, rstd = va.layer_norm_fwd(x, w)
+    calls = [lambda: va.layer_norm_fwd(n(x)), lambda: va.layer_norm(x, n(w)), lambda: va.layer_norm_fwd(x, w, n(w)),
+             lambda: va.layer_norm_fwd(x, out=n(x)), lambda: va.layer_norm_bwd(n(x), w, mean, rstd, x),
+             lambda: va.layer_norm_bwd(x, w, mean, rstd, n(x)), lambda: va.rotary(n(q), k, pos.resolve_neg(), SECTIONS),
+             lambda: va.rotary(q, n(k), pos.resolve_neg(), SECTIONS), lambda: va.rotary(q, k, pos, SECTIONS),
+             lambda: va.diff_attention(n(q), k, v, lam), lambda: va.diff_attention(q, n(k), v, lam),
+             lambda: va.diff_attention(q, k, n(v), lam), lambda: va.diff_fwd(q, k, v, n(lam)),
+             lambda: va.diff_bwd(q, k, v, lam, o, o2, lse, n(do))]
+    for i, call in enumerate(calls):
+        with pytest.raises(TypeError, match="resolve_neg"):
+            call()
+            print("not refused", i)
+    turned = va.rotary(q, k, pos.resolve_neg(), SECTIONS)
+    assert all(t.equal(a, b) for a, b in zip(turned, va.rotary(q, k, -positions(t, 20), SECTIONS)))
