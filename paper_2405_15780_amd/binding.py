@@ -586,15 +586,21 @@ def _type_code(t, name, allowed=_ALL_TYPES):
     if code is None or code not in allowed:
         names = ", ".join(str(d) for d, c in _type_codes().items() if c in allowed)
         raise TypeError(f"{name} must be a CUDA tensor of one of {names}")
-    _as_it_is(t, name)
+    if t.is_neg():
+        _negated(name)
     return code
 
 
+def _negated(name):
+    """Of a tensor whose memory holds its values negated (the imaginary part of a
+    conjugate, which torch negates when it reads it)."""
+    raise TypeError(f"{name} is a lazily negated view: pass {name}.resolve_neg()")
+
+
 def _as_it_is(t, name):
-    """Raise TypeError where t's memory holds its values negated (the imaginary part
-    of a conjugate, which torch negates when it reads it)."""
     if t.is_neg():
-        raise TypeError(f"{name} is a lazily negated view: pass {name}.resolve_neg()")
+        _negated(name)
+    return t
 
 
 def _call(t, fn, *args):
@@ -636,11 +642,10 @@ def plain_memory(t):
 def _new_like(t):
     """A new tensor in t's order of dims, the last one contiguous: torch's order of
     a sliding window's (whose rows start one element apart) may put another there."""
-    torch = _torch()
-    y = torch.empty_like(t)
-    if y.stride(-1) != 1 and y.shape[-1] != 1:
-        y = torch.empty(t.shape, dtype=t.dtype, device=t.device)
-    return y
+    y = _torch().empty_like(t)
+    if y.is_contiguous() or y.stride(-1) == 1 or y.shape[-1] == 1:
+        return y
+    return _torch().empty(t.shape, dtype=t.dtype, device=t.device)
 
 
 def _norm_view(t, name):
@@ -690,7 +695,8 @@ def _norm_weights(x, D, weight, bias):
             raise TypeError(f"{n} must be a contiguous {dtype} or torch.float32 CUDA tensor of shape ({D},) on {device}")
         if wt is not None and t.dtype != wt:
             raise TypeError("weight and bias must be of one type")
-        _as_it_is(t, n)
+        if t.is_neg():
+            _negated(n)
         wt = t.dtype
     return dtype if wt is None else wt
 
@@ -811,22 +817,25 @@ def rotary_fwd(q, k, positions, sections, base=10000.0, interleaved=False, joint
         if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == device and t.dim() == 4
                 and (t.stride(3) == 1 or t.shape[3] == 1)):
             raise TypeError(f"{n} must be a 4-D CUDA tensor [B, H, N, d] of q's type and device with unit stride along d")
-        _as_it_is(t, n)
     B, Hq, N, d = q.shape
     Hk = 0
     if k is not None:
         Bk, Hk, Nk, dk = k.shape
         if (Bk, Nk, dk) != (B, N, d):
             raise ValueError("k must be [B, Hk, N, d] with the B, N and d of q")
-    pairs = tuple(sections)
-    sections = tuple(map(int, pairs))
-    if sections != pairs:
-        raise ValueError("sections must be whole numbers")
+    sections = tuple(sections)
+    try:
+        sections = tuple(map(operator.index, sections))
+    except TypeError:
+        if sections != tuple(map(int, sections)):
+            raise ValueError("sections must be whole numbers") from None
+        sections = tuple(map(int, sections))
     A = len(sections)
     pos_code = _pos_codes().get(positions.dtype) if isinstance(positions, torch.Tensor) else None
     if pos_code is None or positions.device != device or positions.shape not in ((N, A), (B, N, A)):
         raise TypeError(f"positions must be an int32, int64 or float32 tensor [{N}, {A}] or [{B}, {N}, {A}] on {device}")
-    _as_it_is(positions, "positions")
+    if positions.is_neg() or k is not None and k.is_neg():
+        _negated("positions" if positions.is_neg() else "k")
     k_out, sk, sk_out = None, _NO_STRIDES, _NO_STRIDES
     if out is None:
         q_out = _new_like(q)
@@ -867,8 +876,8 @@ def _diff_args(q, k, v, lam, key_lens):
     device = q.device
     _as_input(k, "k", device)
     _as_input(v, "v", device)
-    for t, n in ((q, "q"), (k, "k"), (v, "v")):
-        _as_it_is(t, n)
+    if q.is_neg() or k.is_neg() or v.is_neg():
+        _negated("q" if q.is_neg() else "k" if k.is_neg() else "v")
     B, H2, Nq, d = q.shape
     Bv, H, Nk, e = v.shape
     if H2 != 2 * H or Bv != B or tuple(k.shape) != (B, H2, Nk, d):
