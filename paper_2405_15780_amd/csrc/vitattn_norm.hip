@@ -217,7 +217,7 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_kernel(const NormArgs a) {
       q = at.sum(q, lds);
       float rstd = rsqrtf(__builtin_fmaf(q, inv, a.eps));
       const bool far = is_far(mean, q * inv);
-      if (at.any(far)) {
+      if (__builtin_expect(at.any(far), 0)) {
         deviations(mean, c, q);
         const float m = mean + at.sum(c, lds) * inv;
         deviations(m, c, q);
