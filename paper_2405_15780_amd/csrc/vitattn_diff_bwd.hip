@@ -30,9 +30,11 @@
 // Bound as the forward is. 4 heads of 32,768 tokens, d = 64, e = 128: dK/dV 4.3 ms
 // (4.4 TFLOP, 1.02 PFLOP/s), dQ 3.0 (3.3 TFLOP, 1.1), rows 0.03, the board at its
 // power limit (a large matrix product runs at 1.35 PFLOP/s there). 64 heads of 1,024,
-// d = 32, e = 64: 66, 40 and 9 us, in one and a third rounds of workgroups. Four heads
-// of 5,003, two samples, d = 72, e = 144: dK/dV 226 + 129 us, wide and narrow
-// workgroups in turn, dQ 222.
+// d = 32, e = 64: 67, 40 and 9 us, in one and a third rounds of workgroups. Four heads
+// of 5,003, two samples, d = 72, e = 144: dK/dV 230 + 132 us, wide and narrow
+// workgroups in turn, dQ 221. The wide dK/dV workgroups of d = 64, e = 128 and of d = 72
+// fill 256 registers; two and one more are written to scratch before the loop and read
+// after it.
 #include "vitattn_diff.h"
 
 namespace vitattn {
