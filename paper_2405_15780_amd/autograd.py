@@ -130,6 +130,8 @@ class _Rotary:
                     # the turn by the opposite angles, itself differentiable, of
                     # those that are asked for
                     grads = [_b.plain_memory(g) if need else None for g, need in zip((dq, dk), ctx.needs_input_grad)]
+                    if not any(ctx.needs_input_grad[:2]):  # (for positions that want a gradient: they get none)
+                        return (None,) * 8
                     first, *second = [g for g in grads if g is not None]
                     r = Rotary.apply(first, second[0] if second else None, ctx.saved_tensors[0], *ctx.args, not ctx.inverse)
                     turned = iter(r if second else (r,))
@@ -142,7 +144,7 @@ class _Rotary:
 
 def rotary(q, k, positions, sections, base=10000.0, interleaved=False, joint=False):
     """q [B,Hq,N,d] and k [B,Hk,N,d] (or None) turned by their positions on several
-    axes, with a backward pass (see binding.rotary_fwd)."""
+    axes, with a backward pass (see binding.rotary_fwd); positions get no gradient."""
     sections = tuple(sections)
     if not _wants_grad(q, k):
         return _b.rotary_fwd(q, k, positions, sections, base, interleaved, joint)

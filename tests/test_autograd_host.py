@@ -113,3 +113,13 @@ def test_rotary_turns_back_only_what_is_asked_for(stand_ins, need):
     assert stand_ins[1:] == [("rotary_fwd", tuple((k if need == "k" else q).shape), need == "qk", True)]
     for x, n in ((q, "q"), (k, "k")):
         assert x.grad is None if n not in need else (x.grad == 2).all()
+
+
+def test_positions_get_no_gradient(stand_ins):
+    """Also where they are all that a gradient's own backward could go to."""
+    q, pos = torch.randn((1, 4, 5, 8), requires_grad=True), torch.zeros((5, 1), requires_grad=True)
+    y = va.rotary(q, None, pos, (4,))
+    (g,) = torch.autograd.grad(y.sum(), q, create_graph=True)
+    assert (g == 2).all()
+    g.sum().backward()
+    assert pos.grad is None and q.grad is None
