@@ -421,7 +421,9 @@ enum vitattn_type { VITATTN_BF16 = 0, VITATTN_FP16 = 1, VITATTN_FP32 = 2 };
  *   D           : 1 .. 2^24, else VITATTN_E_UNSUPPORTED; B*H*N below 2^31 - 2^22.
  *   workspace   : vitattn_layer_norm_bwd_workspace_bytes() bytes, 16-byte
  *                 aligned, if dw or db is wanted (partial sums; overwritten).
- * Sums and statistics are fp32; y and dx are rounded once, to their type. dw
+ * Sums and statistics are fp32 (fp64 in the lanes of rows past registers); a mean
+ * of four times the spread or more is corrected to the fp32 number next to the true
+ * one, so equal values have h = 0. y and dx are rounded once, to their type. dw
  * and db are summed in a fixed order that depends on the sizes alone (no
  * atomics): results are bitwise reproducible. Bound by HBM bandwidth.
  */
@@ -489,7 +491,8 @@ int vitattn_rotary(const void* q, vitattn_strides sq, void* q_out, vitattn_strid
  *   lam      : [H], fp32 or bf16 (lam_type), contiguous.
  *   key_lens : null, or int32 [B]: sample b attends to its first key_lens[b]
  *              keys (brought into 0 .. Nk); the rest are not read. A sample
- *              without keys has O = 0, LSE = -inf and no gradients.
+ *              without keys has O = 0, LSE = -inf and no gradients; so has a
+ *              query whose scores are all -inf.
  *   o        : bf16 [B][H][Nq][e], written.
  *   maps     : fp32 [B][2H][Nq][e], dense: each map's output O_m, which the
  *              backward reads; lse: fp32 [B][2H][Nq], dense. Either may be null

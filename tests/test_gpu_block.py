@@ -342,3 +342,37 @@ def test_lazily_negated_operands_are_refused():
             print("not refused", i)
     turned = va.rotary(q, k, pos.resolve_neg(), SECTIONS)
     assert all(t.equal(a, b) for a, b in zip(turned, va.rotary(q, k, -positions(t, 20), SECTIONS)))
+
+
+def test_captured_block_with_its_gradients():
+    """Forward and gradients of the block through the autograd functions, captured and replayed on new inputs."""
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    B, N, W, H, d = 2, 70, 128, 2, 32
+    p = block_params(t, W, H, d, 5, t.bfloat16)
+    x = make((B, N, W), "bfloat16", 6).requires_grad_()
+    g, pos, lens = make((B, N, W), "bfloat16", 7), positions(t, N), t.tensor([70, 41], dtype=t.int32, device="cuda")
+
+    def go():
+        y = block(va, p, x, pos, H, d, lens)
+        return (y.detach(), *t.autograd.grad(y, [x, *p.values()], g))
+
+    side = t.cuda.Stream()
+    side.wait_stream(t.cuda.current_stream())
+    with t.cuda.stream(side):
+        go()
+    t.cuda.current_stream().wait_stream(side)
+    graph = t.cuda.CUDAGraph()
+    with t.cuda.graph(graph):
+        out = go()
+    for seed in (6, 20, 30):
+        with t.no_grad():
+            x.copy_(make((B, N, W), "bfloat16", seed))
+            g.copy_(make((B, N, W), "bfloat16", seed + 1))
+        ref = go()
+        t.cuda.synchronize()
+        graph.replay()
+        go()
+        t.cuda.synchronize()
+        assert all(t.equal(a, b) for a, b in zip(out, ref)), seed
