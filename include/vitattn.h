@@ -436,6 +436,96 @@ int vitattn_layer_norm_bwd(const void* x, vitattn_strides sx, const void* w, con
                            int B, int H, int N, int D, int type, int weight_type, void* workspace,
                            size_t workspace_bytes, void* stream);
 
+/*
+ * Dropout by a counter-based generator: element c of row r (rows counted in the
+ * order [B][H][N], whatever their strides) is kept if its sixteen-bit number is at
+ * least T = round(65536 p), and then multiplied with 65536 / (65536 - T). The numbers
+ * of columns 8 g .. 8 g + 7 are the halves, the lower first, of the four words that
+ * Philox 4x32 with ten rounds gives for the counter (g, r, offset mod 2^32, offset /
+ * 2^32) and the key (seed mod 2^32, seed / 2^32). The mask depends on nothing else, so
+ * the backward forms it again.
+ *   p    : 0 .. 1.
+ *   state: null, or two 64-bit numbers on the device that are added to seed and offset
+ *          (mod 2^64) when the kernels run: a captured graph draws other masks when
+ *          they change between replays.
+ */
+typedef struct vitattn_dropout_spec {
+  unsigned long long seed, offset;
+  const long long* state;
+  double p;
+} vitattn_dropout_spec;
+
+/*
+ * y = residual + dropout(x), or dropout(x) without a residual, of B*H*N rows of D
+ * elements; the gradient of x is the same call on the gradient of y, without a
+ * residual. A dropped element adds nothing, whatever it holds.
+ *   x        : of `type`; residual (or null) and y of residual_type: type or fp32 (type
+ *              without a residual). Rows at any element strides >= 0, the D elements of a
+ *              row contiguous, no alignment beyond the element's. y must not overlap
+ *              itself, and may be x or the residual (the same type and strides).
+ *   sizes    : B*H*N below 2^31 - 2^22, B*H*N*ceil(D/8) below 2^34 - 2^14.
+ * Products and the sum are one fp32 operation, rounded once. Bound by HBM bandwidth.
+ */
+int vitattn_dropout(const void* x, vitattn_strides sx, const void* residual, vitattn_strides sr, void* y,
+                    vitattn_strides sy, int B, int H, int N, int D, int type, int residual_type,
+                    const vitattn_dropout_spec* dropout, void* stream);
+
+#define VITATTN_RMS_MAX_BYTES 32768 /* of a row of x: D up to 16,384 (fp32: 8,192) */
+
+/*
+ * Root-mean-square norm of B*H*N rows of D elements with the residual's addition:
+ *
+ *     h = residual + dropout(x),  r = 1/sqrt(mean(h^2) + eps),  n = h r,  y = n w
+ *
+ * and the backward, given dy and the gradient dh that h has from what follows it:
+ *
+ *     dres = r (g - n mean(g n)) + dh with g = dy w,  dx = dropout(dres),
+ *     dw = sum over the rows of dy n.
+ *
+ * h is rounded to its type and normalised as it is stored. Without a residual (null,
+ * and h null) h is x, in the backward too.
+ *   x, y, dy, dx     : of `type`; residual, h, dh and dres of residual_type: type or
+ *                      fp32 (type without a residual). Rows as for vitattn_dropout. y may
+ *                      be x, h the residual, dx dy and dres dh (the same strides); any other
+ *                      output that shares memory with another operand is rejected.
+ *   w, dw            : [D], contiguous, of weight_type (type or fp32); either may be null.
+ *   rstd             : fp32, one per row in the order [B][H][N]: r. Null in the forward:
+ *                      not wanted.
+ *   dh, dx, dres     : may be null (no such gradient; not wanted).
+ *   dropout          : null: none. The forward's, in the backward; needs a residual.
+ *   eps              : finite, >= 0.
+ *   D                : row bytes up to VITATTN_RMS_MAX_BYTES, else VITATTN_E_UNSUPPORTED;
+ *                      B*H*N below 2^31 - 2^22.
+ *   workspace        : vitattn_rms_norm_bwd_workspace_bytes() bytes, 16-byte aligned, if dw
+ *                      is wanted (partial sums; overwritten).
+ * Sums and r are fp32, outputs rounded once. dw is summed in a fixed order that depends on
+ * the sizes alone (no atomics): results are bitwise reproducible. Bound by HBM bandwidth.
+ */
+int vitattn_rms_norm_fwd(const void* x, vitattn_strides sx, const void* residual, vitattn_strides sr, const void* w,
+                         void* h, vitattn_strides sh, void* y, vitattn_strides sy, float* rstd, int B, int H, int N,
+                         int D, float eps, int type, int residual_type, int weight_type,
+                         const vitattn_dropout_spec* dropout, void* stream);
+size_t vitattn_rms_norm_bwd_workspace_bytes(int B, int H, int N, int D, int type);
+int vitattn_rms_norm_bwd(const void* h, vitattn_strides sh, const void* w, const float* rstd, const void* dy,
+                         vitattn_strides sdy, const void* dh, vitattn_strides sdh, void* dx, vitattn_strides sdx,
+                         void* dres, vitattn_strides sdres, void* dw, int B, int H, int N, int D, int type,
+                         int residual_type, int weight_type, const vitattn_dropout_spec* dropout, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/*
+ * The same norm with an output in 8 bits for a product that takes them: y holds e4m3
+ * bytes (OCP, no infinities, largest 448) at element strides of one byte, and
+ *
+ *     scale = max(max |y| / 448, 2^-126),  byte = y / scale rounded to the nearest even
+ *
+ * with the largest magnitude of the fp32 y over the row (group 0; scale [B*H*N]) or over
+ * each `group` of columns (32, 64 or 128; scale [B*H*N][ceil(D / group)]), dense. NaN stays
+ * NaN and does not count for a scale. Other groups: VITATTN_E_UNSUPPORTED.
+ */
+int vitattn_rms_norm_fp8(const void* x, vitattn_strides sx, const void* residual, vitattn_strides sr, const void* w,
+                         void* h, vitattn_strides sh, void* y, vitattn_strides sy, float* scale, int group, int B,
+                         int H, int N, int D, float eps, int type, int residual_type, int weight_type, void* stream);
+
 /* types of the positions of vitattn_rotary */
 enum vitattn_pos_type { VITATTN_POS_I32 = 0, VITATTN_POS_I64 = 1, VITATTN_POS_F32 = 2 };
 #define VITATTN_ROTARY_INTERLEAVED 1 /* pair p is columns 2p and 2p + 1; else p and R + p */

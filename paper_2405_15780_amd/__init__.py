@@ -26,11 +26,15 @@ from .binding import (  # noqa: F401
     bwd_rowdot,
     diff_bwd,
     diff_fwd,
+    dropout_fwd,
     fwd,
     layer_norm_bwd,
     layer_norm_fwd,
     library,
     merge,
+    rms_norm_bwd,
+    rms_norm_fp8,
+    rms_norm_fwd,
     rotary_fwd,
     status_str,
     strides_of,
@@ -42,4 +46,4 @@ from .binding import (  # noqa: F401
     workspace_bytes,
     workspace_bytes_kv,
 )
-from .autograd import attention, diff_attention, layer_norm, rotary  # noqa: F401,E402
+from .autograd import attention, diff_attention, dropout, layer_norm, rms_norm, rotary  # noqa: F401,E402

@@ -109,6 +109,103 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
     return _LayerNorm.get().apply(x, weight, bias, eps)
 
 
+class _Dropout:
+    _fn = None
+
+    @classmethod
+    def get(cls):
+        if cls._fn is None:
+            torch = _torch()
+
+            class Dropout(torch.autograd.Function):
+                @staticmethod
+                def forward(ctx, x, p, rng, residual):
+                    _save_rng(ctx, p, rng)
+                    ctx.x_dtype = x.dtype
+                    return _b.dropout_fwd(x, p, rng, residual)
+
+                @staticmethod
+                def backward(ctx, dy):
+                    # the same mask on the gradient, itself differentiable
+                    dx = dres = None
+                    if ctx.needs_input_grad[0]:
+                        # (of an fp32 residual's gradient in fp32, rounded once at the end)
+                        dx = Dropout.apply(_b.plain_memory(dy), ctx.p, _saved_rng(ctx), None).to(ctx.x_dtype)
+                    if ctx.needs_input_grad[3]:
+                        dres = dy
+                    return dx, None, None, dres
+
+            cls._fn = Dropout
+        return cls._fn
+
+
+def _save_rng(ctx, p, rng, *tensors):
+    """Keeps p and rng for the backward (and saves `tensors`): a device's state among the
+    saved tensors, whose change in between torch then finds."""
+    state = rng if isinstance(rng, _torch().Tensor) else None
+    ctx.p, ctx.rng = p, None if state is not None else rng
+    ctx.save_for_backward(state, *tensors)
+
+
+def _saved_rng(ctx):
+    state = ctx.saved_tensors[0]
+    return ctx.rng if state is None else state
+
+
+def dropout(x, p, rng, residual=None):
+    """residual + dropout(x) (or dropout(x)) with a backward pass: each element of x is
+    dropped with probability p, by a counter-based generator whose mask is never stored
+    (see binding.dropout_fwd). rng: (seed, offset), or an int64 tensor of both on the
+    device; one of each call's own."""
+    if not _wants_grad(x, residual):
+        return _b.dropout_fwd(x, p, rng, residual)
+    return _Dropout.get().apply(x, p, rng, residual)
+
+
+class _RmsNorm:
+    _fn = None
+
+    @classmethod
+    def get(cls):
+        if cls._fn is None:
+            torch = _torch()
+
+            class RmsNorm(torch.autograd.Function):
+                @staticmethod
+                def forward(ctx, x, weight, residual, eps, p, rng):
+                    y, h, rstd = _b.rms_norm_fwd(x, weight, residual, eps, p, rng)
+                    ctx.set_materialize_grads(False)
+                    _save_rng(ctx, p, rng, h, weight, rstd)
+                    ctx.x_dtype = x.dtype
+                    return y if residual is None else (y, h)
+
+                @staticmethod
+                @torch.autograd.function.once_differentiable
+                def backward(ctx, dy, dh=None):
+                    _, h, weight, rstd = ctx.saved_tensors
+                    if dy is None and dh is None:
+                        return (None,) * 6
+                    dy = torch.zeros(h.shape, dtype=ctx.x_dtype, device=h.device) if dy is None else _b.plain_memory(dy)
+                    need = ctx.needs_input_grad
+                    dx, dres, dw = _b.rms_norm_bwd(h, weight, rstd, dy, None if dh is None else _b.plain_memory(dh), ctx.p,
+                                                   _saved_rng(ctx), want_dx=need[0], want_dresidual=need[2],
+                                                   want_dweight=need[1])
+                    return dx, dw, dres, None, None, None
+
+            cls._fn = RmsNorm
+        return cls._fn
+
+
+def rms_norm(x, weight=None, residual=None, eps=1e-5, p=0.0, rng=None):
+    """Root-mean-square norm over the last dim with a backward pass: y = h / sqrt(mean
+    h^2 + eps) weight with h = x, or with h = residual + dropout(x), which is returned
+    too: (y, h). See binding.rms_norm_fwd."""
+    if not _wants_grad(x, weight, residual):
+        y, h, _ = _b.rms_norm_fwd(x, weight, residual, eps, p, rng, stats=False)
+        return y if residual is None else (y, h)
+    return _RmsNorm.get().apply(x, weight, residual, eps, p, rng)
+
+
 class _Rotary:
     _fn = None
 

@@ -33,7 +33,13 @@ class Forms(ctypes.Structure):
                                               "dkdv_rest64")]
 
 
-_S = Strides
+class DropoutSpec(ctypes.Structure):
+    """vitattn_dropout_spec: dropout's counter and rate."""
+    _fields_ = [("seed", ctypes.c_ulonglong), ("offset", ctypes.c_ulonglong), ("state", ctypes.c_void_p),
+                ("p", ctypes.c_double)]
+
+
+_S, _DROP = Strides, ctypes.POINTER(DropoutSpec)
 
 
 class Int:
@@ -83,6 +89,14 @@ _SIGNATURES = {
     "vitattn_layer_norm_bwd_workspace_bytes": (c_size_t, [_I] * 5),
     "vitattn_layer_norm_bwd": (c_int, [c_void_p, _S] + [c_void_p] * 4 + [_S, c_void_p, _S] + [c_void_p] * 2
                                + [_I] * 6 + [c_void_p, c_size_t, c_void_p]),
+    "vitattn_dropout": (c_int, [c_void_p, _S] * 3 + [_I] * 6 + [_DROP, c_void_p]),
+    "vitattn_rms_norm_fwd": (c_int, [c_void_p, _S] * 2 + [c_void_p] + [c_void_p, _S] * 2 + [c_void_p] + [_I] * 4
+                             + [c_float] + [_I] * 3 + [_DROP, c_void_p]),
+    "vitattn_rms_norm_fp8": (c_int, [c_void_p, _S] * 2 + [c_void_p] + [c_void_p, _S] * 2 + [c_void_p] + [_I] * 5
+                             + [c_float] + [_I] * 3 + [c_void_p]),
+    "vitattn_rms_norm_bwd_workspace_bytes": (c_size_t, [_I] * 5),
+    "vitattn_rms_norm_bwd": (c_int, [c_void_p, _S] + [c_void_p] * 2 + [c_void_p, _S] * 4 + [c_void_p] + [_I] * 7
+                             + [_DROP, c_void_p, c_size_t, c_void_p]),
     "vitattn_rotary": (c_int, ([c_void_p, _S] * 2 + [_I]) * 2 + [c_void_p] + [ctypes.c_longlong] * 3 + [_I]
                        + [ctypes.POINTER(c_int), _I, ctypes.c_double] + [_I] * 5 + [c_void_p]),
     "vitattn_diff_fwd_workspace_bytes": (c_size_t, [_I] * 6),
@@ -781,6 +795,206 @@ def layer_norm_bwd(x, weight, mean, rstd, dy, want_dweight=True, want_dbias=True
           rstd.data_ptr(), dy4.data_ptr(), _norm_strides(dy4, order, D), dx4.data_ptr(), _norm_strides(dx4, order, D),
           _ptr(dw), _ptr(db), *n, D, code, VITATTN_FP32 if wt == torch.float32 else code, _ptr(workspace), size)
     return dx, dw, db
+
+
+# ------------------------------------------------------------------ rms norm, dropout
+
+
+def _rows_of(t, name):
+    """t as rows in up to three leading dims (more become one, by a copy where the
+    layout needs it), whose last dim is contiguous."""
+    n = t.dim()
+    if n < 1 or (t.stride(-1) != 1 and t.shape[-1] != 1):
+        raise TypeError(f"{name} must have at least one dim, the last with unit stride")
+    return t if n <= 4 else t.reshape(-1, t.shape[-1])
+
+
+def _row_sizes(t):
+    """[B, H, N, D] of rows in up to three leading dims."""
+    return (1,) * (4 - t.dim()) + tuple(t.shape)
+
+
+def _row_strides(t):
+    s, n = t.stride(), t.shape
+    lead = [0 if n[i] == 1 else s[i] for i in range(len(n) - 1)]
+    return _strides(*[0] * (3 - len(lead)), *lead)
+
+
+def _rng(p, rng, device):
+    """A DropoutSpec of rate p and rng: (seed, offset), or an int64 tensor of both on the
+    device, read when the kernels run. None where nothing is dropped."""
+    p = float(p)
+    if not 0.0 <= p <= 1.0:
+        raise ValueError("p must be between 0 and 1")
+    if rng is None:
+        if p == 0.0:
+            return None
+        raise ValueError("dropout needs rng: (seed, offset), or an int64 tensor of both on the device")
+    torch = _torch()
+    if isinstance(rng, torch.Tensor):
+        if rng.dtype != torch.int64 or rng.shape != (2,) or rng.device != device or not rng.is_contiguous():
+            raise TypeError(f"rng must be a contiguous int64 tensor of shape (2,) on {device}")
+        return DropoutSpec(0, 0, rng.data_ptr(), p)
+    seed, offset = rng
+    low = 0xffffffffffffffff
+    return DropoutSpec(operator.index(seed) & low, operator.index(offset) & low, None, p)
+
+
+def _like(t, dtype):
+    """A new tensor of t's shape in t's order of dims, the last one contiguous."""
+    torch = _torch()
+    y = torch.empty_like(t, dtype=dtype)
+    if y.is_contiguous() or y.stride(-1) == 1 or y.shape[-1] == 1:
+        return y
+    return torch.empty(t.shape, dtype=dtype, device=t.device)
+
+
+def _row_out(out, name, like, dtype, t4):
+    """The tensor to write and its rows: `out` (checked), or a new one of like's shape."""
+    if out is None:
+        y = _like(like, dtype) if t4 is like else _torch().empty(like.shape, dtype=dtype, device=like.device)
+    else:
+        y = _expect_out(out, name, dtype, like.shape, like.device, dense=t4 is not like)
+    return y, (y if t4 is like else y.view(t4.shape))
+
+
+def _residual_of(x, residual):
+    """The residual's type code, checked (x's without one)."""
+    code = _type_code(x, "x")
+    if x.numel() == 0:
+        raise ValueError("at least one row and one column are needed")
+    if residual is None:
+        return code, code
+    torch = _torch()
+    if not (isinstance(residual, torch.Tensor) and residual.dtype in (x.dtype, torch.float32)):
+        raise TypeError(f"residual must be a {x.dtype} or torch.float32 CUDA tensor of x's shape and device")
+    _as_it_is(_expect(residual, "residual", residual.dtype, x.shape, x.device), "residual")
+    return code, _type_codes()[residual.dtype]
+
+
+def dropout_fwd(x, p, rng, residual=None, out=None):
+    """residual + dropout(x) (or dropout(x)): elements of x (bf16, fp16 or fp32, any
+    strides with the last dim contiguous) are dropped with probability p (in steps of
+    1/65536) and the others multiplied with 1/(1 - p). rng: (seed, offset), or an int64
+    tensor of both on the device, which is read when the kernel runs. The mask goes by
+    rng and an element's place alone and is not stored: the gradient of x is
+    dropout_fwd(dy, p, rng). residual: x's shape, x's type or fp32; the output has its
+    type. out: the tensor to write, may be x or the residual."""
+    code, rcode = _residual_of(x, residual)
+    spec = _rng(p, rng, x.device) or DropoutSpec(0, 0, None, 0.0)
+    x4 = _rows_of(x, "x")
+    r4 = None if residual is None else _rows_of(residual, "residual")
+    y, y4 = _row_out(out, "out", x, x.dtype if residual is None else residual.dtype, x4)
+    B, H, N, D = _row_sizes(x4)
+    _call(x, library().vitattn_dropout, x4.data_ptr(), _row_strides(x4), _ptr(r4),
+          _NO_STRIDES if r4 is None else _row_strides(r4), y4.data_ptr(), _row_strides(y4), B, H, N, D, code, rcode, spec)
+    if out is not None:
+        _written(out)
+    return y
+
+
+def rms_norm_fwd(x, weight=None, residual=None, eps=1e-5, p=0.0, rng=None, out=None, stats=True):
+    """Root-mean-square norm over the last dim of h = residual + dropout(x) (x without
+    a residual): y = h / sqrt(mean h^2 + eps) weight, of x's type. x: bf16, fp16 or fp32,
+    any strides with the last dim contiguous; residual: x's shape, x's type or fp32, which
+    h has too; weight [D]: x's type or fp32. p, rng: see dropout_fwd (they need a
+    residual). Returns y, h (rounded to its type and normalised as it is stored; x without
+    a residual) and 1/sqrt(mean h^2 + eps) in fp32 (None without stats). out: the tensors
+    (y, h) to write, which may be x and the residual; y alone without a residual."""
+    torch = _torch()
+    code, rcode = _residual_of(x, residual)
+    spec = _rng(p, rng, x.device)
+    x4 = _rows_of(x, "x")
+    D = x4.shape[-1]
+    wt = _norm_weights(x, D, weight, None)
+    y_out = h_out = None
+    if out is not None:
+        y_out, h_out = out if residual is not None else (out, None)
+    y, y4 = _row_out(y_out, "out y", x, x.dtype, x4)
+    h, h4, r4, sr, sh = x, None, None, _NO_STRIDES, _NO_STRIDES
+    if residual is not None:
+        h, h4 = _row_out(h_out, "out h", x, residual.dtype, x4)
+        r4 = _rows_of(residual, "residual")
+        sr, sh = _row_strides(r4), _row_strides(h4)
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if stats else None
+    _call(x, library().vitattn_rms_norm_fwd, x4.data_ptr(), _row_strides(x4), _ptr(r4), sr, _ptr(weight), _ptr(h4), sh,
+          y4.data_ptr(), _row_strides(y4), _ptr(rstd), *_row_sizes(x4), eps, code, rcode,
+          VITATTN_FP32 if wt == torch.float32 else code, spec)
+    if out is not None:
+        _written(y) if residual is None else _written(y, h)
+    return y, h, rstd
+
+
+def rms_norm_fp8(x, weight=None, residual=None, eps=1e-5, group=None):
+    """rms_norm_fwd for a product in 8 bits: y / scale as torch.float8_e4m3fn, the
+    scales in fp32 (max |y| / 448 over the row, x.shape[:-1]; or over each `group` of 32, 64
+    or 128 columns, x.shape[:-1] + (ceil(D / group),)), and h."""
+    torch = _torch()
+    code, rcode = _residual_of(x, residual)
+    x4 = _rows_of(x, "x")
+    D = x4.shape[-1]
+    wt = _norm_weights(x, D, weight, None)
+    if group is not None and group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64, 128 or None (the row)")
+    y, y4 = _row_out(None, "", x, torch.float8_e4m3fn, x4)
+    h, h4, r4, sr, sh = x, None, None, _NO_STRIDES, _NO_STRIDES
+    if residual is not None:
+        h, h4 = _row_out(None, "", x, residual.dtype, x4)
+        r4 = _rows_of(residual, "residual")
+        sr, sh = _row_strides(r4), _row_strides(h4)
+    shape = x.shape[:-1] if group is None else x.shape[:-1] + ((D + group - 1) // group,)
+    scale = torch.empty(shape, dtype=torch.float32, device=x.device)
+    _call(x, library().vitattn_rms_norm_fp8, x4.data_ptr(), _row_strides(x4), _ptr(r4), sr, _ptr(weight), _ptr(h4), sh,
+          y4.data_ptr(), _row_strides(y4), scale.data_ptr(), group or 0, *_row_sizes(x4), eps, code, rcode,
+          VITATTN_FP32 if wt == torch.float32 else code)
+    return y, scale, h
+
+
+def rms_norm_bwd(h, weight, rstd, dy, dh=None, p=0.0, rng=None, want_dx=True, want_dresidual=True, want_dweight=True,
+                 workspace=None):
+    """dx, dresidual and dweight of rms_norm_fwd (with its p and rng) for the upstream
+    gradients dy of y (x's type) and dh of h (h's type, or None). Those that are not wanted
+    are None, and dweight without a weight; dx and dresidual are one tensor where they are
+    the same values (one type, nothing dropped)."""
+    torch = _torch()
+    rcode = _type_code(h, "h")
+    code = _type_code(dy, "dy")
+    if h.dtype not in (dy.dtype, torch.float32):
+        raise TypeError("h must have dy's type or fp32")
+    shape, device = h.shape, h.device
+    if h.numel() == 0:
+        raise ValueError("at least one row and one column are needed")
+    _expect(dy, "dy", dy.dtype, shape, device)
+    if dh is not None:
+        _as_it_is(_expect(dh, "dh", h.dtype, shape, device), "dh")
+    if not (isinstance(rstd, torch.Tensor) and rstd.device == device and rstd.dtype == torch.float32
+            and rstd.shape == shape[:-1]):
+        raise TypeError(f"rstd must be a torch.float32 CUDA tensor of shape {tuple(shape[:-1])} on {device}")
+    spec = _rng(p, rng, device)
+    h4, dy4 = _rows_of(h, "h"), _rows_of(dy, "dy")
+    D = h4.shape[-1]
+    wt = _norm_weights(dy, D, weight, None)
+    rstd = rstd.contiguous()
+    one = h.dtype == dy.dtype and (spec is None or spec.p * 65536 <= 0.5) and want_dx and want_dresidual
+    dres, dres4 = _row_out(None, "", h, h.dtype, h4) if want_dresidual else (None, None)
+    dx, dx4 = _row_out(None, "", h, dy.dtype, h4) if want_dx and not one else (None, None)
+    dh4 = None if dh is None else _rows_of(dh, "dh")
+    dw = torch.empty(D, dtype=wt, device=device) if want_dweight and weight is not None else None
+    lib, size = library(), 0
+    sizes = _row_sizes(h4)
+    if workspace is not None:
+        size = _expect_workspace(workspace, device).numel() * workspace.element_size()
+    elif dw is not None:
+        size = lib.vitattn_rms_norm_bwd_workspace_bytes(*sizes, code)
+        workspace = torch.empty(size // 4, dtype=torch.float32, device=device)
+
+    def strides(t):
+        return _NO_STRIDES if t is None else _row_strides(t)
+
+    _call(h, lib.vitattn_rms_norm_bwd, h4.data_ptr(), strides(h4), _ptr(weight), rstd.data_ptr(), dy4.data_ptr(),
+          strides(dy4), _ptr(dh4), strides(dh4), _ptr(dx4), strides(dx4), _ptr(dres4), strides(dres4), _ptr(dw), *sizes,
+          code, rcode, VITATTN_FP32 if wt == torch.float32 else code, spec, _ptr(workspace), size)
+    return dres if one else dx, dres, dw
 
 
 def _strides_any(t):

@@ -216,6 +216,58 @@ int norm_partials(int rows, int D, int elem_bytes);  // rows of the backward's p
 hipError_t launch_norm_fwd(const NormArgs& a);
 hipError_t launch_norm_bwd(const NormArgs& a);
 
+// Dropout's counter and rate; see vitattn_random.h.
+struct DropArgs {
+  unsigned long long seed, offset;
+  const long long* state;  // null, or two numbers on the device that add to them
+  uint32_t threshold;      // of 65536; 0: nothing is dropped
+  float up;
+};
+
+// y = [residual +] dropout(x) of rows of D elements; see vitattn_dropout.hip.
+struct DropoutArgs {
+  const void* x;
+  const void* residual;  // may be null
+  void* y;               // of residual_type
+  RowMap mx, mr, my;
+  RowMap ml;  // a row's index among all, by which the counter goes
+  int rows, n1, n2, D, pieces;  // pieces of eight columns of a row
+  uint32_t recip, shift;
+  int type, residual_type;
+  DropArgs drop;
+  hipStream_t stream;
+};
+hipError_t launch_dropout(const DropoutArgs& a);
+
+// Root-mean-square norm with the residual's addition; see vitattn_rms.hip.
+struct RmsArgs {
+  const void* x;         // forward: the branch (or the rows, without a residual)
+  const void* residual;  // forward; may be null
+  void* h;               // forward: written, residual + dropout(x); backward: read
+  const void* w;         // may be null
+  void* y;               // forward, of type; or of 8 bits
+  float* scale;          // forward: the 8-bit output's, else null
+  float* rstd;           // one per row; written by the forward unless null
+  const void* dy;        // backward
+  const void* dh;        // backward: the gradient of h from what follows, may be null
+  void* dx;              // backward, may be null
+  void* dres;            // backward, may be null
+  void* dw;              // backward, may be null
+  float* partial;        // workspace: [rms_partials()][D], null without dw
+  RowMap mx, mr, mh, my, mdy, mdh, mdx, mdres;
+  RowMap ml;  // a row's index among all: the counter's and the statistics'
+  int rows, n1, n2, D, lanes;
+  int group;  // columns that share a scale (0: the row)
+  float eps;
+  int type, residual_type;
+  bool w_f32, drop_on;
+  DropArgs drop;
+  hipStream_t stream;
+};
+int rms_partials(int rows, int D, int elem_bytes);
+hipError_t launch_rms_fwd(const RmsArgs& a);
+hipError_t launch_rms_bwd(const RmsArgs& a);
+
 // Rotary positions; see vitattn_rotary.hip.
 constexpr int kRotaryMaxPairs = 128;  // VITATTN_ROTARY_MAX_PAIRS
 struct RotaryArgs {

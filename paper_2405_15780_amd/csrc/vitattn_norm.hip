@@ -39,7 +39,7 @@ namespace vitattn {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kRowThreads;
 
 // row r -> its three indexes
 __device__ __forceinline__ void split_row(const NormArgs& a, int r, int& i0, int& i1, int& i2) {
@@ -53,65 +53,6 @@ __device__ __forceinline__ long long row_at(const NormArgs& a, const RowMap& m, 
   split_row(a, r, i0, i1, i2);
   return m.at(i0, i1, i2);
 }
-
-// V weights from element c on (n of them real, zeros behind), fp32 or T
-template <typename T>
-__device__ __forceinline__ void load_weights(const void* p, bool f32, long long c, int n, float (&w)[Piece<T>::V]) {
-  constexpr int V = Piece<T>::V;
-  if (f32) {
-#pragma unroll
-    for (int e = 0; e < V; ++e) w[e] = e < n ? static_cast<const float*>(p)[c + e] : 0.f;
-  } else {
-    Piece<T> x;
-    x.load(static_cast<const T*>(p) + c, n);
-#pragma unroll
-    for (int e = 0; e < V; ++e) w[e] = x.get(e);
-  }
-}
-
-// Where a thread stands: its row of the workgroup's `per` at a time (outside
-// them: a wave's lanes behind its last whole row) and its lane of the row.
-template <bool BLOCK>
-struct Place {
-  int L, lane, row, per;
-  __device__ __forceinline__ explicit Place(int lanes) : L(lanes) {
-    if constexpr (BLOCK) {
-      lane = threadIdx.x;
-      row = 0;
-      per = 1;
-    } else {
-      const int wl = threadIdx.x & 63, rpw = 64 / L, g = wl / L;
-      lane = wl - g * L;
-      per = rpw * (kThreads / 64);
-      row = g < rpw ? (int)(threadIdx.x >> 6) * rpw + g : -1;
-    }
-  }
-  // Sum over the row's lanes (BLOCK: over the workgroup), the same in all.
-  __device__ __forceinline__ float sum(float x, float* lds) const {
-    if (BLOCK || (L & (L - 1)) == 0) {
-#pragma unroll
-      for (int m = 32; m >= 1; m >>= 1)
-        if (BLOCK || m < L) x += __shfl_xor(x, m, 64);
-    } else {
-      const int at = threadIdx.x & 63;
-      for (int m = 32; m >= 1; m >>= 1) {
-        if (m >= L) continue;
-        const float y = __shfl(x, (at + m) & 63, 64);
-        x += lane + m < L ? y : 0.f;
-      }
-      x = __shfl(x, at - lane, 64);
-    }
-    if constexpr (BLOCK) {
-      __syncthreads();
-      if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-      __syncthreads();
-      x = lds[0] + lds[1] + lds[2] + lds[3];
-    }
-    return x;
-  }
-  // whether it holds anywhere in the wave (BLOCK: all of which agree)
-  __device__ __forceinline__ static bool any(bool x) { return BLOCK ? x : __any(x); }
-};
 
 // A mean that a row's spread (var about it) is small beside. Below this bound the
 // mean's error of n 2^-24 |mean|, n the length of a lane's sum and the lanes' tree,
@@ -520,42 +461,6 @@ __global__ __launch_bounds__(64 * kWeightWaves) void norm_weights_kernel(const N
   else static_cast<T*>(out)[at] = (T)s;
 }
 
-// Lanes that share a row and pieces per lane (lanes = 0: too long for registers).
-// With a piece per lane a wave sums over up to 64 lanes for 16 bytes of each; more
-// pieces need fewer lanes, hence fewer steps, and are as many loads. The forward
-// takes two from 4 pieces on (D = 64, 46 MB 17.6 -> 15.8 us, 400 MB 165 -> 171; 72
-// 22.4 -> 19.8 and 178 -> 185; 128 19.8 -> 17.3 and 164 -> 157) and from 16 pieces on
-// two or three, whichever keeps more lanes at work (D = 192 25.3 -> 17.3 and 195 ->
-// 157, 768 21.3 -> 17.4 and 161 -> 152). The backward keeps dw's and db's share of
-// each piece as well: one below 16 pieces (two: D = 64 35 -> 43 us), then two, or
-// three where two leave a fifth of the lanes idle (D = 192 42 -> 37 and 313 -> 235,
-// 384 42 -> 37 and 320 -> 230, 768, against two, 40 -> 35 and 269 -> 228). Four are
-// for rows of more. These are rules on D alone: a row's bits do not depend on the
-// call it is part of.
-struct Shape {
-  int lanes, np;
-};
-Shape shape_of(int D, int V, bool fwd) {
-  const int pieces = (D + V - 1) / V;
-  if (pieces > 256) {
-    const int np = (pieces + kThreads - 1) / kThreads;
-    return np > 8 ? Shape{0, 0} : Shape{kThreads, np == 7 ? 8 : np};
-  }
-  if (pieces < (fwd ? 4 : 16)) return {pieces, 1};
-  if (pieces < 16) return {(pieces + 1) / 2, 2};
-  Shape best = {(pieces + 3) / 4, 4};
-  int most = 0;
-  for (int np = 2; np <= 3; ++np) {
-    const int L = (pieces + np - 1) / np;
-    const int used = L > 64 ? 0 : pieces * (64 / L) * 60 / np;  // of 64 * 60
-    if (used <= most) continue;
-    most = used;
-    best = {L, np};
-    if (!fwd && used >= 64 * 48) break;
-  }
-  return best;
-}
-
 // Workgroups of the backward that a CU holds, from the registers of a lane:
 // five fp32 values per element (w, dw, db and the row's h and g), the rows as
 // they are and about 48 more, at most four. The grid is this many for each of
@@ -569,10 +474,10 @@ constexpr int bwd_resident(int np, int v, bool block) {
 }
 
 // Rows of a workgroup at a time.
-int rows_of(const Shape& s, bool fwd) {
+int rows_of(const RowShape& s, bool fwd) {
   return s.lanes > 64 ? 1 : 64 / s.lanes * (kThreads / 64) * (fwd ? rows_at_once(s.np) : 1);
 }
-int groups_of(const Shape& s, int rows, bool fwd) {
+int groups_of(const RowShape& s, int rows, bool fwd) {
   return (int)(((long long)rows + rows_of(s, fwd) - 1) / rows_of(s, fwd));
 }
 
@@ -597,7 +502,7 @@ hipError_t go(const NormArgs& a, int n) {
 }
 
 template <typename T, bool FWD>
-hipError_t go_shape(const NormArgs& a, const Shape& s, int n) {
+hipError_t go_shape(const NormArgs& a, const RowShape& s, int n) {
   const bool block = s.lanes > 64;
   switch (s.np) {
     case 1: return go<T, FWD, 1, false>(a, n);  // (long rows have two pieces per lane or more)
@@ -612,7 +517,7 @@ hipError_t go_shape(const NormArgs& a, const Shape& s, int n) {
 
 template <typename T>
 hipError_t fwd_t(NormArgs a) {
-  const Shape s = shape_of(a.D, Piece<T>::V, true);
+  const RowShape s = row_shape(a.D, Piece<T>::V, true);
   if (s.lanes == 0) {
     norm_fwd_long_kernel<T><<<min(a.rows, 2048), kThreads, 0, a.stream>>>(a);
     return hipGetLastError();
@@ -623,7 +528,7 @@ hipError_t fwd_t(NormArgs a) {
 
 template <typename T>
 hipError_t bwd_t(NormArgs a) {
-  const Shape s = shape_of(a.D, Piece<T>::V, false);
+  const RowShape s = row_shape(a.D, Piece<T>::V, false);
   const int n = norm_partials(a.rows, a.D, (int)sizeof(T));
   hipError_t err;
   if (s.lanes == 0) {
@@ -643,7 +548,7 @@ hipError_t bwd_t(NormArgs a) {
 }  // namespace
 
 int norm_partials(int rows, int D, int elem_bytes) {
-  const Shape s = shape_of(D, 16 / elem_bytes, false);
+  const RowShape s = row_shape(D, 16 / elem_bytes, false);
   if (s.lanes == 0) return rows < 64 ? rows : 64;
   return min(groups_of(s, rows, false), 256 * bwd_resident(s.np, 16 / elem_bytes, s.lanes > 64));
 }
