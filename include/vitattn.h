@@ -619,6 +619,89 @@ int vitattn_diff_bwd(const void* q, vitattn_strides sq, const void* k, vitattn_s
                      vitattn_strides sdk, void* dv, vitattn_strides sdv, void* dlam, int B, int H, int Nq, int Nk, int d,
                      int e, float scale, void* workspace, size_t workspace_bytes, void* stream);
 
+#define VITATTN_SELECT_MAX 256          /* blocks that a group may choose */
+#define VITATTN_SPARSE_MAX_TOPK 1024    /* listed blocks of a group that the attention takes */
+#define VITATTN_SPARSE_MAX_BLOCK 1024   /* keys of a block */
+#define VITATTN_SPARSE_MAX_BLOCKS 16384 /* blocks of a sample's keys */
+
+/*
+ * Attention over blocks of keys that a cheap score chooses. The Nk keys of a sample are
+ * cut into nb = ceil(Nk / block) blocks of `block` keys, the Nq queries into groups of
+ * q_block neighbours (1: each query by itself), and each group of each head attends to
+ * topk blocks. The queries' H heads share the Hk heads of keys and values, H / Hk
+ * neighbouring heads each.
+ *
+ * The means of the blocks' keys, in 8 bits: with m the mean of a block's keys (of the
+ * sample's first key_lens[b]),
+ *
+ *     means = round(m (127 (1 / max|m|))),  scales = max|m| (1 / 127); -1 of a block without keys.
+ *
+ *   k       : bf16 [B][Hk][Nk][d]; strides as for vitattn_fwd_strided.
+ *   key_lens: null, or int32 [B], brought into 0 .. Nk.
+ *   means   : int8 [B][Hk][nb][P], dense, 16-byte aligned, P = d rounded up to a multiple of
+ *             64, columns from d on zero; scales: fp32 [B][Hk][nb].
+ *   block   : a multiple of 64 up to VITATTN_SPARSE_MAX_BLOCK, nb up to
+ *             VITATTN_SPARSE_MAX_BLOCKS, d as for vitattn_fwd; else VITATTN_E_UNSUPPORTED.
+ * Sums are fp64 (exact for values within 2^37 of each other), and so is each step of the
+ * scaling; a mean that is not finite counts as 0. Bound by HBM bandwidth.
+ */
+int vitattn_block_means(const void* k, vitattn_strides sk, const int* key_lens, void* means, float* scales, int B,
+                        int Hk, int Nk, int d, int block, void* stream);
+
+/*
+ * The choice: with x the mean of a group's queries and X = round(x (127 (1 / max|x|))), block
+ * j has the score (X . means_j) scales_j, a whole number times an fp32 number, rounded
+ * once. Written are the topk blocks of highest score in ascending order (of equal ones the
+ * lowest), then -1 where there are fewer blocks with keys.
+ *   q     : bf16 [B][H][Nq][d].
+ *   blocks: int32 [B][H][ceil(Nq / q_block)][topk], dense.
+ *   topk  : 1 .. VITATTN_SELECT_MAX, else VITATTN_E_UNSUPPORTED.
+ */
+int vitattn_block_select(const void* q, vitattn_strides sq, const void* means, const float* scales, int* blocks, int B,
+                         int H, int Hk, int Nq, int d, int nb, int q_block, int topk, void* stream);
+
+/*
+ * The attention: row i of head h attends to the keys of the blocks blocks[b][h][i /
+ * q_block][0 .. topk - 1] among the sample's first key_lens[b]:
+ *
+ *     S_ij = scale q_i . k_j,  LSE_i = log sum_j exp(S_ij),  P = exp(S - LSE),  O = P V
+ *
+ * and the backward as for vitattn_bwd, dK and dV summed over the heads that share them.
+ * Numbers outside 0 .. nb - 1 stand for no block, a block given twice counts once, and the
+ * order does not matter. A row without keys has O = 0, LSE = -inf and no gradients; so has a
+ * row whose scores are all -inf. Keys that a row does not attend to do not reach it, also
+ * where they are not finite.
+ *   q, o, dout, dq : bf16 [B][H][Nq][d]; k, v, dk, dv: bf16 [B][Hk][Nk][d]; strides as for
+ *                    vitattn_fwd_strided, (rows + 1280) * row * 2 below 2^31.
+ *   blocks         : int32, dense, from vitattn_block_select or any other choice.
+ *   o32, lse       : fp32, dense, [B][H][Nq][d] and [B][H][Nq]: the unrounded output and LSE,
+ *                    which the backward reads; either may be null in the forward.
+ *   topk           : 1 .. VITATTN_SPARSE_MAX_TOPK; d, block and nb as above, H / Hk up to
+ *                    2047; else VITATTN_E_UNSUPPORTED.
+ *   sizes          : Nq up to 2^26, B*H*(Nq + 128) and B*Hk*nb*block below 2^30.
+ *   workspace      : at least the bytes the matching function gives (0 if invalid; the
+ *                    forward's is 0 unless up to 256 queries split their blocks over
+ *                    workgroups), 16-byte aligned.
+ *   overlaps       : an output (or the workspace) that shares memory with another operand
+ *                    is rejected.
+ * Fastest where q_block is a multiple of 64 (better 128): else 64 neighbouring rows go over
+ * the union of what they chose. Scores, statistics and sums are fp32; P and dS are rounded to
+ * bf16 as operands of the matrix cores, outputs once. Results are bitwise deterministic, and a
+ * head's results do not depend on the call it is part of. Atomics count integers only.
+ */
+size_t vitattn_block_fwd_workspace_bytes(int B, int H, int Hk, int Nq, int Nk, int d, int block, int q_block, int topk);
+int vitattn_block_fwd(const void* q, vitattn_strides sq, const void* k, vitattn_strides sk, const void* v,
+                      vitattn_strides sv, const int* blocks, const int* key_lens, void* o, vitattn_strides so,
+                      float* o32, float* lse, int B, int H, int Hk, int Nq, int Nk, int d, int block, int q_block,
+                      int topk, float scale, void* workspace, size_t workspace_bytes, void* stream);
+size_t vitattn_block_bwd_workspace_bytes(int B, int H, int Hk, int Nq, int Nk, int d, int block, int q_block, int topk);
+int vitattn_block_bwd(const void* q, vitattn_strides sq, const void* k, vitattn_strides sk, const void* v,
+                      vitattn_strides sv, const int* blocks, const int* key_lens, const float* o32, const float* lse,
+                      const void* dout, vitattn_strides sdo, void* dq, vitattn_strides sdq, void* dk,
+                      vitattn_strides sdk, void* dv, vitattn_strides sdv, int B, int H, int Hk, int Nq, int Nk, int d,
+                      int block, int q_block, int topk, float scale, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
 /* Human-readable name of a status code (static storage, never NULL). */
 const char* vitattn_status_str(int status);
 

@@ -17,6 +17,10 @@ from .binding import (  # noqa: F401
     VitattnError,
     agg_bwd,
     agg_fwd,
+    block_bwd,
+    block_fwd,
+    block_means,
+    block_select,
     bwd,
     bwd_dkdv,
     bwd_dkdv_ds,
@@ -46,4 +50,4 @@ from .binding import (  # noqa: F401
     workspace_bytes,
     workspace_bytes_kv,
 )
-from .autograd import attention, diff_attention, dropout, layer_norm, rms_norm, rotary  # noqa: F401,E402
+from .autograd import attention, block_attention, diff_attention, dropout, layer_norm, rms_norm, rotary  # noqa: F401,E402

@@ -248,6 +248,17 @@ def rotary(q, k, positions, sections, base=10000.0, interleaved=False, joint=Fal
     return _Rotary.get().apply(q, k, positions, sections, base, interleaved, joint, False)
 
 
+def _rows_in_reach(g, behind):
+    """An upstream gradient as the attention kernels take it: shared or misaligned rows, and
+    those that 32-bit offsets do not reach (`behind` rows past the last), are laid out anew."""
+    g = _b.plain_memory(g)
+    s = _b._diff_strides(g)
+    if s.row < g.shape[3] or s.row % 8 or s.head % 8 or s.batch % 8 or g.data_ptr() % 16 \
+            or (g.shape[2] + behind) * s.row * 2 > 0x7fffffff:
+        g = _torch().empty(g.shape, dtype=g.dtype, device=g.device).copy_(g)
+    return g
+
+
 class _DiffAttention:
     _fn = None
 
@@ -268,12 +279,7 @@ class _DiffAttention:
                 @torch.autograd.function.once_differentiable
                 def backward(ctx, grad_o):
                     q, k, v, lam, o2, lse, key_lens = ctx.saved_tensors
-                    g = _b.plain_memory(grad_o)
-                    s = _b._diff_strides(g)
-                    # shared or misaligned rows are laid out anew
-                    if s.row < g.shape[3] or s.row % 8 or s.head % 8 or s.batch % 8 or g.data_ptr() % 16 \
-                            or (g.shape[2] + 512) * s.row * 2 > 0x7fffffff:
-                        g = torch.empty(g.shape, dtype=g.dtype, device=g.device).copy_(g)
+                    g = _rows_in_reach(grad_o, 512)
                     dq, dk, dv, dlam = _b.diff_bwd(q, k, v, lam, None, o2, lse, g, ctx.scale, key_lens,
                                                    want_dlam=ctx.needs_input_grad[3])
                     return dq, dk, dv, dlam, None, None
@@ -296,3 +302,41 @@ def diff_attention(q, k, v, lam, scale=None, key_lens=None):
     if not _wants_grad(q, k, v, lam):
         return _b.diff_fwd(q, k, v, lam, scale, key_lens, save=False)[0]
     return _DiffAttention.get().apply(q, k, v, lam, scale, key_lens)
+
+
+class _BlockAttention:
+    _fn = None
+
+    @classmethod
+    def get(cls):
+        if cls._fn is None:
+            torch = _torch()
+
+            class BlockAttention(torch.autograd.Function):
+                @staticmethod
+                def forward(ctx, q, k, v, blocks, block, q_block, scale, key_lens):
+                    o, o32, lse = _b.block_fwd(q, k, v, blocks, block, q_block, scale, key_lens)
+                    ctx.save_for_backward(q, k, v, blocks, o32, lse, key_lens)
+                    ctx.args = (block, q_block, scale)
+                    return o
+
+                @staticmethod
+                @torch.autograd.function.once_differentiable
+                def backward(ctx, grad_o):
+                    q, k, v, blocks, o32, lse, key_lens = ctx.saved_tensors
+                    grads = _b.block_bwd(q, k, v, blocks, o32, lse, _rows_in_reach(grad_o, 1280), *ctx.args, key_lens)
+                    return *grads, None, None, None, None, None
+
+            cls._fn = BlockAttention
+        return cls._fn
+
+
+def block_attention(q, k, v, blocks, block=128, q_block=1, scale=None, key_lens=None):
+    """softmax(scale Q K^T) V over the key blocks that each group of q_block queries chose,
+    with a backward pass (the choice itself has no gradient): q [B,H,Nq,d], k and v
+    [B,Hk,Nk,d] bf16, H a multiple of Hk; blocks int32 [B,H,ceil(Nq/q_block),topk], as
+    block_select gives them (see binding.block_fwd); scale defaults to 1/sqrt(d). Returns o,
+    bf16 [B,H,Nq,d]."""
+    if not _wants_grad(q, k, v):
+        return _b.block_fwd(q, k, v, blocks, block, q_block, scale, key_lens, save=False)[0]
+    return _BlockAttention.get().apply(q, k, v, blocks, block, q_block, scale, key_lens)

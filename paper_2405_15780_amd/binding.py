@@ -105,6 +105,14 @@ _SIGNATURES = {
     "vitattn_diff_bwd_workspace_bytes": (c_size_t, [_I] * 6),
     "vitattn_diff_bwd": (c_int, [c_void_p, _S] * 3 + [c_void_p, _I] + [c_void_p] * 3
                          + [c_void_p, _S] * 4 + [c_void_p] + [_I] * 6 + [c_float, c_void_p, c_size_t, c_void_p]),
+    "vitattn_block_means": (c_int, [c_void_p, _S] + [c_void_p] * 3 + [_I] * 5 + [c_void_p]),
+    "vitattn_block_select": (c_int, [c_void_p, _S] + [c_void_p] * 3 + [_I] * 8 + [c_void_p]),
+    "vitattn_block_fwd_workspace_bytes": (c_size_t, [_I] * 9),
+    "vitattn_block_fwd": (c_int, [c_void_p, _S] * 3 + [c_void_p] * 2 + [c_void_p, _S] + [c_void_p] * 2 + [_I] * 9
+                          + [c_float, c_void_p, c_size_t, c_void_p]),
+    "vitattn_block_bwd_workspace_bytes": (c_size_t, [_I] * 9),
+    "vitattn_block_bwd": (c_int, [c_void_p, _S] * 3 + [c_void_p] * 4 + [c_void_p, _S] * 4 + [_I] * 9
+                          + [c_float, c_void_p, c_size_t, c_void_p]),
     "vitattn_status_str": (ctypes.c_char_p, [c_int]),
     "vitattn_version": (ctypes.c_char_p, []),
 }
@@ -1170,3 +1178,125 @@ def diff_bwd(q, k, v, lam, o, o2, lse, dout, scale=None, key_lens=None, want_dla
           _diff_strides(dout), dq.data_ptr(), _diff_strides(dq), dk.data_ptr(), _diff_strides(dk), dv.data_ptr(),
           _diff_strides(dv), _ptr(dlam), *sizes, _default_scale(d, scale), ws.data_ptr(), ws.numel() * ws.element_size())
     return dq, dk, dv, dlam
+
+# ------------------------------------------------------------------ attention over chosen key blocks
+
+
+def _bf16_heads(t, name, device=None):
+    _as_input(t, name, device)
+    if t.is_neg():
+        _negated(name)
+    return t
+
+
+def _key_lens(key_lens, B, device):
+    if key_lens is not None:
+        _expect(key_lens, "key_lens", _torch().int32, (B,), device, dense=True)
+
+
+def block_means(k, block=128, key_lens=None):
+    """The means of each block of `block` keys (bf16 [B,Hk,Nk,d], a multiple of 64) in 8
+    bits, for block_select: (means int8 [B,Hk,blocks,d up to a multiple of 64], scales fp32
+    [B,Hk,blocks], -1 of a block without keys). key_lens: int32 [B], sample b has its first
+    key_lens[b] keys. A program that serves keeps them beside its keys."""
+    torch = _torch()
+    _bf16_heads(k, "k")
+    B, Hk, Nk, d = k.shape
+    _key_lens(key_lens, B, k.device)
+    block = operator.index(block)
+    if block < 1:
+        raise ValueError("block must be at least 1")
+    nb = -(-Nk // block)
+    means = torch.empty((B, Hk, nb, -(-d // 64) * 64), dtype=torch.int8, device=k.device)
+    scales = torch.empty((B, Hk, nb), dtype=torch.float32, device=k.device)
+    _call(k, library().vitattn_block_means, k.data_ptr(), _diff_strides(k), _ptr(key_lens), means.data_ptr(),
+          scales.data_ptr(), B, Hk, Nk, d, block)
+    return means, scales
+
+
+def block_select(q, means, topk, q_block=1):
+    """The topk blocks that each group of q_block neighbouring queries (bf16 [B,H,Nq,d])
+    scores highest, by the product of their mean with the blocks' (block_means; H a multiple
+    of Hk), both in 8 bits: int32 [B,H,ceil(Nq/q_block),topk] in ascending order, ties to the
+    lowest, -1 behind the last if there are fewer. topk up to 256."""
+    torch = _torch()
+    _bf16_heads(q, "q")
+    B, H, Nq, d = q.shape
+    m, scales = means
+    if not (isinstance(m, torch.Tensor) and m.dim() == 4):
+        raise TypeError("means must be what block_means returned")
+    Hk, nb = m.shape[1:3]
+    _expect(m, "means[0]", torch.int8, (B, Hk, nb, -(-d // 64) * 64), q.device, dense=True)
+    _expect(scales, "means[1]", torch.float32, (B, Hk, nb), q.device, dense=True)
+    topk, q_block = operator.index(topk), operator.index(q_block)
+    if topk < 1 or q_block < 1 or Hk < 1 or H % Hk:
+        raise ValueError("topk and q_block must be at least 1, and H a multiple of the means' heads")
+    blocks = torch.empty((B, H, -(-Nq // q_block), topk), dtype=torch.int32, device=q.device)
+    _call(q, library().vitattn_block_select, q.data_ptr(), _diff_strides(q), m.data_ptr(), scales.data_ptr(),
+          blocks.data_ptr(), B, H, Hk, Nq, d, nb, q_block, topk)
+    return blocks
+
+
+def _block_args(q, k, v, blocks, block, q_block, key_lens):
+    _bf16_heads(q, "q")
+    device = q.device
+    _bf16_heads(k, "k", device)
+    _bf16_heads(v, "v", device)
+    B, H, Nq, d = q.shape
+    Bk, Hk, Nk, dk = k.shape
+    if (Bk, dk) != (B, d) or v.shape != k.shape or Hk < 1 or H % Hk:
+        raise ValueError("k and v must be [B, Hk, Nk, d] with the B and d of q, whose heads are a multiple of Hk")
+    block, q_block = operator.index(block), operator.index(q_block)
+    if block < 1 or q_block < 1:
+        raise ValueError("block and q_block must be at least 1")
+    if not (isinstance(blocks, _torch().Tensor) and blocks.dim() == 4):
+        raise TypeError("blocks must be an int32 CUDA tensor [B, H, groups, topk]")
+    topk = blocks.shape[3]
+    _expect(blocks, "blocks", _torch().int32, (B, H, -(-Nq // q_block), topk), device, dense=True)
+    _key_lens(key_lens, B, device)
+    return B, H, Hk, Nq, Nk, d, block, q_block, topk
+
+
+def block_fwd(q, k, v, blocks, block=128, q_block=1, scale=None, key_lens=None, out=None, save=True, workspace=None):
+    """Attention of q (bf16 [B,H,Nq,d]) over chosen blocks of `block` keys (k, v [B,Hk,Nk,d],
+    H a multiple of Hk): row i attends to the blocks blocks[b,h,i // q_block] (int32, from
+    block_select or any other choice; numbers outside the blocks stand for none, one given
+    twice counts once) within the sample's first key_lens[b] keys. Returns o (bf16
+    [B,H,Nq,d], in q's order of heads and rows) and what block_bwd needs: o32 (the output
+    unrounded, fp32) and lse (fp32 [B,H,Nq]); None, None unless save."""
+    torch = _torch()
+    sizes = _block_args(q, k, v, blocks, block, q_block, key_lens)
+    B, H, _, Nq, _, d = sizes[:6]
+    o = _like_layout(q, (B, H, Nq, d)) if out is None else _expect_out(out, "out", torch.bfloat16, (B, H, Nq, d), q.device)
+    o32 = lse = None
+    if save:
+        o32 = torch.empty((B, H, Nq, d), dtype=torch.float32, device=q.device)
+        lse = torch.empty((B, H, Nq), dtype=torch.float32, device=q.device)
+    lib = library()
+    need = int(lib.vitattn_block_fwd_workspace_bytes(*sizes))
+    ws = _diff_workspace(workspace, need, q.device) if need or workspace is not None else None
+    _call(q, lib.vitattn_block_fwd, q.data_ptr(), _diff_strides(q), k.data_ptr(), _diff_strides(k), v.data_ptr(),
+          _diff_strides(v), blocks.data_ptr(), _ptr(key_lens), o.data_ptr(), _diff_strides(o), _ptr(o32), _ptr(lse),
+          *sizes, _default_scale(d, scale), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+    if out is not None:
+        _written(out)
+    return o, o32, lse
+
+
+def block_bwd(q, k, v, blocks, o32, lse, dout, block=128, q_block=1, scale=None, key_lens=None, workspace=None):
+    """dq, dk and dv (bf16, like q, k and v; dk and dv summed over the heads that share
+    them) of block_fwd for the upstream gradient dout (bf16 [B,H,Nq,d])."""
+    torch = _torch()
+    sizes = _block_args(q, k, v, blocks, block, q_block, key_lens)
+    B, H, _, Nq, _, d = sizes[:6]
+    _expect(o32, "o32", torch.float32, (B, H, Nq, d), q.device, dense=True)
+    _expect(lse, "lse", torch.float32, (B, H, Nq), q.device, dense=True)
+    _as_it_is(_expect(dout, "dout", torch.bfloat16, (B, H, Nq, d), q.device), "dout")
+    dq, dk, dv = _like_layout(q, q.shape), _like_layout(k, k.shape), _like_layout(v, v.shape)
+    lib = library()
+    ws = _diff_workspace(workspace, int(lib.vitattn_block_bwd_workspace_bytes(*sizes)), q.device)
+    _call(q, lib.vitattn_block_bwd, q.data_ptr(), _diff_strides(q), k.data_ptr(), _diff_strides(k), v.data_ptr(),
+          _diff_strides(v), blocks.data_ptr(), _ptr(key_lens), o32.data_ptr(), lse.data_ptr(), dout.data_ptr(),
+          _diff_strides(dout), dq.data_ptr(), _diff_strides(dq), dk.data_ptr(), _diff_strides(dk), dv.data_ptr(),
+          _diff_strides(dv), *sizes, _default_scale(d, scale), ws.data_ptr(), ws.numel() * ws.element_size())
+    return dq, dk, dv

@@ -317,4 +317,51 @@ size_t diff_bwd_workspace_floats(int B, int H, int Nq, int Nk, int d);
 hipError_t launch_diff_fwd(const DiffArgs& a);
 hipError_t launch_diff_bwd(const DiffArgs& a);
 
+// The choice of key blocks by a cheap score; see vitattn_select.hip.
+constexpr int kSelectMax = 256;       // VITATTN_SELECT_MAX: blocks that a group may choose
+constexpr int kSparseMaxBlocks = 16384;  // VITATTN_SPARSE_MAX_BLOCKS: key blocks of a sample
+inline int means_pitch(int d) { return (d + 63) / 64 * 64; }
+struct SelectArgs {
+  const uint16_t* x;    // k [B][Hk][Nk][d] for the means, q [B][H][Nq][d] for the choice
+  Map mx;
+  const int* key_lens;  // means: [B] or null
+  int8_t* means;        // [B][Hk][nb][means_pitch(d)], dense
+  float* scales;        // [B][Hk][nb]: -1 of a block without keys
+  int* blocks;          // [B][H][groups][topk]
+  int B, H, Hk, N, d;   // N: keys, or queries
+  int nb, block, q_block, groups, topk;
+  hipStream_t stream;
+};
+hipError_t launch_means(const SelectArgs& a);
+hipError_t launch_select(const SelectArgs& a);
+
+// Attention of groups of queries over the key blocks that they chose; see
+// vitattn_sparse_fwd.hip and vitattn_sparse_bwd.hip.
+struct SparseArgs {
+  const uint16_t* q;    // [B][H][Nq][d]
+  const uint16_t* k;    // [B][Hk][Nk][d]
+  const uint16_t* v;    // [B][Hk][Nk][d]
+  const int* blocks;    // [B][H][groups][topk]
+  const int* key_lens;  // [B] or null
+  uint16_t* o;          // [B][H][Nq][d]
+  float* o32;           // [B][H][Nq][d], dense (may be null in the forward)
+  float* lse;           // [B][H][Nq], dense (may be null in the forward)
+  // backward
+  const uint16_t* dout;
+  uint16_t* dq;
+  uint16_t* dk;
+  uint16_t* dv;
+  char* work;  // workspace (the layout is each pass's own)
+  Map mq, mk, mv, mo, mg, mdq, mdk, mdv;  // mo: o (forward); mg: dout
+  int B, H, Hk, Nq, Nk, d;
+  int block, q_block, topk, groups, nb;  // nb: blocks of Nk keys
+  float scale;
+  hipStream_t stream;
+};
+size_t sparse_fwd_workspace_bytes(const SparseArgs& a);
+size_t sparse_bwd_workspace_bytes(const SparseArgs& a);
+long long sparse_bwd_items(const SparseArgs& a);  // work items of dK/dV per key head, at most
+hipError_t launch_sparse_fwd(const SparseArgs& a);
+hipError_t launch_sparse_bwd(const SparseArgs& a);
+
 }  // namespace vitattn
