@@ -22,9 +22,8 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const DropoutArgs
   const long long first = (long long)blockIdx.x * (kDropThreads * kDropPieces);
   const long long row0 = first / a.pieces;
   const uint32_t col0 = (uint32_t)(first - row0 * a.pieces);
-  constexpr int VT = Piece<T>::V, VR = Piece<R>::V;
-  Piece<T> x[kDropPieces][8 / VT];
-  Piece<R> r[kDropPieces][8 / VR];
+  Span<T, 8> x[kDropPieces];
+  Span<R, 8> r[kDropPieces];
   long long at_y[kDropPieces];
   uint32_t eighth[kDropPieces], logical[kDropPieces];
   int n[kDropPieces];  // columns of the piece that are there
@@ -41,33 +40,22 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const DropoutArgs
     const int c = (int)eighth[u] * 8;
     n[u] = min(a.D - c, 8);
     logical[u] = (uint32_t)a.ml.at(i0, i1, i2);
-    const T* px = static_cast<const T*>(a.x) + a.mx.at(i0, i1, i2) + c;
-#pragma unroll
-    for (int i = 0; i < 8 / VT; ++i) x[u][i].load(px + i * VT, min(max(n[u] - i * VT, 0), VT));
-    if constexpr (ADD) {
-      const R* pr = static_cast<const R*>(a.residual) + a.mr.at(i0, i1, i2) + c;
-#pragma unroll
-      for (int i = 0; i < 8 / VR; ++i) r[u][i].load(pr + i * VR, min(max(n[u] - i * VR, 0), VR));
-    }
+    x[u].load(static_cast<const T*>(a.x) + a.mx.at(i0, i1, i2), c, a.D);
+    if constexpr (ADD) r[u].load(static_cast<const R*>(a.residual) + a.mr.at(i0, i1, i2), c, a.D);
     at_y[u] = a.my.at(i0, i1, i2) + c;
   }
 #pragma unroll
   for (int u = 0; u < kDropPieces; ++u) {
     if (n[u] == 0) continue;
+    x[u].settle((int)eighth[u] * 8, a.D, true);
+    if constexpr (ADD) r[u].settle((int)eighth[u] * 8, a.D, true);
     const u32x4 w = drop.words(eighth[u], logical[u]);
     float y[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = drop.add(w, e, x[u][e / VT].get(e % VT), ADD ? r[u][e / VR].get(e % VR) : 0.f);
-    R* py = static_cast<R*>(a.y) + at_y[u];
-#pragma unroll
-    for (int i = 0; i < 8 / VR; ++i) {
-      float part[VR];
-#pragma unroll
-      for (int e = 0; e < VR; ++e) part[e] = y[i * VR + e];
-      Piece<R> o;
-      o.set(part);
-      o.store(py + i * VR, min(max(n[u] - i * VR, 0), VR));
-    }
+    for (int e = 0; e < 8; ++e) y[e] = drop.add(w, e, x[u].get(e), ADD ? r[u].get(e) : 0.f);
+    Span<R, 8> o;
+    o.set(y);
+    o.store(static_cast<R*>(a.y) + at_y[u], n[u]);
   }
 }
 

@@ -103,9 +103,10 @@ __global__ __launch_bounds__(kThreads) void rms_fwd_kernel(const RmsArgs a) {
     const R* res = static_cast<const R*>(a.residual) + (a.residual ? i.in(a.mr) : 0);
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
-      const int c = (lane + k * L) * V, n = on ? columns_of<V>(a.D, c) : 0;
-      row.x[k].load(x + c, n);
-      row.h[k].load(res + c, a.residual ? n : 0);
+      const int c = (lane + k * L) * V;
+      row.x[k].load(x, c, a.D);
+      if (a.residual) row.h[k].load(res, c, a.D);
+      else row.h[k].clear();
     }
   };
   Row row[U], next;
@@ -130,6 +131,8 @@ __global__ __launch_bounds__(kThreads) void rms_fwd_kernel(const RmsArgs a) {
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
         float v[V];
+        row[u].x[i].settle((lane + i * L) * V, a.D, on);
+        if (a.residual) row[u].h[i].settle((lane + i * L) * V, a.D, on);
         if (a.drop_on) {
           const PieceMask<V> mask(drop, (lane + i * L) * V, (uint32_t)logical);
 #pragma unroll
@@ -221,7 +224,7 @@ hipError_t go(const RmsArgs& a, int groups) {
 template <typename T, typename R>
 hipError_t fwd_t(RmsArgs a) {
   constexpr int V = Piece<T>::V;
-  RowShape s = row_shape(a.D, V, true);
+  RowShape s = rms_shape(a.D, V, true, sizeof(R) > sizeof(T));
   if (a.group && s.lanes <= 64) {  // (divides 64)
     const int gl = a.group / V;
     s.lanes = (s.lanes + gl - 1) / gl * gl;
@@ -230,10 +233,10 @@ hipError_t fwd_t(RmsArgs a) {
   const int n = (int)(((long long)a.rows + rows_of(s) - 1) / rows_of(s));
   const bool block = s.lanes > 64;
   switch (s.np) {
-    case 1: return go<T, R, 1, false>(a, n);
+    case 1: return block ? go<T, R, 1, true>(a, n) : go<T, R, 1, false>(a, n);
     case 2: return block ? go<T, R, 2, true>(a, n) : go<T, R, 2, false>(a, n);
-    case 3: return block ? go<T, R, 3, true>(a, n) : go<T, R, 3, false>(a, n);
-    case 4: return block ? go<T, R, 4, true>(a, n) : go<T, R, 4, false>(a, n);
+    case 3: return block || sizeof(R) > sizeof(T) ? go<T, R, 3, true>(a, n) : go<T, R, 3, sizeof(R) != sizeof(T)>(a, n);
+    case 4: return block || sizeof(R) > sizeof(T) ? go<T, R, 4, true>(a, n) : go<T, R, 4, sizeof(R) != sizeof(T)>(a, n);
     case 5:
     case 6: return go<T, R, 6, true>(a, n);
     default: return go<T, R, 8, true>(a, n);

@@ -57,10 +57,11 @@ __global__ __launch_bounds__(kThreads) void rms_bwd_kernel(const RmsArgs a) {
     const T* g = static_cast<const T*>(a.dy) + i.in(a.mdy);
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
-      const int c = (lane + k * L) * V, n = on ? columns_of<V>(a.D, c) : 0;
-      row.h[k].load(h + c, n);
-      row.g[k].load(g + c, n);
-      row.dh[k].load(dh + c, a.dh ? n : 0);
+      const int c = (lane + k * L) * V;
+      row.h[k].load(h, c, a.D);
+      row.g[k].load(g, c, a.D);
+      if (a.dh) row.dh[k].load(dh, c, a.D);
+      else row.dh[k].clear();
     }
     row.rstd = on ? a.rstd[i.in(a.ml)] : 0.f;
   };
@@ -77,6 +78,13 @@ __global__ __launch_bounds__(kThreads) void rms_bwd_kernel(const RmsArgs a) {
     }
     const bool on = at.row >= 0 && r0 < a.rows;
     const float rstd = row.rstd;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int c = (lane + i * L) * V;
+      row.h[i].settle(c, a.D, on);
+      row.g[i].settle(c, a.D, on);
+      if (a.dh) row.dh[i].settle(c, a.D, on);
+    }
     // lanes past the row hold dy = 0 and add nothing to any sum
     float s = 0.f;
 #pragma unroll
@@ -186,7 +194,7 @@ constexpr int resident(int np, int v, bool block) {
 
 int rows_of(const RowShape& s) { return s.lanes > 64 ? 1 : 64 / s.lanes * (kThreads / 64); }
 RowShape shape(int D, int V) {
-  RowShape s = row_shape(D, V, false);
+  RowShape s = rms_shape(D, V, false, true);
   if (s.np == 5) s.np = 6;
   return s;
 }
@@ -201,10 +209,10 @@ template <typename T, typename R>
 hipError_t go_shape(const RmsArgs& a, const RowShape& s, int n) {
   const bool block = s.lanes > 64;
   switch (s.np) {
-    case 1: return go<T, R, 1, false>(a, n);
+    case 1: return block ? go<T, R, 1, true>(a, n) : go<T, R, 1, false>(a, n);
     case 2: return block ? go<T, R, 2, true>(a, n) : go<T, R, 2, false>(a, n);
-    case 3: return block ? go<T, R, 3, true>(a, n) : go<T, R, 3, false>(a, n);
-    case 4: return block ? go<T, R, 4, true>(a, n) : go<T, R, 4, false>(a, n);
+    case 3: return go<T, R, 3, true>(a, n);
+    case 4: return go<T, R, 4, true>(a, n);
     case 6: return go<T, R, 6, true>(a, n);
     default: return go<T, R, 8, true>(a, n);
   }

@@ -67,6 +67,76 @@ struct Piece {
   }
 };
 
+// V elements of type R, in as many 16-byte pieces as they take. Every lane loads whole
+// pieces, at the row's end the 16 bytes that end with it (lanes past the row too), and
+// they are put in place when all loads are on their way: read element by element, a
+// last piece waits for memory before the next load.
+template <typename R, int V>
+struct Span {
+  static constexpr int P = Piece<R>::V, K = V / P;
+  static_assert(V % P == 0, "whole pieces");
+  Piece<R> p[K];
+  __device__ __forceinline__ float get(int e) const { return p[e / P].get(e % P); }
+  __device__ __forceinline__ void set(const float (&x)[V]) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float part[P];
+#pragma unroll
+      for (int e = 0; e < P; ++e) part[e] = x[k * P + e];
+      p[k].set(part);
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int k = 0; k < K; ++k) p[k].raw = u32x4{0, 0, 0, 0};
+  }
+  // columns c .. c + V - 1 of a row of D, those past it left open until settled
+  __device__ __forceinline__ void load(const R* row, int c, int D) {
+    if (D >= P) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) p[k].raw = *reinterpret_cast<const u32x4_any*>(row + min(c + k * P, D - P));
+      return;
+    }
+    clear();
+    if (c == 0)  // (a row of less than one piece)
+      for (int e = D - 1; e >= 0; --e) {
+        u32x4& w = p[0].raw;
+        if constexpr (sizeof(R) == 4) {
+          w = u32x4{reinterpret_cast<const uint32_t*>(row)[e], w[0], w[1], w[2]};
+        } else {
+          const uint32_t x = reinterpret_cast<const uint16_t*>(row)[e];
+          w = u32x4{w[0] << 16 | x, w[1] << 16 | w[0] >> 16, w[2] << 16 | w[1] >> 16, w[3] << 16 | w[2] >> 16};
+        }
+      }
+  }
+  // puts a row's last piece in place, and zeros past it (all of it unless `on`)
+  __device__ __forceinline__ void settle(int c, int D, bool on) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int m = on ? D - c - k * P : 0;
+      if (!__any(m < P)) continue;
+      if (m <= 0) {
+        p[k].raw = u32x4{0, 0, 0, 0};
+      } else if (m < P && D >= P) {
+        const int by = (P - m) * 8 * (int)sizeof(R);  // bits, below 128
+        uint64_t lo = (uint64_t)p[k].raw[1] << 32 | p[k].raw[0], hi = (uint64_t)p[k].raw[3] << 32 | p[k].raw[2];
+        if (by >= 64) {
+          lo = hi >> (by - 64);
+          hi = 0;
+        } else {
+          lo = lo >> by | hi << (64 - by);
+          hi >>= by;
+        }
+        p[k].raw = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+      }
+    }
+  }
+  __device__ __forceinline__ void store(R* x, int n) const {
+#pragma unroll
+    for (int k = 0; k < K; ++k) p[k].store(x + k * P, min(max(n - k * P, 0), P));
+  }
+};
+
 constexpr int kRowThreads = 256;  // of a workgroup of the norms
 
 // V weights from element c on (n of them real, zeros behind), fp32 or T

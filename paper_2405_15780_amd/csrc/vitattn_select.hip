@@ -15,9 +15,10 @@
 // The means are bound by reading the keys. The choice takes its scores from the matrix
 // cores' 8-bit products (16 groups by 16 blocks by 64 columns an operation), 16 groups
 // of one head per workgroup, and keeps them in LDS: 2,048 a group, with more blocks the
-// best so far stay and compete with the next ones. A wave then takes a group at a time:
-// its scores in registers as whole numbers that order alike, the topk-th largest found
-// bit by bit by counting (ballots), and the chosen ones written in order.
+// best so far stay and compete with the next ones. A wave then takes two groups at a time,
+// their scores in registers as whole numbers that order alike. The topk-th largest of the
+// lanes' highest, found bit by bit by counting (ballots), is reached by topk scores and few
+// more; these go to a lane each, where the same search finds the threshold.
 #include "vitattn_common.h"
 #include "vitattn_launch.h"
 
@@ -93,11 +94,37 @@ __global__ __launch_bounds__(256) void means_kernel(const SelectArgs a) {
 // order-preserving whole numbers of fp32 values; 0 stands for none
 __device__ __forceinline__ uint32_t ordered(float x) {
   const uint32_t u = __float_as_uint(x);
-  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+  return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
 }
 
-__device__ __forceinline__ float unordered(uint32_t u) {
-  return __uint_as_float((u & 0x80000000u) ? u ^ 0x80000000u : ~u);
+
+// the value of a lane in another place: of the quad, half a row of 16 or a row mirrored,
+// the neighbouring row, the other half of the wave
+template <int CTRL>
+__device__ __forceinline__ uint32_t lane_swap(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, CTRL, 0xf, 0xf, false);
+}
+__device__ __forceinline__ uint32_t row_swap(uint32_t x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return (threadIdx.x & 16) ? r[0] : r[1];
+}
+__device__ __forceinline__ uint32_t half_swap(uint32_t x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return (threadIdx.x & 32) ? r[0] : r[1];
+}
+// the largest over the wave, the same (scalar) in all
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  x = max(x, lane_swap<0xB1>(x));
+  x = max(x, lane_swap<0x4E>(x));
+  x = max(x, lane_swap<0x141>(x));
+  x = max(x, lane_swap<0x140>(x));
+  x = max(x, row_swap(x));
+  x = max(x, half_swap(x));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+// of this mask's lanes, those before the lane
+__device__ __forceinline__ int lanes_before(uint64_t m) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
 }
 
 constexpr int kTile = 16;  // groups of a workgroup
@@ -105,21 +132,44 @@ constexpr int kTile = 16;  // groups of a workgroup
 // NPL scores of a group per lane, KT 64-column steps of d, NW waves; MORE: blocks come in
 // several turns, the first kSelectMax places hold the best of those before.
 template <int NPL, int KT, int NW, bool MORE>
-__global__ __launch_bounds__(64 * NW) void select_kernel(const SelectArgs a, int tiles) {
+__global__ __launch_bounds__(64 * NW) void select_kernel(const SelectArgs a, int per_key) {
   constexpr int CH = KT == 1 ? 8 : KT == 2 ? 16 : 32;  // lanes of 8 columns
   constexpr int PITCH = 64 * KT;                       // means_pitch(d)
   constexpr int SP = 64 * NPL + 4;                     // a row of scores: rows four apart fall on other banks
   constexpr int FIRST = MORE ? kSelectMax : 0;
   __shared__ __attribute__((aligned(16))) int8_t qs[kTile][PITCH + 16];
-  __shared__ float sc[kTile][SP];
+  __shared__ uint32_t sc[kTile][SP];  // scores as whole numbers in their order, 0: none
+  __shared__ uint32_t best[NW][2][2][68];  // a wave's candidates: scores and places (behind 64: dropped)
   __shared__ int ids[MORE ? kTile : 1][MORE ? kSelectMax : 1];
-  debug_poison_lds(qs, sc, ids);
-  const int bh = blockIdx.x / tiles, g0 = (blockIdx.x - bh * tiles) * kTile;
-  const int b = bh / a.H, head = bh - b * a.H, hk = head / (a.H / a.Hk);
+  debug_poison_lds(qs, sc, best, ids);
+  const int b = blockIdx.z, head = blockIdx.y, bh = b * a.H + head, hk = head / per_key, g0 = blockIdx.x * kTile;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 
+  const int8_t* const means = a.means + ((long long)b * a.Hk + hk) * a.nb * PITCH;
+  const float* const scales = a.scales + ((long long)b * a.Hk + hk) * a.nb;
+  constexpr int ROOM = 64 * NPL - FIRST;  // blocks of a turn
+  // Batches of four times 16 blocks per wave, the next one on its way while one is
+  // multiplied, the first while the queries are.
+  constexpr int TB = 4;
+  struct Batch {
+    i32x4 m[TB][KT];
+    float s[TB];
+  };
+  auto load = [&](Batch& x, int j0, int j, int n) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < TB; ++u) {
+      const int jj = min(j + u * NW * 16 + (lane & 15), n - 1);  // (those past the last are not kept)
+      x.s[u] = scales[j0 + jj];
+#pragma unroll
+      for (int k = 0; k < KT; ++k)
+        x.m[u][k] = *reinterpret_cast<const i32x4*>(means + (long long)(j0 + jj) * PITCH + 64 * k + 16 * (lane >> 4));
+    }
+  };
+  Batch next;
+  load(next, 0, wave * 16, min(a.nb, ROOM));
+
   // the groups' queries: a wave per group, or 64 / CH groups of one query each
-  const uint16_t* const q = a.x + a.mx.head(bh, a.H);
+  const uint16_t* const q = a.x + b * a.mx.sb + head * a.mx.sh;
   const int c = lane % CH, slot = lane / CH;
   const bool single = a.q_block == 1;
   const int step = single ? 64 / CH : 1;
@@ -155,110 +205,150 @@ __global__ __launch_bounds__(64 * NW) void select_kernel(const SelectArgs a, int
 #pragma unroll
   for (int k = 0; k < KT; ++k) qf[k] = *reinterpret_cast<const i32x4*>(&qs[lane & 15][64 * k + 16 * (lane >> 4)]);
 
-  const int8_t* const means = a.means + ((long long)b * a.Hk + hk) * a.nb * PITCH;
-  const float* const scales = a.scales + ((long long)b * a.Hk + hk) * a.nb;
-  constexpr int ROOM = 64 * NPL - FIRST;  // blocks of a turn
   if constexpr (MORE)
-    for (int i = threadIdx.x; i < kTile * kSelectMax; i += 64 * NW) sc[i / kSelectMax][i % kSelectMax] = -INFINITY;
+    for (int i = threadIdx.x; i < kTile * kSelectMax; i += 64 * NW) sc[i / kSelectMax][i % kSelectMax] = 0;
   for (int j0 = 0; j0 < a.nb; j0 += ROOM) {
     const int n = min(a.nb - j0, ROOM);  // of this turn
-    // scores: a wave takes 16 blocks at a time, two of them in flight
-    for (int j = wave * 16; j < n; j += NW * 32) {
-      i32x4 m[2][KT];
-      float s[2];
+    for (int j = wave * 16; j < n; j += NW * 16 * TB) {
+      const Batch x = next;
+      if (j + NW * 16 * TB < n) load(next, j0, j + NW * 16 * TB, n);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int jj = j + u * NW * 16 + (lane & 15);
-        const bool there = jj < n;
-        s[u] = there ? scales[j0 + jj] : -1.f;
-#pragma unroll
-        for (int k = 0; k < KT; ++k)
-          m[u][k] = there ? *reinterpret_cast<const i32x4*>(means + (long long)(j0 + jj) * PITCH + 64 * k + 16 * (lane >> 4))
-                          : i32x4{0, 0, 0, 0};
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < TB; ++u) {
         i32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-        for (int k = 0; k < KT; ++k) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(qf[k], m[u][k], acc, 0, 0, 0);
-        const int jj = j + u * NW * 16 + (lane & 15);
-        if (jj < n)
+        for (int k = 0; k < KT; ++k) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(qf[k], x.m[u][k], acc, 0, 0, 0);
+        const int j1 = j + u * NW * 16, jj = j1 + (lane & 15);
+        if (MORE && j1 >= ROOM) break;
+        const uint32_t there = x.s[u] < 0.f || jj >= n ? 0u : ~0u;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) sc[4 * (lane >> 4) + r][FIRST + jj] = s[u] < 0.f ? -INFINITY : (float)acc[r] * s[u];
+        for (int r = 0; r < 4; ++r) sc[4 * (lane >> 4) + r][FIRST + jj] = ordered((float)acc[r] * x.s[u]) & there;
       }
     }
+    for (int r = wave; r < kTile && n < ROOM; r += NW)  // no blocks behind the last
+      for (int i = n + lane; i < ROOM; i += 64) sc[r][FIRST + i] = 0;
+    if (j0 + ROOM < a.nb) load(next, j0 + ROOM, wave * 16, min(a.nb - j0 - ROOM, ROOM));
     __syncthreads();
     const bool last = j0 + ROOM >= a.nb;
-    for (int t = wave; t < kTile; t += NW) {
-      const int g = g0 + t;
-      if (g >= a.groups) break;
-      uint32_t key[NPL];
+    // two groups at a time, whose counts overlap
+    for (int t = 2 * wave; t < kTile; t += 2 * NW) {
+      if (g0 + t >= a.groups) break;
+      uint32_t key[2][NPL], most[2] = {0, 0}, T[2], hi[2];
 #pragma unroll
-      for (int i = 0; i < NPL; ++i) {
-        const int p = 64 * i + lane;
-        const float x = p < FIRST + n ? sc[t][p] : -INFINITY;
-        key[i] = x == -INFINITY ? 0u : ordered(x);
-      }
-      auto at_least = [&](uint32_t x) __attribute__((always_inline)) {
-        int n_ = 0;
-#pragma unroll
-        for (int i = 0; i < NPL; ++i) n_ += __popcll(__ballot(key[i] >= x));
-        return n_;
-      };
-      // the largest T that at least topk scores reach (1: fewer are there)
-      uint32_t T = 0, hi = 0, lo = 0xffffffffu;
-      if (at_least(1u) > a.topk) {
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int i = 0; i < NPL; ++i) {
-          hi = max(hi, key[i]);
-          lo = min(lo, key[i]);
+          const int p = 64 * i + lane;
+          key[u][i] = sc[t + u][p] & (g0 + t + u < a.groups ? ~0u : 0u);
+          most[u] = max(most[u], key[u][i]);
         }
 #pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) {
-          hi = max(hi, (uint32_t)__shfl_xor((int)hi, d, 64));
-          lo = min(lo, (uint32_t)__shfl_xor((int)lo, d, 64));
-        }
-        hi = __builtin_amdgcn_readfirstlane(hi);
-        lo = __builtin_amdgcn_readfirstlane(lo);
-        // bits above the first in which they differ are common to all
-        const uint32_t differ = hi ^ lo;
-        uint32_t bit = differ ? 0x80000000u >> __builtin_clz(differ) : 0u;
-        T = differ ? hi & ~(2u * bit - 1u) : hi;
-        for (; bit != 0; bit >>= 1) {
-          const int reach = at_least(T | bit);
-          if (reach >= a.topk) T |= bit;
-          if (reach == a.topk) break;
-        }
-      }
-      if (T == 0) T = 1;
-      // those above T, and as many of T's own as are left, in order
-      int ties = T == 0xffffffffu ? a.topk : a.topk - at_least(T + 1), out = 0;
-      int* const to = a.blocks + ((long long)bh * a.groups + g) * a.topk;
+      for (int u = 0; u < 2; ++u) hi[u] = wave_max(most[u]);
+      auto at_least = [&](int u, uint32_t x) __attribute__((always_inline)) {
+        int n_ = 0;
 #pragma unroll
-      for (int i = 0; i < NPL; ++i) {
-        const uint64_t above = __ballot(key[i] > T), equal = __ballot(key[i] == T);
-        if ((above | equal) == 0) continue;
-        const uint64_t before = (1ULL << lane) - 1;
-        const bool mine = key[i] > T || (key[i] == T && (int)__popcll(equal & before) < ties);
-        const uint64_t taken = __ballot(mine);
-        if (mine) {
-          const int p = 64 * i + lane, at = out + __popcll(taken & before);
-          int id = j0 + p - FIRST;
-          if (MORE && p < FIRST) id = ids[t][p];
-          if (last) {
-            to[at] = id;
-          } else if constexpr (MORE) {  // (at <= p: read before, or in registers)
-            ids[t][at] = id;
-            sc[t][at] = unordered(key[i]);
+        for (int i = 0; i < NPL; ++i) n_ += (int)__popcll(__ballot(key[u][i] >= x));
+        return n_;
+      };
+      // The largest T >= from that at least topk of the numbers counted reach, or the first
+      // that topk to `enough` do: those between it and the highest share its leading bits.
+      auto search = [&](auto count, const uint32_t (&from)[2], int enough) __attribute__((always_inline)) {
+        uint32_t bit[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const uint32_t differ = hi[u] ^ from[u];
+          bit[u] = differ ? 0x80000000u >> __builtin_clz(differ) : 0u;
+          T[u] = differ ? hi[u] & ~(2u * bit[u] - 1u) : hi[u];
+          while (bit[u] != 0 && (T[u] | bit[u]) <= from[u]) {
+            T[u] |= bit[u];
+            bit[u] >>= 1;
           }
         }
-        ties -= __popcll(taken & equal);
-        out += __popcll(taken);
+        while ((bit[0] | bit[1]) != 0) {
+          int reach[2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) reach[u] = count(u, T[u] | bit[u]);
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            T[u] = reach[u] >= a.topk ? T[u] | bit[u] : T[u];
+            bit[u] = (unsigned)(reach[u] - a.topk) <= (unsigned)(enough - a.topk) ? 0 : bit[u] >> 1;
+          }
+        }
+      };
+      // What topk of the lanes' highest reach, at least topk scores do, and seldom many
+      // more: these are the candidates, at most one a lane if all goes well.
+      uint32_t from[2] = {0, 0};
+      int found[2] = {65, 65};
+      if (a.topk <= 64) {
+        search([&](int u, uint32_t x) __attribute__((always_inline)) { return (int)__popcll(__ballot(most[u] >= x)); }, from, a.topk + a.topk / 4);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          from[u] = max(T[u], 1u);
+          found[u] = 0;
+#pragma unroll
+          for (int i = 0; i < NPL; ++i) {
+            const bool mine = key[u][i] >= from[u];
+            const uint64_t taken = __ballot(mine);
+            int at = min(found[u] + lanes_before(taken), 64);
+            asm("" : "+v"(at));  // (formed by every lane, not behind a branch)
+            at = mine ? at : 64;
+            best[wave][u][0][at] = key[u][i];
+            best[wave][u][1][at] = 64 * i + lane;
+            found[u] += (int)__popcll(taken);
+          }
+        }
       }
-      if (last) {
-        for (int i = out + lane; i < a.topk; i += 64) to[i] = -1;
-      } else if constexpr (MORE) {
-        for (int i = out + lane; i < FIRST; i += 64) sc[t][i] = -INFINITY;
+      const bool few = found[0] <= 64 && found[1] <= 64;
+      uint32_t cand[2] = {0, 0};
+      if (few) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) cand[u] = lane < found[u] ? best[wave][u][0][lane] : 0u;
+        search([&](int u, uint32_t x) __attribute__((always_inline)) { return (int)__popcll(__ballot(cand[u] >= x)); }, from, a.topk);
+      } else {
+        search(at_least, from, a.topk);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int g = g0 + t + u;
+        if (g >= a.groups) break;
+        const uint32_t least = max(T[u], 1u);  // (0: fewer are there)
+        int* const to = a.blocks + ((long long)bh * a.groups + g) * a.topk;
+        int out = 0;
+        // writes the places p of the lanes with `mine`
+        auto put = [&](bool mine, int p, uint32_t score) __attribute__((always_inline)) {
+          const uint64_t taken = __ballot(mine);
+          if (mine) {
+            const int at = out + lanes_before(taken);
+            int id = j0 + p - FIRST;
+            if (MORE && p < FIRST) id = ids[t + u][p];
+            if (last) {
+              to[at] = id;
+            } else if constexpr (MORE) {  // (at <= p: read before, or in registers)
+              ids[t + u][at] = id;
+              sc[t + u][at] = score;
+            }
+          }
+          out += (int)__popcll(taken);
+        };
+        // those above the least, and as many of its own as are left, in order
+        if (few) {
+          const uint64_t above = __ballot(cand[u] > least), equal = __ballot(cand[u] == least);
+          const bool mine = cand[u] > least || (cand[u] == least && lanes_before(equal) < a.topk - (int)__popcll(above));
+          put(mine, lane < found[u] ? (int)best[wave][u][1][lane] : 0, cand[u]);
+        } else {
+          int ties = a.topk - (least == 0xffffffffu ? 0 : at_least(u, least + 1));
+#pragma unroll
+          for (int i = 0; i < NPL; ++i) {
+            const uint64_t equal = __ballot(key[u][i] == least);
+            const bool mine = key[u][i] > least || (key[u][i] == least && lanes_before(equal) < ties);
+            ties -= (int)__popcll(equal);
+            put(mine, 64 * i + lane, key[u][i]);
+          }
+        }
+        if (last) {
+          for (int i = out + lane; i < a.topk; i += 64) to[i] = -1;
+        } else if constexpr (MORE) {
+          for (int i = out + lane; i < FIRST; i += 64) sc[t + u][i] = 0;
+        }
       }
     }
     __syncthreads();
@@ -267,13 +357,15 @@ __global__ __launch_bounds__(64 * NW) void select_kernel(const SelectArgs a, int
 
 template <int KT>
 hipError_t go(const SelectArgs& a) {
-  const int tiles = (a.groups + kTile - 1) / kTile;
-  const unsigned grid = (unsigned)(a.B * a.H) * tiles;
-  if (a.nb <= 256) select_kernel<4, KT, 4, false><<<grid, 256, 0, a.stream>>>(a, tiles);
-  else if (a.nb <= 512) select_kernel<8, KT, 4, false><<<grid, 256, 0, a.stream>>>(a, tiles);
-  else if (a.nb <= 1024) select_kernel<16, KT, 4, false><<<grid, 256, 0, a.stream>>>(a, tiles);
-  else if (a.nb <= 2048) select_kernel<32, KT, 8, false><<<grid, 512, 0, a.stream>>>(a, tiles);
-  else select_kernel<32, KT, 8, true><<<grid, 512, 0, a.stream>>>(a, tiles);
+  const dim3 grid((a.groups + kTile - 1) / kTile, a.H, a.B);
+  const int per_key = a.H / a.Hk;
+  // (a few queries: more waves read the means at once)
+  if (a.groups <= kTile && a.nb > 256 && a.nb <= 1024) select_kernel<16, KT, 16, false><<<grid, 1024, 0, a.stream>>>(a, per_key);
+  else if (a.nb <= 256) select_kernel<4, KT, 4, false><<<grid, 256, 0, a.stream>>>(a, per_key);
+  else if (a.nb <= 512) select_kernel<8, KT, 4, false><<<grid, 256, 0, a.stream>>>(a, per_key);
+  else if (a.nb <= 1024) select_kernel<16, KT, 4, false><<<grid, 256, 0, a.stream>>>(a, per_key);
+  else if (a.nb <= 2048) select_kernel<32, KT, 8, false><<<grid, 512, 0, a.stream>>>(a, per_key);
+  else select_kernel<32, KT, 8, true><<<grid, 512, 0, a.stream>>>(a, per_key);
   return hipGetLastError();
 }
 

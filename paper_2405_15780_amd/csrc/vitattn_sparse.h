@@ -9,7 +9,7 @@ namespace vitattn {
 // chosen blocks that are listed at a time: all that one group may choose, or (MASKED)
 // some of a tile's union
 constexpr int kListAll = 1024;  // VITATTN_SPARSE_MAX_TOPK
-constexpr int kListUnion = 512;
+constexpr int kListUnion = 128;
 
 // keys of sample b: the first key_lens[b] of Nk, brought into 0 .. Nk
 __device__ __forceinline__ int sparse_keys(const SparseArgs& a, int b) {
@@ -38,12 +38,13 @@ struct Chosen {
 // The blocks that any row of a query tile chose, each once and in ascending order
 // whatever the order they were given in, and (MASKED) the rows that chose each. A bit
 // per key block; numbers outside the sample's blocks set none.
+constexpr int kNone = 0xffff;
 template <bool MASKED>
 struct BlockList {
   static constexpr int kCap = MASKED ? kListUnion : kListAll;
   uint32_t bits[kSparseMaxBlocks / 32];
   uint16_t before[kSparseMaxBlocks / 32];  // blocks listed before a word's
-  int key0[kCap + 8];                  // first keys, then Nk: past the last key
+  uint16_t id[kCap + 8];               // then kNone
   uint64_t masks[MASKED ? kCap + 8 : 1];
   int total;
 
@@ -82,28 +83,33 @@ struct BlockList {
     __syncthreads();
     return __builtin_amdgcn_readfirstlane(total);
   }
-  // Lists the blocks r0 .. r0 + n - 1 (n <= kCap) of those; Nk: the sample's keys.
+  // Lists the blocks r0 .. r0 + n - 1 (n <= kCap) of those.
   template <int NT>
-  __device__ __forceinline__ void fill(const SparseArgs& a, const Chosen& c, int real, int Nk, uint64_t filter, int r0, int n) {
+  __device__ __forceinline__ void fill(const SparseArgs& a, const Chosen& c, int real, uint64_t filter, int r0, int n) {
     const int words = (a.nb + 31) >> 5;
     for (int i = threadIdx.x; i < words; i += NT) {
       uint32_t m = bits[i];
       for (int r = before[i] - r0; m != 0 && r < n; ++r, m &= m - 1)
-        if (r >= 0) key0[r] = (32 * i + __builtin_ctz(m)) * a.block;
+        if (r >= 0) id[r] = (uint16_t)(32 * i + __builtin_ctz(m));
     }
-    if (threadIdx.x < 8) key0[n + threadIdx.x] = Nk;
+    if (threadIdx.x < 8) id[n + threadIdx.x] = kNone;
     if constexpr (MASKED) {
       for (int i = threadIdx.x; i < n + 8; i += NT) masks[i] = 0;
       __syncthreads();
       for (int e = threadIdx.x; e < c.n; e += NT) {
-        const int id = c.at[e];
-        if ((unsigned)id >= (unsigned)real) continue;
+        const int x = c.at[e];
+        if ((unsigned)x >= (unsigned)real) continue;
         const uint64_t rows = c.rows_of(a, e) & filter;
-        const int r = before[id >> 5] + __popc(bits[id >> 5] & ((1u << (id & 31)) - 1)) - r0;
+        const int r = before[x >> 5] + __popc(bits[x >> 5] & ((1u << (x & 31)) - 1)) - r0;
         if (rows != 0 && r >= 0 && r < n) atomicOr(reinterpret_cast<unsigned long long*>(&masks[r]), (unsigned long long)rows);
       }
     }
     __syncthreads();
+  }
+  // the first key of a listed block from its entry as it was read (Nk behind the last)
+  __device__ __forceinline__ static int key_of(uint32_t entry, int block, int Nk) {
+    const int x = __builtin_amdgcn_readfirstlane((int)entry);
+    return x == kNone ? Nk : x * block;
   }
 };
 

@@ -111,7 +111,8 @@ int vitattn_block_select(const void* q, vitattn_strides sq, const void* means, c
     if (!aligned16(q) || !aligned16(means) || !aligned_to(scales, 4) || !aligned_to(blocks, 4)) return VITATTN_E_INVAL;
     if (check_map(sq, B, H, Nq, d, 2, false)) return VITATTN_E_INVAL;
     const int groups = (Nq - 1) / q_block + 1;
-    if ((double)B * H * (groups / 16 + 1) * 512. >= kMaxWorkItems) return VITATTN_E_INVAL;
+    // a launch's second and third dimensions have 16 bits, the first 32 of work-items
+    if (B > 65535 || H > 65535 || (groups / 16 + 1.) * 1024. >= kMaxWorkItems) return VITATTN_E_INVAL;
     const size_t n = (size_t)B * Hk * nb;
     const Memory used[] = {dense_memory(blocks, (size_t)B * H * groups * topk * 4), strided_memory(q, sq, B, H, Nq, d, 2),
                            dense_memory(means, n * vitattn::means_pitch(d)), dense_memory(scales, n * 4)};

@@ -35,7 +35,7 @@ constexpr int kTileRows = 64;   // of a query tile
 constexpr int kMapTiles = 64;   // query tiles of a map word
 constexpr int kMapRows = kTileRows * kMapTiles;
 constexpr int kRowBlock = 64;   // query rows of a row-pass workgroup
-constexpr int kRunList = 256;   // query tiles that an item lists at a time
+constexpr int kRunList = 128;   // query tiles that an item lists at a time
 constexpr int kStat = 64;       // floats per 32 queries: -D, then LSE log2(e)
 
 struct Plan {  // sizes of the backward's workspace
@@ -51,9 +51,9 @@ Plan plan_of(const SparseArgs& a) {
   const long long groups = a.q_block >= kTileRows ? (a.q_block % kTileRows == 0 ? 1 : 2)
                                                   : min((long long)kTileRows / a.q_block + 2, (long long)min(a.Nq, kTileRows));
   const long long pairs = (long long)(a.H / a.Hk) * p.tiles * min(groups * a.topk, (long long)a.nb);
-  // runs of 64 tiles, longer ones where the shares of as many items would outgrow four
-  // times the keys
-  p.run = (int)max(64LL, min(4096LL, (pairs + 4LL * a.nb - 1) / (4LL * a.nb)));
+  // runs of 64 tiles, of 32 where there are few blocks to fill the card with, and longer
+  // ones where the shares of as many items would outgrow eight times the keys
+  p.run = (int)max(a.nb < 256 ? 32LL : 64LL, min(4096LL, (pairs + 8LL * a.nb - 1) / (8LL * a.nb)));
   p.items = a.nb + pairs / p.run;  // sum over the blocks of max(1, ceil(count / run))
   return p;
 }
@@ -64,7 +64,7 @@ struct Work {
   uint64_t* map;     // [BH][words][nb]
   int* counts;       // [B Hk][nb]
   int* first;        // [B Hk][nb + 1]: a block's first item; the number of items
-  int* items;        // [B Hk][items]: an item's block
+  int4* items;       // [B Hk][items]: an item's block, its run, the block's runs and query tiles
   float* shares;     // [B Hk][items][2][block][d]
   size_t bytes;
 };
@@ -83,7 +83,7 @@ Work work_of(const SparseArgs& a, const Plan& p) {
   w.map = reinterpret_cast<uint64_t*>(take(bh * p.words * a.nb * 8));
   w.counts = reinterpret_cast<int*>(take(bhk * a.nb * 4));
   w.first = reinterpret_cast<int*>(take(bhk * (a.nb + 1) * 4));
-  w.items = reinterpret_cast<int*>(take(bhk * p.items * 4));
+  w.items = reinterpret_cast<int4*>(take(bhk * p.items * sizeof(int4)));
   w.shares = reinterpret_cast<float*>(take(p.items > a.nb ? bhk * p.items * 2 * a.block * a.d * 4 : 0));
   w.bytes = n;
   return w;
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(1024) void sparse_map_kernel(const SparseArgs a, ui
 
 // Items of each key block, max(1, ceil(count / run)), and their places: a workgroup per
 // key head.
-__global__ __launch_bounds__(1024) void sparse_plan_kernel(const SparseArgs a, const int* __restrict__ counts, int* __restrict__ first, int* __restrict__ items, int run,
+__global__ __launch_bounds__(1024) void sparse_plan_kernel(const SparseArgs a, const int* __restrict__ counts, int* __restrict__ first, int4* __restrict__ items, int run,
                                                            long long n_items) {
   __shared__ int sums[16];
   debug_poison_lds(sums);
@@ -193,7 +193,7 @@ __global__ __launch_bounds__(1024) void sparse_plan_kernel(const SparseArgs a, c
   for (int j = j0; j < min(j0 + per, a.nb); ++j) {
     first[j] = at;
     const int m = of(j);
-    for (int i = 0; i < m; ++i) items[at + i] = j;
+    for (int i = 0; i < m; ++i) items[at + i] = make_int4(j, i, m, counts[j]);
     at += m;
   }
   if (threadIdx.x == 1023) first[a.nb] = at;
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(1024) void sparse_plan_kernel(const SparseArgs a, c
 // dK += dS(j)^T Q(j). Blocks of 32 queries arrive in a ring of four slots, three steps
 // ahead. Steps past the last read zeros: P is 1 there, and dO and Q are zero.
 template <int D, int KS, int NW, bool MASKED>
-__global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void sparse_dkdv_kernel(const SparseArgs a, const Work w, int words, int run, long long n_items, int subs, float c) {
+__global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void sparse_dkdv_kernel(const SparseArgs a, const Work w, int words, int run, int n_items, int subs, float c) {
   constexpr int BQ = 32, RING = 4, PF = 3;
   constexpr int NC = (KS + 1) / 2;  // 32-column blocks of d that may hold data
   constexpr int T = BQ * D * 2;
@@ -223,24 +223,28 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void sparse_dkdv_kernel(c
   __shared__ __attribute__((aligned(16))) float sbuf1[kStat];
   __shared__ __attribute__((aligned(16))) float sbuf2[kStat];
   __shared__ __attribute__((aligned(16))) float sbuf3[kStat];
-  __shared__ int list[kRunList + 4];  // query tiles: head of the group << 20 | tile
-  __shared__ uint64_t rows[MASKED ? kRunList + 4 : 1];
+  __shared__ int list[kRunList];  // query tiles: head of the group << 20 | tile
+  __shared__ uint64_t rows[MASKED ? kRunList : 1];  // of each tile, those that chose the block
+  __shared__ uint2 steps[MASKED ? 2 * kRunList : 1];  // halves that any did: head << 21 | half, rows
+  __shared__ int n_halves;
   char* const qbuf[RING] = {qbuf0, qbuf1, qbuf2, qbuf3};
   char* const gbuf[RING] = {gbuf0, gbuf1, gbuf2, gbuf3};
   float* const sbuf[RING] = {sbuf0, sbuf1, sbuf2, sbuf3};
-  debug_poison_lds(qbuf0, qbuf1, qbuf2, qbuf3, gbuf0, gbuf1, gbuf2, gbuf3, sbuf0, sbuf1, sbuf2, sbuf3, list, rows);
+  debug_poison_lds(qbuf0, qbuf1, qbuf2, qbuf3, gbuf0, gbuf1, gbuf2, gbuf3, sbuf0, sbuf1, sbuf2, sbuf3, list, rows, steps, n_halves);
 
   // the item: a block, a run of its query tiles, and 32 NW of its keys
-  const long long at = blockIdx.x / subs;
-  const int sub = (int)(blockIdx.x - at * subs);
-  const int bhk = (int)(at / n_items);
+  // (each XCD takes a run of them, whose blocks share queries in its L2, unless samples
+  // differ in length)
+  const unsigned work = a.key_lens ? blockIdx.x : (unsigned)xcd_remap((int)blockIdx.x, (int)gridDim.x);
+  const unsigned at = work / (unsigned)subs;
+  const int sub = (int)(work - at * subs);
+  const int bhk = (int)(at / (unsigned)n_items);
   const int item = (int)(at - bhk * n_items);
-  const int* const first = w.first + (long long)bhk * (a.nb + 1);
-  if (item >= first[a.nb]) return;  // (the whole workgroup)
-  const int j = w.items[(long long)bhk * n_items + item];
-  const int place = item - first[j], n_runs = first[j + 1] - first[j];
-  const int count = w.counts[(long long)bhk * a.nb + j];
-  const int rank0 = place * run, n_tiles = min(count - rank0, run);
+  const int total = w.first[(long long)bhk * (a.nb + 1) + a.nb];
+  const int4 rec = w.items[(long long)bhk * n_items + item];
+  if (item >= total) return;  // (the whole workgroup; what it read was never written)
+  const int j = rec.x, n_runs = rec.z;
+  const int rank0 = rec.y * run, n_tiles = min(rec.w - rank0, run);
   const int b = bhk / a.Hk, hk = bhk - b * a.Hk, G = a.H / a.Hk;
   const int lane = threadIdx.x & 63, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -271,14 +275,19 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void sparse_dkdv_kernel(c
     int head, row;
     uint32_t mine;
   };
-  auto step_of = [&](int s, int n) __attribute__((always_inline)) {  // (n: tiles listed)
-    const int e = s >> 1;
-    const int x = __builtin_amdgcn_readfirstlane(list[min(e, n)]);
-    Step st{x >> 20, (x & 0xfffff) * kTileRows + 32 * (s & 1), 0xffffffffu};
-    if (e >= n) st = Step{0, 32 * blocks32, 0xffffffffu};
-    if constexpr (MASKED)
-      if (e < n) st.mine = (uint32_t)__builtin_amdgcn_readfirstlane((int)reinterpret_cast<const uint32_t*>(rows)[2 * e + (s & 1)]);
-    return st;
+  // Step s of n, as it is read from LDS and (later) where it is; past the last: rows past
+  // the end.
+  auto peek = [&](int s, int n) __attribute__((always_inline)) -> uint2 {
+    s = min(s, n - 1);
+    if constexpr (MASKED) return steps[s];
+    else return make_uint2((uint32_t)list[s >> 1], 0xffffffffu);
+  };
+  auto step_of = [&](uint2 raw, int s, int n) __attribute__((always_inline)) {
+    const uint32_t x = (uint32_t)__builtin_amdgcn_readfirstlane((int)raw.x);
+    const uint32_t mine = MASKED ? (uint32_t)__builtin_amdgcn_readfirstlane((int)raw.y) : 0xffffffffu;
+    if (s >= n) return Step{0, 32 * blocks32, 0xffffffffu};
+    if (MASKED) return Step{(int)(x >> 21), (int)(x & 0x1fffff) * 32, mine};
+    return Step{(int)(x >> 20), (int)(x & 0xfffff) * kTileRows + 32 * (s & 1), mine};
   };
   auto request = [&](auto slot_tag, const Step& st, int r) __attribute__((always_inline)) {
     constexpr int SL = decltype(slot_tag)::value;
@@ -315,8 +324,9 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void sparse_dkdv_kernel(c
 #pragma unroll
   for (int i = 0; i < NC; ++i) dk[i] = dv[i] = zero16();
 
-  // Lists tiles r0 .. r0 + n - 1 of the block's (ranks over all heads of the group).
-  auto fill = [&](int r0, int n) __attribute__((always_inline)) {
+  // Lists tiles r0 .. r0 + n - 1 of the block's (ranks over all heads of the group);
+  // returns the steps.
+  auto fill = [&](int r0, int n) __attribute__((always_inline)) -> int {
     if (wave == 0) {
       int base = 0;
       for (int i0 = 0; i0 < G * words && base < r0 + n; i0 += 64) {
@@ -333,7 +343,6 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void sparse_dkdv_kernel(c
           if (r >= 0) list[r] = g << 20 | (word * kMapTiles + __builtin_ctzll(m));
         base += __shfl(upto, 63, 64);
       }
-      if (lane == 0) list[n] = 0;
     }
     __syncthreads();
     if constexpr (MASKED) {
@@ -349,14 +358,30 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void sparse_dkdv_kernel(c
         if (lane == 0) rows[e] = bits;
       }
       __syncthreads();
+      if (wave == 0) {
+        int found = 0;
+        for (int i0 = 0; i0 < 2 * n; i0 += 64) {
+          const int i = i0 + lane;
+          const uint32_t mine = i < 2 * n ? reinterpret_cast<const uint32_t*>(rows)[i] : 0u;
+          const uint64_t taken = __ballot(mine != 0);
+          if (mine != 0) {
+            const int x = list[i >> 1];
+            steps[found + (int)__popcll(taken & ((1ULL << lane) - 1))] = make_uint2((uint32_t)(x >> 20) << 21 | (uint32_t)(2 * (x & 0xfffff) + (i & 1)), mine);
+          }
+          found += (int)__popcll(taken);
+        }
+        if (lane == 0) n_halves = found;
+      }
+      __syncthreads();
+      return __builtin_amdgcn_readfirstlane(n_halves);
     }
+    return 2 * n;
   };
 
-  // adds the n tiles listed
+  // adds the n steps listed (n > 0: a listed tile has a row that chose the block)
   auto attend = [&](int n) __attribute__((always_inline)) {
-    const int n_steps = 2 * n;
     static_for<0, PF>([&](auto SC) __attribute__((always_inline)) {
-      const Step st = step_of(decltype(SC)::value, n);
+      const Step st = step_of(peek(decltype(SC)::value, n), decltype(SC)::value, n);
 #pragma unroll
       for (int r = 0; r < NREQ; ++r) request(SC, st, r);
     });
@@ -365,38 +390,60 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void sparse_dkdv_kernel(c
     f32x16 sa = zero16(), sb;
 #pragma unroll
     for (int i = 0; i < KS; ++i) sa = mfma32(lds_frag_row(qbuf0, rf.at(i)), kf[i], sa);
-    auto step = [&](auto slot_tag, f32x16& s, f32x16& sn, int i0) __attribute__((always_inline)) {
-      constexpr int SL = decltype(slot_tag)::value, NX = (SL + 1) % RING, RF = (SL + PF) % RING;
-      constexpr int NP = KS, NS = KS, NV = 2 * NC, NOPS = NP + NS + 2 * NV;
-      constexpr int W = NP + NS - 2;  // exponentials on the first W ops
-      static_assert(NREQ <= NOPS, "requests fit the op stream");
-      const Step ahead = step_of(i0 + PF, n);
-      const float* st = sbuf[SL];
-      f32x16 dp;
-      float4 l[4];
+    bf16x8 lead[2] = {lds_frag_row(gbuf0, rf.at(0)), lds_frag_row(gbuf0, rf.at(1))};  // the next step's first operands
+    f32x16 dpn;                                                                       // -D of its rows
+    auto start_of = [&](const float* st) __attribute__((always_inline)) {
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const float4 x = *reinterpret_cast<const float4*>(st + 8 * g + 4 * h);
-        l[g] = *reinterpret_cast<const float4*>(st + 32 + 8 * g + 4 * h);
-        dp[4 * g] = x.x;
-        dp[4 * g + 1] = x.y;
-        dp[4 * g + 2] = x.z;
-        dp[4 * g + 3] = x.w;
+        dpn[4 * g] = x.x;
+        dpn[4 * g + 1] = x.y;
+        dpn[4 * g + 2] = x.z;
+        dpn[4 * g + 3] = x.w;
+      }
+    };
+    start_of(sbuf0);
+    uint2 raw = peek(PF, n);  // of the step that the next one requests
+    auto step = [&](auto slot_tag, f32x16& s, f32x16& sn, int i0) __attribute__((always_inline)) {
+      constexpr int SL = decltype(slot_tag)::value, NX = (SL + 1) % RING, RF = (SL + PF) % RING;
+      constexpr int NP = KS, NS = KS, NV = 2 * NC, NOPS = NP + NS + 2 * NV;
+      // Vector work on the ops, evenly: row r's exponential before the dV op that reads
+      // it, two ops ahead, then its dS before the dK op.
+      constexpr auto exp_at = [](int r) { return r * (NP + NS + NC - 1) / 16; };
+      constexpr auto ds_at = [](int r) { return NP + 2 + r * (NS + NV + NC - 3) / 16; };
+      static_assert(exp_at(7) <= NP + NS - 2 && exp_at(15) <= NP + NS + NC - 2, "P before dV");
+      static_assert(ds_at(0) > exp_at(7) && ds_at(8) > exp_at(15), "P is handed over before dS takes its place");
+      static_assert(ds_at(7) <= NP + NS + NV - 2 && ds_at(15) <= NP + NS + NV + NC - 2, "dS before dK");
+      static_assert(NREQ <= NOPS, "requests fit the op stream");
+      const Step ahead = step_of(raw, i0 + PF, n);
+      raw = peek(i0 + PF + 1, n);
+      f32x16 dp = dpn;
+      f32x16 l;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 x = *reinterpret_cast<const float4*>(sbuf[SL] + 32 + 8 * g + 4 * h);
+        l[4 * g] = x.x;
+        l[4 * g + 1] = x.y;
+        l[4 * g + 2] = x.z;
+        l[4 * g + 3] = x.w;
       }
       bf16x8 pb[2], db[2];
       auto load_op = [&](int i) -> bf16x8 {
+        if (i >= NOPS) return lds_frag_row(gbuf[NX], rf.at(i - NOPS));
         if (i < NP) return lds_frag_row(gbuf[SL], rf.at(i));
         if (i < NP + NS) return lds_frag_row(qbuf[NX], rf.at(i - NP));
         const int t = (i - NP - NS) % NV;
         return tf.load(i < NP + NS + NV ? gbuf[SL] : qbuf[SL], 16 * (t / NC), t % NC);
       };
       bf16x8 aq[3];
-      aq[0] = load_op(0);
-      aq[1] = load_op(1);
+      aq[0] = lead[0];
+      aq[1] = lead[1];
       sched_fence();
       static_for<0, NOPS>([&](auto IC) __attribute__((always_inline)) {
         constexpr int i = decltype(IC)::value;
+        if constexpr (i == 0) __builtin_amdgcn_s_setprio(1);
         if constexpr (i + 2 < NOPS) aq[(i + 2) % 3] = load_op(i + 2);
+        else lead[i + 2 - NOPS] = load_op(i + 2);
         if constexpr (i < NP) {
           dp = mfma32(aq[i % 3], vf[i], dp);
         } else if constexpr (i < NP + NS) {
@@ -410,16 +457,16 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void sparse_dkdv_kernel(c
           dk[t % NC] = mfma32(aq[i % 3], db[t / NC], dk[t % NC]);
         }
         if constexpr (i < NREQ) request(std::integral_constant<int, RF>{}, ahead, i);
+        if constexpr (i == NOPS - 2) start_of(sbuf[NX]);
         static_for<0, 16>([&](auto RC) __attribute__((always_inline)) {
           constexpr int r = decltype(RC)::value;
-          if constexpr (r * W / 16 == i) {
-            float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -(r % 4 == 0 ? l[r / 4].x : r % 4 == 1 ? l[r / 4].y : r % 4 == 2 ? l[r / 4].z : l[r / 4].w)));
+          if constexpr (exp_at(r) == i) {
+            float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -l[r]));
             pin(x);
             s[r] = x;
             if constexpr ((r & 7) == 7) pb[r >> 3] = acc_to_operand(s, r >> 3);
           }
-          // dS of rows 0..7 by the first dK op, of 8..15 beside dV and by its second half
-          if constexpr (NP + NS + r * NV / 16 == i) {
+          if constexpr (ds_at(r) == i) {
             float x = s[r] * dp[r];
             pin(x);
             s[r] = x;
@@ -428,11 +475,12 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void sparse_dkdv_kernel(c
         });
         sched_fence();
       });
+      __builtin_amdgcn_s_setprio(0);
       // this wave's requests of the step before last have landed
       wait_vmem_leave<(PF - 2) * 2 * (decltype(dmq)::ALL_ACTIVE ? PW : 0)>();
       barrier_lds();
     };
-    const int padded_steps = (n_steps + RING - 1) / RING * RING;
+    const int padded_steps = (n + RING - 1) / RING * RING;
     for (int i = 0; i < padded_steps; i += RING) {
       step(std::integral_constant<int, 0>{}, sa, sb, i);
       step(std::integral_constant<int, 1>{}, sb, sa, i + 1);
@@ -445,8 +493,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void sparse_dkdv_kernel(c
 
   for (int r = 0; r < n_tiles; r += kRunList) {
     const int n = min(n_tiles - r, kRunList);
-    fill(rank0 + r, n);
-    attend(n);
+    attend(fill(rank0 + r, n));
   }
 
   const bool there = key < Nk;  // (of the sample's keys)
@@ -513,7 +560,7 @@ __global__ __launch_bounds__(256) void sparse_share_kernel(const SparseArgs a, c
 //
 // A workgroup of NW waves = 32 NW queries, Q and dO held; the listed blocks' K and V
 // stream through a ring of four slots in tiles of 32 keys. Per tile: S^T = K Q^T, dP^T =
-// V dO^T (from -D) beside the exponentials, dS^T, dQ^T += K^T dS^T.
+// V dO^T (from -D), dS^T, dQ^T += K^T dS^T.
 template <int D, int KS, int NW, bool MASKED>
 __global__ __launch_bounds__(64 * NW, D <= 96 ? 2 : 1) void sparse_dq_kernel(const SparseArgs a, const float* __restrict__ stats, int n_qtiles, int total, float c) {
   constexpr int BM = 32 * NW, BN = 32, RING = 4, PF = 3, NT = 64 * NW;
@@ -577,98 +624,116 @@ __global__ __launch_bounds__(64 * NW, D <= 96 ? 2 : 1) void sparse_dq_kernel(con
   rf.init(lane);
   tf.init(lane);
   f32x16 acc[NC];  // dQ^T
+  constexpr bool HELD = D <= 96;  // dP starts at -D: held where there are registers
+  f32x16 start;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) start[r] = nd;
 
   auto attend = [&](int n) __attribute__((always_inline)) {
     const int n_kt = n * tiles;
     TileAt ahead{0, 0};
-    auto key_of = [&]() __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(list.key0[min(ahead.e, n)]) + ahead.s * BN; };
-    int keys[RING];  // first key of the tile in each slot, and its entry
+    int keys[RING];    // first key of the tile in each slot, and its entry
     int entry[RING];
     static_for<0, PF>([&](auto SC) __attribute__((always_inline)) {
       constexpr int s = decltype(SC)::value;
-      keys[s] = key_of();
-      entry[s] = ahead.e;
+      entry[s] = min(ahead.e, n);
+      keys[s] = list.key_of(list.id[entry[s]], a.block, Nk) + ahead.s * BN;
       ahead.next(tiles);
 #pragma unroll
       for (int r = 0; r < NREQ; ++r) request(SC, keys[s], r);
     });
+    uint32_t raw_id = list.id[min(ahead.e, n)];  // of the tile that the next stage requests
     wait_vmem();
     __syncthreads();
-    constexpr int NS = 2 * KS, NQ = 2 * NC;
-    auto stage = [&](auto slot_tag) __attribute__((always_inline)) {
-      constexpr int SL = decltype(slot_tag)::value, RF = (SL + PF) % RING;
-      const int key0 = keys[SL];
-      keys[RF] = key_of();
-      entry[RF] = ahead.e;
-      ahead.next(tiles);
-      uint32_t mine = 0xffffffffu;
-      if constexpr (MASKED) mine = reinterpret_cast<const uint32_t*>(list.masks)[2 * min(entry[SL], list.kCap) + wave];
-      f32x16 s, dp;
+    // Tile j's scores are in s; the stream of ops runs dP(j), the scores of tile j + 1 and
+    // dQ += K(j)^T dS(j), the vector work of tile j spread over the first two.
+    constexpr int NP = KS, NS = KS, NQ = 2 * NC, NOPS = NP + NS + NQ;
+    constexpr auto exp_at = [](int r) { return r * (NP + NS - 2) / 16; };
+    constexpr auto ds_at = [](int r) { return NP + 1 + r * (NS + NC - 2) / 16; };
+    static_assert(ds_at(7) <= NP + NS - 2 && ds_at(15) <= NP + NS + NC - 2, "dS before dQ");
+    static_assert(exp_at(15) <= ds_at(0) || exp_at(15) < ds_at(8), "P before dS");
+    static_assert(NREQ <= NOPS, "requests fit the op stream");
+    // keys past the last: P = 0
+    auto cut = [&](f32x16& s, int key0) __attribute__((always_inline)) {
+      if (key0 + BN > Nk)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) dp[r] = nd;
+        for (int r = 0; r < 16; ++r)
+          if (key0 + acc_row(r, h) >= Nk) s[r] = -INFINITY;
+    };
+    f32x16 sa = zero16(), sb;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) sa = mfma32(lds_frag_row(kbuf0, rf.at(i)), qf[i], sa);
+    cut(sa, keys[0]);
+    bf16x8 lead[2] = {lds_frag_row(vbuf0, rf.at(0)), lds_frag_row(vbuf0, rf.at(1))};
+    auto stage = [&](auto slot_tag, f32x16& s, f32x16& sn) __attribute__((always_inline)) {
+      constexpr int SL = decltype(slot_tag)::value, NX = (SL + 1) % RING, RF = (SL + PF) % RING;
+      uint32_t mine = 0xffffffffu;
+      if constexpr (MASKED) mine = reinterpret_cast<const uint32_t*>(list.masks)[2 * entry[SL] + wave];
+      entry[RF] = min(ahead.e, n);
+      keys[RF] = list.key_of(raw_id, a.block, Nk) + ahead.s * BN;
+      ahead.next(tiles);
+      raw_id = list.id[min(ahead.e, n)];
+      f32x16 dp;
+      if constexpr (!HELD)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[r] = nd;
       bf16x8 db[2];
       bf16x8 aq[3];
       auto load_op = [&](int i) -> bf16x8 {
-        if (i < KS) return lds_frag_row(kbuf[SL], rf.at(i));
-        if (i < NS) return lds_frag_row(vbuf[SL], rf.at(i - KS));
-        return tf.load(kbuf[SL], 16 * ((i - NS) / NC), (i - NS) % NC);
+        if (i >= NOPS) return lds_frag_row(vbuf[NX], rf.at(i - NOPS));
+        if (i < NP) return lds_frag_row(vbuf[SL], rf.at(i));
+        if (i < NP + NS) return lds_frag_row(kbuf[NX], rf.at(i - NP));
+        return tf.load(kbuf[SL], 16 * ((i - NP - NS) / NC), (i - NP - NS) % NC);
       };
-      aq[0] = load_op(0);
-      aq[1] = load_op(1);
+      aq[0] = lead[0];
+      aq[1] = lead[1];
       sched_fence();
-      static_for<0, NS + NQ>([&](auto IC) __attribute__((always_inline)) {
+      static_for<0, NOPS>([&](auto IC) __attribute__((always_inline)) {
         constexpr int i = decltype(IC)::value;
-        if constexpr (i + 2 < NS + NQ) aq[(i + 2) % 3] = load_op(i + 2);
-        if constexpr (i < KS) {
-          if constexpr (i == 0) s = zero16();
-          s = mfma32(aq[i % 3], qf[i], s);
-        } else if constexpr (i < NS) {
-          dp = mfma32(aq[i % 3], gf[i - KS], dp);
-          static_for<0, 16>([&](auto RC) __attribute__((always_inline)) {
-            constexpr int r = decltype(RC)::value;
-            if constexpr (r * KS / 16 == i - KS) {
-              float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse2));
-              pin(x);
-              s[r] = x;
-            }
-          });
+        if constexpr (i == 0) __builtin_amdgcn_s_setprio(1);
+        if constexpr (i + 2 < NOPS) aq[(i + 2) % 3] = load_op(i + 2);
+        else lead[i + 2 - NOPS] = load_op(i + 2);
+        if constexpr (i < NP) {
+          dp = mfma32(aq[i % 3], gf[i], HELD && i == 0 ? start : dp);
+        } else if constexpr (i < NP + NS) {
+          if constexpr (i == NP) sn = zero16();
+          sn = mfma32(aq[i % 3], qf[i - NP], sn);
         } else {
-          if constexpr (i == NS) {
-            // keys past the last, and of rows that did not choose the block: dS = 0
-            if (key0 + BN > Nk)
-#pragma unroll
-              for (int r = 0; r < 16; ++r)
-                if (key0 + acc_row(r, h) >= Nk) s[r] = 0.f;
-            if constexpr (MASKED) {
-              if (mine != 0xffffffffu) {
-                const bool on = (mine >> (lane & 31)) & 1;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                  s[r] = on ? s[r] : 0.f;
-                  dp[r] = on ? dp[r] : 0.f;
-                }
-              }
-            }
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] *= dp[r];
-            db[0] = acc_to_operand(s, 0);
-            db[1] = acc_to_operand(s, 1);
-          }
-          constexpr int t = i - NS;
+          constexpr int t = i - NP - NS;
           acc[t % NC] = mfma32(aq[i % 3], db[t / NC], acc[t % NC]);
         }
         if constexpr (i < NREQ) request(std::integral_constant<int, RF>{}, keys[RF], i);
+        static_for<0, 16>([&](auto RC) __attribute__((always_inline)) {
+          constexpr int r = decltype(RC)::value;
+          if constexpr (exp_at(r) == i) {
+            float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse2));
+            pin(x);
+            s[r] = x;
+          }
+        });
+        static_for<0, 16>([&](auto RC) __attribute__((always_inline)) {
+          constexpr int r = decltype(RC)::value;
+          if constexpr (ds_at(r) == i) {
+            float x = s[r] * dp[r];
+            if constexpr (MASKED) x = (mine >> (lane & 31)) & 1 ? x : 0.f;  // (of a block that the row did not choose)
+            pin(x);
+            s[r] = x;
+            if constexpr ((r & 7) == 7) db[r >> 3] = acc_to_operand(s, r >> 3);
+          }
+        });
+        if constexpr (i == NOPS - 1) cut(sn, keys[NX]);
         sched_fence();
       });
+      __builtin_amdgcn_s_setprio(0);
       wait_vmem_leave<(PF - 2) * 2 * (decltype(dma)::ALL_ACTIVE ? PW : 0)>();
       barrier_lds();
     };
     const int padded_tiles = (n_kt + RING - 1) / RING * RING;
     for (int j = 0; j < padded_tiles; j += RING) {
-      stage(std::integral_constant<int, 0>{});
-      stage(std::integral_constant<int, 1>{});
-      stage(std::integral_constant<int, 2>{});
-      stage(std::integral_constant<int, 3>{});
+      stage(std::integral_constant<int, 0>{}, sa, sb);
+      stage(std::integral_constant<int, 1>{}, sb, sa);
+      stage(std::integral_constant<int, 2>{}, sa, sb);
+      stage(std::integral_constant<int, 3>{}, sb, sa);
     }
     wait_vmem();
     __syncthreads();
@@ -681,7 +746,7 @@ __global__ __launch_bounds__(64 * NW, D <= 96 ? 2 : 1) void sparse_dq_kernel(con
     const int count = list.template build<NT>(a, chosen, real, filter);
     for (int r = 0; r < count; r += list.kCap) {
       const int n = min(count - r, list.kCap);
-      list.template fill<NT>(a, chosen, real, Nk, filter, r, n);
+      list.template fill<NT>(a, chosen, real, filter, r, n);
       attend(n);
     }
     if (qrow < a.Nq && (!MASKED || ((filter >> (wave * 32 + (lane & 31))) & 1))) {
@@ -718,7 +783,7 @@ template <int D, int KS, int NW, bool MASKED>
 hipError_t go_dkdv(const SparseArgs& a, const Work& w, const Plan& p) {
   const int subs = a.block / (32 * NW);
   const long long grid = (long long)a.B * a.Hk * p.items * subs;
-  sparse_dkdv_kernel<D, KS, NW, MASKED><<<(unsigned)grid, 64 * NW, 0, a.stream>>>(a, w, p.words, p.run, p.items, subs, a.scale * kLog2e);
+  sparse_dkdv_kernel<D, KS, NW, MASKED><<<(unsigned)grid, 64 * NW, 0, a.stream>>>(a, w, p.words, p.run, (int)p.items, subs, a.scale * kLog2e);
   return hipGetLastError();
 }
 

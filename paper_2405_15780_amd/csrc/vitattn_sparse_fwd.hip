@@ -46,7 +46,7 @@ constexpr int exp_window(int NS, int CPB, int KB, int NOPS) {
 }
 
 template <int D, int KS, int KB, int NW, bool MASKED, bool SPLIT>
-__global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && NW == 4 ? 3 : 2) void sparse_fwd_kernel(const SparseArgs a, int n_qtiles, int n_split, int total,
+__global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && (NW == 4 || (KB == 1 && !MASKED)) ? 3 : 2) void sparse_fwd_kernel(const SparseArgs a, int n_qtiles, int n_split, int total,
                                                                 float c) {
   constexpr int BM = 32 * NW, BN = 32 * KB, NT = 64 * NW;
   constexpr int TILE = BN * D * 2;
@@ -123,6 +123,7 @@ __global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && NW == 4 
     if constexpr (MASKED) return reinterpret_cast<const uint32_t*>(list.masks)[2 * e + wave];
     else return 0xffffffffu;
   };
+  auto uniform = [](uint32_t x) __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
   auto max_quarter = [&](const f32x16 (&s)[KB], int q) {
     float m = -INFINITY;
 #pragma unroll
@@ -144,11 +145,25 @@ __global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && NW == 4 
 
   // Stage j as in vitattn_fwd.hip: s holds tile j's scores, sn gets tile j + 1's (of
   // key0 k1 and the rows' bits r1); K of tile j + 2 (k2) and V of tile j + 1 are requested.
-  auto stage = [&](auto parity, auto has_next, f32x16 (&s)[KB], f32x16 (&sn)[KB], int k1, int k2, uint32_t r1) __attribute__((always_inline)) {
+  // A wave none of whose rows chose either tile (r0, r1) has the requests alone.
+  auto stage = [&](auto parity, auto has_next, f32x16 (&s)[KB], f32x16 (&sn)[KB], int k1, int k2, uint32_t r0, uint32_t r1) __attribute__((always_inline)) {
     constexpr int P = decltype(parity)::value;
     constexpr bool NEXT = decltype(has_next)::value;
     const char* ks = kbuf[1 - P];
     const char* vs = vbuf[P];
+    if constexpr (MASKED && NEXT) {
+      if ((r0 | r1) == 0) {
+        dma.issue(rk, k2, ldk, kbuf[P]);
+        dmv.issue(rv, k1, ldv, vbuf[1 - P]);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sn[kb][r] = -INFINITY;
+        wait_vmem();
+        __syncthreads();
+        return;
+      }
+    }
     const float m_cur = m_run;
     float ls0 = 0.f, ls1 = 0.f;
     u32x4 pq[2 * KB];
@@ -243,17 +258,21 @@ __global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && NW == 4 
     using P1 = std::integral_constant<int, 1>;
     f32x16 sa[KB], sb[KB];
     const int n_kt = n * tiles;
+    // Tile j + 3's entry is read in stage j and used in the next: a wave does not wait for
+    // LDS between two stages. (Past the last block: Nk and more.)
     TileAt at{0, 0};
-    auto key_of = [&]() __attribute__((always_inline)) {  // (past the last block: Nk and more)
-      return __builtin_amdgcn_readfirstlane(list.key0[at.e]) + at.s * BN;
-    };
-    const int k0 = key_of();
-    uint32_t r1 = rows_of(at.e);
+    auto key_of = [&](uint32_t entry, int s) __attribute__((always_inline)) { return list.key_of(entry, a.block, Nk) + s * BN; };
+    const int k0 = key_of(list.id[0], 0);
+    uint32_t r0 = uniform(rows_of(0)), r1, r2;
     dma.issue(rk, k0, ldk, kbuf[0]);
     dmv.issue(rv, k0, ldv, vbuf[0]);
     at.next(tiles);
-    int k1 = key_of();
+    int k1 = key_of(list.id[at.e], at.s), k2;
+    r1 = uniform(rows_of(at.e));
     dma.issue(rk, k1, ldk, kbuf[1]);
+    at.next(tiles);
+    k2 = key_of(list.id[at.e], at.s);
+    r2 = uniform(rows_of(at.e));
     wait_vmem();
     __syncthreads();
 #pragma unroll
@@ -261,32 +280,37 @@ __global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && NW == 4 
       if (i % KS == 0) sa[i / KS] = zero16();
       sa[i / KS] = mfma32(lds_frag_row(kbuf[0], (i / KS) * 32 * 2 * D + kfrag.at(i % KS)), qf[i % KS], sa[i / KS]);
     }
-    mask(sa, k0, r1);
+    mask(sa, k0, r0);
     fold_max(fmaxf(fmaxf(max_quarter(sa, 0), max_quarter(sa, 1)), fmaxf(max_quarter(sa, 2), max_quarter(sa, 3))));
-    r1 = rows_of(at.e);
-    at.next(tiles);
-    int k2 = key_of(), e2 = at.e;
     __syncthreads();  // kbuf[0] is refilled by the first stage
+    uint32_t raw_id, raw_rows;
+    auto peek = [&]() __attribute__((always_inline)) {
+      at.next(tiles);
+      raw_id = list.id[at.e];
+      raw_rows = rows_of(at.e);
+    };
     // the next stage's tiles
     auto step = [&]() __attribute__((always_inline)) {
       k1 = k2;
-      r1 = rows_of(e2);
-      at.next(tiles);
-      k2 = key_of();
-      e2 = at.e;
+      r0 = r1;
+      r1 = r2;
+      k2 = key_of(raw_id, at.s);
+      r2 = uniform(raw_rows);
     };
     int j = 0;
     for (; j + 2 < n_kt; j += 2) {
-      stage(P0{}, std::true_type{}, sa, sb, k1, k2, r1);
+      peek();
+      stage(P0{}, std::true_type{}, sa, sb, k1, k2, r0, r1);
       step();
-      stage(P1{}, std::true_type{}, sb, sa, k1, k2, r1);
+      peek();
+      stage(P1{}, std::true_type{}, sb, sa, k1, k2, r0, r1);
       step();
     }
     if (j + 1 < n_kt) {
-      stage(P0{}, std::true_type{}, sa, sb, k1, k2, r1);
-      stage(P1{}, std::false_type{}, sb, sa, 0, 0, 0);
+      stage(P0{}, std::true_type{}, sa, sb, k1, k2, r0, r1);
+      stage(P1{}, std::false_type{}, sb, sa, 0, 0, 0, 0);
     } else {
-      stage(P0{}, std::false_type{}, sa, sb, 0, 0, 0);
+      stage(P0{}, std::false_type{}, sa, sb, 0, 0, 0, 0);
     }
     __syncthreads();  // before another list's tiles
   };
@@ -303,11 +327,11 @@ __global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && NW == 4 
     if constexpr (MASKED) {
       for (int r = r0; r < r1; r += list.kCap) {
         const int n = min(r1 - r, list.kCap);
-        list.template fill<NT>(a, chosen, real, Nk, filter, r, n);
+        list.template fill<NT>(a, chosen, real, filter, r, n);
         attend(n);
       }
     } else if (r1 > r0) {  // (one group's are never more)
-      list.template fill<NT>(a, chosen, real, Nk, filter, r0, r1 - r0);
+      list.template fill<NT>(a, chosen, real, filter, r0, r1 - r0);
       attend(r1 - r0);
     }
     const float l = sum_halves(l_part);
@@ -417,13 +441,13 @@ hipError_t go_tile(const SparseArgs& a) {
 
 }  // namespace
 
-// Up to 256 queries: at least four tiles of 64 keys for each split of a tile's list,
+// Up to 256 queries: at least two tiles of 64 keys for each split of a tile's list,
 // at most 32 splits.
 int sparse_splits(const SparseArgs& a) {
   if (a.Nq > 256) return 1;
   const int in_tile = one_group(a, 64) ? 1 : (min(a.Nq, 64) + a.q_block - 1) / a.q_block + 1;
   const long long most = min((long long)in_tile * a.topk, (long long)a.nb) * (a.block / 64);
-  return (int)max(1LL, min(32LL, most / 4));
+  return (int)max(1LL, min(32LL, most / 2));
 }
 
 size_t sparse_fwd_workspace_bytes(const SparseArgs& a) {
@@ -433,7 +457,7 @@ size_t sparse_fwd_workspace_bytes(const SparseArgs& a) {
 
 hipError_t launch_sparse_fwd(const SparseArgs& a) {
   switch (tile_width(a.d)) {
-    case 64: return go_tile<64, 4, 2, 2>(a);
+    case 64: return go_tile<64, 4, 2, 1>(a);
     case 96: return a.d <= 80 ? go_tile<96, 5, 2, 1>(a) : go_tile<96, 6, 2, 1>(a);
     case 128: return go_tile<128, 8, 2, 1>(a);
     default: return go_tile<160, 10, 1, 1>(a);
