@@ -27,3 +27,4 @@ from . import ulysses  # noqa: F401
 from . import aggregation  # noqa: F401
 from . import naive  # noqa: F401
 from . import block  # noqa: F401
+from . import sparse  # noqa: F401

@@ -83,6 +83,11 @@ struct BlockList {
     __syncthreads();
     return __builtin_amdgcn_readfirstlane(total);
   }
+  // How many of build's `count` blocks lie before block x.
+  __device__ __forceinline__ int below(int x, int nb, int count) const {
+    if (x >= nb) return count;
+    return __builtin_amdgcn_readfirstlane(before[x >> 5] + __popc(bits[x >> 5] & ((1u << (x & 31)) - 1)));
+  }
   // Lists the blocks r0 .. r0 + n - 1 (n <= kCap) of those.
   template <int NT>
   __device__ __forceinline__ void fill(const SparseArgs& a, const Chosen& c, int real, uint64_t filter, int r0, int n) {

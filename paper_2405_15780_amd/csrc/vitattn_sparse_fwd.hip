@@ -315,6 +315,8 @@ __global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && (NW == 4
     __syncthreads();  // before another list's tiles
   };
 
+  // Of a split: the blocks lo .. hi - 1, which all of the tile's rows keep to.
+  int lo = 0, hi = 0;
   // The outputs of the rows of `filter` from the blocks that they chose.
   auto rows = [&](uint64_t filter) __attribute__((always_inline)) {
 #pragma unroll
@@ -322,12 +324,17 @@ __global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && (NW == 4
     m_run = -3.0e38f;  // (finite, so that a tile of scores -inf leaves zeros and not NaN)
     l_part = 0.f;
     const int count = list.template build<NT>(a, chosen, real, filter);
-    const int r0 = SPLIT ? (int)((long long)count * sp / n_split) : 0;
-    const int r1 = SPLIT ? (int)((long long)count * (sp + 1) / n_split) : count;
+    const bool first = filter == ~0ULL;
+    const int r0 = !SPLIT ? 0 : first ? (int)((long long)count * sp / n_split) : list.below(lo, a.nb, count);
+    const int r1 = !SPLIT ? count : first ? (int)((long long)count * (sp + 1) / n_split) : list.below(hi, a.nb, count);
     if constexpr (MASKED) {
       for (int r = r0; r < r1; r += list.kCap) {
         const int n = min(r1 - r, list.kCap);
         list.template fill<NT>(a, chosen, real, filter, r, n);
+        if (SPLIT && first) {
+          if (r == r0) lo = __builtin_amdgcn_readfirstlane((int)list.id[0]);
+          hi = __builtin_amdgcn_readfirstlane((int)list.id[n - 1]) + 1;
+        }
         attend(n);
       }
     } else if (r1 > r0) {  // (one group's are never more)

@@ -1,0 +1,171 @@
+"""Dropout by its counter: the very mask of the oracle, values to half a step."""
+import numpy as np
+import pytest
+
+import oracle.sparse as os_
+from gpu_util import torch
+from test_gpu_layer_norm import close, half_step, make, np64
+from test_gpu_rms_norm import TYPES, tiny
+
+pytestmark = pytest.mark.gpu
+
+
+def check(x, p, rng, res=None):
+    import paper_2405_15780_amd as va
+
+    y = va.dropout_fwd(x, p, rng, res)
+    keep, up = os_.kept(tuple(x.shape) if x.dim() > 1 else (1, x.shape[0]), p, *rng)
+    keep = keep.reshape(x.shape)
+    X = np64(x)
+    want = np.where(keep, X * up, 0.0) + (0.0 if res is None else np64(res))
+    out = str(y.dtype)[6:]
+    off = 3 * 2.0 ** -24 * (np.abs(want) + np.abs(X) * up)
+    close(y, want, np.where(keep | (res is not None), off + half_step(out) * (np.abs(want) + off) + tiny(out), 0.0), "y")
+    if res is not None:
+        assert torch().equal(y[torch().from_numpy(~keep).cuda()], res[torch().from_numpy(~keep).cuda()])
+    return y
+
+
+@pytest.mark.parametrize("dtype,rtype", TYPES)
+@pytest.mark.parametrize("D", [1, 3, 7, 8, 9, 15, 16, 17, 72, 129, 1000, 4096])
+def test_widths(dtype, rtype, D):
+    print(f"case dropout D={D} {dtype} {rtype}", flush=True)
+    x, res = make((5, 13, D), dtype, D, 0.1), make((5, 13, D), rtype, D + 1)
+    check(x, 0.3, (D, 2 ** 40 + D), res)
+    check(x, 0.3, (D, 2 ** 40 + D))
+
+
+@pytest.mark.parametrize("p", [0.0, 1e-6, 2.0 ** -16, 0.1, 0.5, 0.999, 65535 / 65536, 1.0])
+def test_rates(p):
+    x = make((40, 250), "float32", 3)
+    y = check(x, p, (2 ** 64 - 1, 2 ** 63))
+    if p < 2.0 ** -17:
+        assert torch().equal(y, x)
+    if p == 1.0:
+        assert (y == 0).all()
+
+
+@pytest.mark.parametrize("n", [1, 5, 1023, 1024, 70001])
+def test_one_dim_and_many_rows(n):
+    check(make((n,), "bfloat16", n), 0.5, (1, 2))
+    check(make((n, 3), "float16", n), 0.25, (3, 4))
+
+
+def test_layouts_and_in_place():
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    x, res = (make((3, 4, 21, 40), "bfloat16", i, layout=[0, 2, 1, 3]) for i in (1, 2))
+    want = check(x.contiguous(), 0.4, (5, 6), res.contiguous())
+    assert t.equal(check(x, 0.4, (5, 6), res), want)
+    assert t.equal(check(x, 0.4, (5, 6), res.contiguous()), want)
+    wide = t.zeros((3, 4, 21, 45), dtype=x.dtype, device="cuda")[..., 2:42]
+    wide.copy_(x)
+    assert t.equal(check(wide, 0.4, (5, 6), res), want)
+    y = va.dropout_fwd(x.reshape(3, 2, 2, 21, 40), 0.4, (5, 6), res.reshape(3, 2, 2, 21, 40))
+    assert t.equal(y.reshape(x.shape), want)
+    a = x.clone()
+    assert va.dropout_fwd(a, 0.4, (5, 6), res, out=a) is a and t.equal(a, want)
+    b = res.clone()
+    va.dropout_fwd(x, 0.4, (5, 6), b, out=b)
+    assert t.equal(b, want)
+    odd = make((50, 19), "float16", 9)
+    c = odd.clone()
+    va.dropout_fwd(c, 0.4, (5, 6), out=c)  # rows end inside a piece
+    assert t.equal(c, check(odd, 0.4, (5, 6)))
+    with pytest.raises(va.VitattnError):
+        va.dropout_fwd(a[:2], 0.4, (5, 6), out=a[1:])
+
+
+def test_dropped_values_do_not_matter():
+    t = torch()
+    x = make((20, 100), "float32", 4)
+    keep = t.from_numpy(os_.kept((20, 100), 0.5, 7, 8)[0]).cuda()
+    bad = t.where(keep, x, t.full_like(x, float("nan")))
+    bad[~keep & (x > 0)] = float("inf")
+    import paper_2405_15780_amd as va
+
+    assert t.equal(va.dropout_fwd(bad, 0.5, (7, 8)), va.dropout_fwd(x, 0.5, (7, 8)))
+
+
+def test_past_two_to_the_31_elements():
+    """A row far behind 2^31 elements has the mask of its index."""
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    x = t.ones((2 ** 21 + 3, 1032), dtype=t.bfloat16, device="cuda")
+    y = va.dropout_fwd(x, 0.5, (11, 12))
+    for r in (0, 2 ** 21 - 1, 2 ** 21 + 2):
+        c = np.zeros((129, 4), dtype=np.uint64)
+        c[:, 0], c[:, 1], c[:, 2] = np.arange(129), r, 12
+        w = os_.philox(c, np.array([11, 0], dtype=np.uint64))
+        half = np.stack((w & np.uint64(0xffff), w >> np.uint64(16)), -1).reshape(-1)
+        assert np.array_equal(np64(y[r]), np.where(half >= 32768, 2.0, 0.0)), r
+    assert abs(y.float().mean().item() - 1.0) < 1e-3
+    del x, y
+    t.cuda.empty_cache()
+
+
+def test_autograd():
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    for dtype, rtype in TYPES:
+        x, res, g = (make((7, 50), d, i).requires_grad_(i < 2) for i, d in enumerate((dtype, rtype, rtype)))
+        va.dropout(x, 0.3, (1, 2), res).backward(g)
+        keep, up = os_.kept((7, 50), 0.3, 1, 2)
+        want = np.where(keep, np64(g) * up, 0.0)
+        close(x.grad, want, half_step(dtype) * np.abs(want) * (1 + 2.0 ** -22) + 2.0 ** -22 * np.abs(want) + tiny(dtype), "dx")
+        assert x.grad.dtype == x.dtype and t.equal(res.grad, g)
+    # the gradient of the gradient is the mask again
+    x = make((7, 50), "float32", 3).requires_grad_()
+    (dx,) = t.autograd.grad((va.dropout(x, 0.3, (1, 2)) ** 2).sum(), x, create_graph=True)
+    (ddx,) = t.autograd.grad(dx.sum(), x)
+    assert np.allclose(np64(ddx), np.where(keep, 2 * up * up, 0.0), rtol=1e-6)
+    z = t.zeros(3, 8, device="cuda").requires_grad_()
+    va.dropout(z, 0.5, (1, 2)).sum().backward()  # (a gradient without memory of its own)
+    assert t.isfinite(z.grad).all()
+
+
+def test_graph_draws_new_masks():
+    """A captured call reads its state when it is replayed."""
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    x, res = make((64, 130), "bfloat16", 5), make((64, 130), "bfloat16", 6)
+    state = t.tensor([3, 0], device="cuda")
+    side = t.cuda.Stream()
+    side.wait_stream(t.cuda.current_stream())
+    with t.cuda.stream(side):
+        va.dropout_fwd(x, 0.5, state, res)
+    t.cuda.current_stream().wait_stream(side)
+    g = t.cuda.CUDAGraph()
+    with t.cuda.graph(g):
+        y = va.dropout_fwd(x, 0.5, state, res)
+        state[1] += 1
+    seen = []
+    for i in range(4):
+        g.replay()
+        t.cuda.synchronize()
+        assert t.equal(y, va.dropout_fwd(x, 0.5, (3, i), res))
+        seen.append(y.clone())
+        state.add_(0)
+        t.cuda.synchronize()
+    assert not any(t.equal(a, b) for a, b in zip(seen, seen[1:]))
+
+
+def test_refusals():
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    x = make((6, 64), "bfloat16", 8)
+    bad = [(ValueError, lambda: va.dropout_fwd(x, 1.2, (1, 2))), (ValueError, lambda: va.dropout_fwd(x, float("nan"), (1, 2))),
+           (ValueError, lambda: va.dropout_fwd(x, 0.5, None)), (TypeError, lambda: va.dropout_fwd(x.double(), 0.5, (1, 2))),
+           (TypeError, lambda: va.dropout_fwd(x.t(), 0.5, (1, 2))), (TypeError, lambda: va.dropout_fwd(x, 0.5, (1, 2), x.half())),
+           (TypeError, lambda: va.dropout_fwd(x, 0.5, (1, 2), out=x.float())), (ValueError, lambda: va.dropout_fwd(x[:0], 0.5, (1, 2))),
+           (TypeError, lambda: va.dropout_fwd(x, 0.5, t.zeros(3, dtype=t.int64, device="cuda"))),
+           (TypeError, lambda: va.dropout_fwd(t._neg_view(x.float()), 0.5, (1, 2)))]
+    for i, (error, call) in enumerate(bad):
+        with pytest.raises(error):
+            call()
+            print("not refused", i)
