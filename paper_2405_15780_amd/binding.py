@@ -842,7 +842,7 @@ def _rng(p, rng, device):
     if isinstance(rng, torch.Tensor):
         if rng.dtype != torch.int64 or rng.shape != (2,) or rng.device != device or not rng.is_contiguous():
             raise TypeError(f"rng must be a contiguous int64 tensor of shape (2,) on {device}")
-        return DropoutSpec(0, 0, rng.data_ptr(), p)
+        return DropoutSpec(0, 0, _as_it_is(rng, "rng").data_ptr(), p)
     seed, offset = rng
     low = 0xffffffffffffffff
     return DropoutSpec(operator.index(seed) & low, operator.index(offset) & low, None, p)
@@ -982,7 +982,7 @@ def rms_norm_bwd(h, weight, rstd, dy, dh=None, p=0.0, rng=None, want_dx=True, wa
     h4, dy4 = _rows_of(h, "h"), _rows_of(dy, "dy")
     D = h4.shape[-1]
     wt = _norm_weights(dy, D, weight, None)
-    rstd = rstd.contiguous()
+    rstd = _as_it_is(rstd, "rstd").contiguous()
     one = h.dtype == dy.dtype and (spec is None or spec.p * 65536 <= 0.5) and want_dx and want_dresidual
     dres, dres4 = _row_out(None, "", h, h.dtype, h4) if want_dresidual else (None, None)
     dx, dx4 = _row_out(None, "", h, dy.dtype, h4) if want_dx and not one else (None, None)
@@ -1191,7 +1191,7 @@ def _bf16_heads(t, name, device=None):
 
 def _key_lens(key_lens, B, device):
     if key_lens is not None:
-        _expect(key_lens, "key_lens", _torch().int32, (B,), device, dense=True)
+        _as_it_is(_expect(key_lens, "key_lens", _torch().int32, (B,), device, dense=True), "key_lens")
 
 
 def block_means(k, block=128, key_lens=None):
@@ -1226,8 +1226,8 @@ def block_select(q, means, topk, q_block=1):
     if not (isinstance(m, torch.Tensor) and m.dim() == 4):
         raise TypeError("means must be what block_means returned")
     Hk, nb = m.shape[1:3]
-    _expect(m, "means[0]", torch.int8, (B, Hk, nb, -(-d // 64) * 64), q.device, dense=True)
-    _expect(scales, "means[1]", torch.float32, (B, Hk, nb), q.device, dense=True)
+    _as_it_is(_expect(m, "means[0]", torch.int8, (B, Hk, nb, -(-d // 64) * 64), q.device, dense=True), "means[0]")
+    _as_it_is(_expect(scales, "means[1]", torch.float32, (B, Hk, nb), q.device, dense=True), "means[1]")
     topk, q_block = operator.index(topk), operator.index(q_block)
     if topk < 1 or q_block < 1 or Hk < 1 or H % Hk:
         raise ValueError("topk and q_block must be at least 1, and H a multiple of the means' heads")
@@ -1252,7 +1252,7 @@ def _block_args(q, k, v, blocks, block, q_block, key_lens):
     if not (isinstance(blocks, _torch().Tensor) and blocks.dim() == 4):
         raise TypeError("blocks must be an int32 CUDA tensor [B, H, groups, topk]")
     topk = blocks.shape[3]
-    _expect(blocks, "blocks", _torch().int32, (B, H, -(-Nq // q_block), topk), device, dense=True)
+    _as_it_is(_expect(blocks, "blocks", _torch().int32, (B, H, -(-Nq // q_block), topk), device, dense=True), "blocks")
     _key_lens(key_lens, B, device)
     return B, H, Hk, Nq, Nk, d, block, q_block, topk
 
@@ -1289,8 +1289,8 @@ def block_bwd(q, k, v, blocks, o32, lse, dout, block=128, q_block=1, scale=None,
     torch = _torch()
     sizes = _block_args(q, k, v, blocks, block, q_block, key_lens)
     B, H, _, Nq, _, d = sizes[:6]
-    _expect(o32, "o32", torch.float32, (B, H, Nq, d), q.device, dense=True)
-    _expect(lse, "lse", torch.float32, (B, H, Nq), q.device, dense=True)
+    _as_it_is(_expect(o32, "o32", torch.float32, (B, H, Nq, d), q.device, dense=True), "o32")
+    _as_it_is(_expect(lse, "lse", torch.float32, (B, H, Nq), q.device, dense=True), "lse")
     _as_it_is(_expect(dout, "dout", torch.bfloat16, (B, H, Nq, d), q.device), "dout")
     dq, dk, dv = _like_layout(q, q.shape), _like_layout(k, k.shape), _like_layout(v, v.shape)
     lib = library()
