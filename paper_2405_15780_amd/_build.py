@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libvitattn.so")
 SOURCES = ["vitattn_api.hip", "vitattn_fwd.hip", "vitattn_bwd.hip", "vitattn_merge.hip", "vitattn_ulysses.hip", "vitattn_agg.hip",
            "vitattn_block_api.hip", "vitattn_rows_api.hip", "vitattn_norm.hip", "vitattn_rms.hip", "vitattn_rms_bwd.hip", "vitattn_dropout.hip", "vitattn_rotary.hip", "vitattn_diff_fwd.hip", "vitattn_diff_bwd.hip",
-           "vitattn_sparse_api.hip", "vitattn_select.hip", "vitattn_sparse_fwd.hip", "vitattn_sparse_bwd.hip"]
+           "vitattn_sparse_api.hip", "vitattn_select.hip", "vitattn_sparse_fwd.hip", "vitattn_sparse_bwd.hip",
+           "vitattn_sparse_dkdv.hip", "vitattn_sparse_dq.hip"]
 ARCH = "gfx950"
 
 HIP_FLAGS = [

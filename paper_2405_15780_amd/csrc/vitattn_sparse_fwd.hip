@@ -99,8 +99,8 @@ __global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && (NW == 4
   float m_run, l_part;
 
   constexpr int NE = 16 * KB;
-  // scores of keys past the last, and of rows that did not choose the block, are -inf
-  auto mask = [&](f32x16 (&s)[KB], int key0, uint32_t rows) __attribute__((always_inline)) {
+  // scores of keys past the last are -inf
+  auto mask = [&](f32x16 (&s)[KB], int key0) __attribute__((always_inline)) {
     if (key0 + BN > Nk) {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
@@ -108,15 +108,10 @@ __global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && (NW == 4
         for (int r = 0; r < 16; ++r)
           if (key0 + kb * 32 + acc_row(r, h) >= Nk) s[kb][r] = -INFINITY;
     }
-    if constexpr (MASKED) {
-      if (rows != 0xffffffffu) {
-        const bool mine = (rows >> (lane & 31)) & 1;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[kb][r] = mine ? s[kb][r] : -INFINITY;
-      }
-    }
+  };
+  // x where the lane's row chose the block (of the wave's bits), or else what stands for it
+  auto chose = [&](uint32_t rows, float x, float other) __attribute__((always_inline)) {
+    return !MASKED || ((rows >> (lane & 31)) & 1) ? x : other;
   };
   // the wave's 32 bits of entry e's mask
   auto rows_of = [&](int e) __attribute__((always_inline)) -> uint32_t {
@@ -158,13 +153,13 @@ __global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && (NW == 4
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sn[kb][r] = -INFINITY;
+          for (int r = 0; r < 16; ++r) sn[kb][r] = 0.f;
         wait_vmem();
         __syncthreads();
         return;
       }
     }
-    const float m_cur = m_run;
+    const float m_cur = chose(r0, m_run, INFINITY);  // (P = exp2(s - inf) = 0)
     float ls0 = 0.f, ls1 = 0.f;
     u32x4 pq[2 * KB];
     float xe[NE];
@@ -226,14 +221,14 @@ __global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && (NW == 4
         }
         exp_slice(IC, std::integral_constant<int, W>{});
         if constexpr (i >= W && i < W + 4) {
-          if constexpr (i == W) mask(sn, k1, r1);
+          if constexpr (i == W) mask(sn, k1);
           mq[i - W] = max_quarter(sn, i - W);
           pin(mq[i - W]);
         }
         sched_fence();
       });
       l_part += ls0 + ls1;
-      fold_max(fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])));
+      fold_max(chose(r1, fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])), -INFINITY));
       wait_vmem();
       __syncthreads();
     } else {
@@ -280,8 +275,8 @@ __global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && (NW == 4
       if (i % KS == 0) sa[i / KS] = zero16();
       sa[i / KS] = mfma32(lds_frag_row(kbuf[0], (i / KS) * 32 * 2 * D + kfrag.at(i % KS)), qf[i % KS], sa[i / KS]);
     }
-    mask(sa, k0, r0);
-    fold_max(fmaxf(fmaxf(max_quarter(sa, 0), max_quarter(sa, 1)), fmaxf(max_quarter(sa, 2), max_quarter(sa, 3))));
+    mask(sa, k0);
+    fold_max(chose(r0, fmaxf(fmaxf(max_quarter(sa, 0), max_quarter(sa, 1)), fmaxf(max_quarter(sa, 2), max_quarter(sa, 3))), -INFINITY));
     __syncthreads();  // kbuf[0] is refilled by the first stage
     uint32_t raw_id, raw_rows;
     auto peek = [&]() __attribute__((always_inline)) {
@@ -308,9 +303,9 @@ __global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && (NW == 4
     }
     if (j + 1 < n_kt) {
       stage(P0{}, std::true_type{}, sa, sb, k1, k2, r0, r1);
-      stage(P1{}, std::false_type{}, sb, sa, 0, 0, 0, 0);
+      stage(P1{}, std::false_type{}, sb, sa, 0, 0, r1, 0);
     } else {
-      stage(P0{}, std::false_type{}, sa, sb, 0, 0, 0, 0);
+      stage(P0{}, std::false_type{}, sa, sb, 0, 0, r0, 0);
     }
     __syncthreads();  // before another list's tiles
   };
