@@ -817,15 +817,17 @@ def _rows_of(t, name):
     return t if n <= 4 else t.reshape(-1, t.shape[-1])
 
 
-def _row_sizes(t):
-    """[B, H, N, D] of rows in up to three leading dims."""
-    return (1,) * (4 - t.dim()) + tuple(t.shape)
-
-
-def _row_strides(t):
-    s, n = t.stride(), t.shape
-    lead = [0 if n[i] == 1 else s[i] for i in range(len(n) - 1)]
-    return _strides(*[0] * (3 - len(lead)), *lead)
+def _row_args(*ts):
+    """Of tensors (or None) of one shape: (B, H, N, D) of their rows in up to three leading
+    dims, and the strides of each. Where all are contiguous their rows are one dim."""
+    n = ts[0].shape
+    if all(t is None or t.is_contiguous() for t in ts):
+        D = n[-1]
+        return (1, 1, ts[0].numel() // D, D), [_strides(0, 0, D)] * len(ts)
+    lead = len(n) - 1
+    none = [0] * (3 - lead)
+    return ((1,) * (3 - lead) + tuple(n),
+            [_NO_STRIDES if t is None else _strides(*none, *(0 if n[i] == 1 else t.stride(i) for i in range(lead))) for t in ts])
 
 
 def _rng(p, rng, device):
@@ -893,9 +895,8 @@ def dropout_fwd(x, p, rng, residual=None, out=None):
     x4 = _rows_of(x, "x")
     r4 = None if residual is None else _rows_of(residual, "residual")
     y, y4 = _row_out(out, "out", x, x.dtype if residual is None else residual.dtype, x4)
-    B, H, N, D = _row_sizes(x4)
-    _call(x, library().vitattn_dropout, x4.data_ptr(), _row_strides(x4), _ptr(r4),
-          _NO_STRIDES if r4 is None else _row_strides(r4), y4.data_ptr(), _row_strides(y4), B, H, N, D, code, rcode, spec)
+    sizes, (sx, sr, sy) = _row_args(x4, r4, y4)
+    _call(x, library().vitattn_dropout, x4.data_ptr(), sx, _ptr(r4), sr, y4.data_ptr(), sy, *sizes, code, rcode, spec)
     if out is not None:
         _written(out)
     return y
@@ -919,14 +920,14 @@ def rms_norm_fwd(x, weight=None, residual=None, eps=1e-5, p=0.0, rng=None, out=N
     if out is not None:
         y_out, h_out = out if residual is not None else (out, None)
     y, y4 = _row_out(y_out, "out y", x, x.dtype, x4)
-    h, h4, r4, sr, sh = x, None, None, _NO_STRIDES, _NO_STRIDES
+    h, h4, r4 = x, None, None
     if residual is not None:
         h, h4 = _row_out(h_out, "out h", x, residual.dtype, x4)
         r4 = _rows_of(residual, "residual")
-        sr, sh = _row_strides(r4), _row_strides(h4)
     rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if stats else None
-    _call(x, library().vitattn_rms_norm_fwd, x4.data_ptr(), _row_strides(x4), _ptr(r4), sr, _ptr(weight), _ptr(h4), sh,
-          y4.data_ptr(), _row_strides(y4), _ptr(rstd), *_row_sizes(x4), eps, code, rcode,
+    sizes, (sx, sr, sh, sy) = _row_args(x4, r4, h4, y4)
+    _call(x, library().vitattn_rms_norm_fwd, x4.data_ptr(), sx, _ptr(r4), sr, _ptr(weight), _ptr(h4), sh,
+          y4.data_ptr(), sy, _ptr(rstd), *sizes, eps, code, rcode,
           VITATTN_FP32 if wt == torch.float32 else code, spec)
     if out is not None:
         _written(y) if residual is None else _written(y, h)
@@ -945,15 +946,15 @@ def rms_norm_fp8(x, weight=None, residual=None, eps=1e-5, group=None):
     if group is not None and group not in (32, 64, 128):
         raise ValueError("group must be 32, 64, 128 or None (the row)")
     y, y4 = _row_out(None, "", x, torch.float8_e4m3fn, x4)
-    h, h4, r4, sr, sh = x, None, None, _NO_STRIDES, _NO_STRIDES
+    h, h4, r4 = x, None, None
     if residual is not None:
         h, h4 = _row_out(None, "", x, residual.dtype, x4)
         r4 = _rows_of(residual, "residual")
-        sr, sh = _row_strides(r4), _row_strides(h4)
     shape = x.shape[:-1] if group is None else x.shape[:-1] + ((D + group - 1) // group,)
     scale = torch.empty(shape, dtype=torch.float32, device=x.device)
-    _call(x, library().vitattn_rms_norm_fp8, x4.data_ptr(), _row_strides(x4), _ptr(r4), sr, _ptr(weight), _ptr(h4), sh,
-          y4.data_ptr(), _row_strides(y4), scale.data_ptr(), group or 0, *_row_sizes(x4), eps, code, rcode,
+    sizes, (sx, sr, sh, sy) = _row_args(x4, r4, h4, y4)
+    _call(x, library().vitattn_rms_norm_fp8, x4.data_ptr(), sx, _ptr(r4), sr, _ptr(weight), _ptr(h4), sh,
+          y4.data_ptr(), sy, scale.data_ptr(), group or 0, *sizes, eps, code, rcode,
           VITATTN_FP32 if wt == torch.float32 else code)
     return y, scale, h
 
@@ -989,19 +990,14 @@ def rms_norm_bwd(h, weight, rstd, dy, dh=None, p=0.0, rng=None, want_dx=True, wa
     dh4 = None if dh is None else _rows_of(dh, "dh")
     dw = torch.empty(D, dtype=wt, device=device) if want_dweight and weight is not None else None
     lib, size = library(), 0
-    sizes = _row_sizes(h4)
+    sizes, (sh, sdy, sdh, sdx, sdr) = _row_args(h4, dy4, dh4, dx4, dres4)
     if workspace is not None:
         size = _expect_workspace(workspace, device).numel() * workspace.element_size()
     elif dw is not None:
         size = lib.vitattn_rms_norm_bwd_workspace_bytes(*sizes, code)
         workspace = torch.empty(size // 4, dtype=torch.float32, device=device)
-
-    def strides(t):
-        return _NO_STRIDES if t is None else _row_strides(t)
-
-    _call(h, lib.vitattn_rms_norm_bwd, h4.data_ptr(), strides(h4), _ptr(weight), rstd.data_ptr(), dy4.data_ptr(),
-          strides(dy4), _ptr(dh4), strides(dh4), _ptr(dx4), strides(dx4), _ptr(dres4), strides(dres4), _ptr(dw), *sizes,
-          code, rcode, VITATTN_FP32 if wt == torch.float32 else code, spec, _ptr(workspace), size)
+    _call(h, lib.vitattn_rms_norm_bwd, h4.data_ptr(), sh, _ptr(weight), rstd.data_ptr(), dy4.data_ptr(),
+          sdy, _ptr(dh4), sdh, _ptr(dx4), sdx, _ptr(dres4), sdr, _ptr(dw), *sizes, code, rcode, VITATTN_FP32 if wt == torch.float32 else code, spec, _ptr(workspace), size)
     return dres if one else dx, dres, dw
 
 

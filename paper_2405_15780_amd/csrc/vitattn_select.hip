@@ -91,7 +91,8 @@ __global__ __launch_bounds__(256) void means_kernel(const SelectArgs a) {
   if (lane == 0) a.scales[item] = count > 0 ? (float)(top * (1. / 127.)) : -1.f;
 }
 
-// order-preserving whole numbers of fp32 values; 0 stands for none
+// order-preserving whole numbers of fp32 values; 0 stands for none. (No score is -0: the
+// scale of keys that are not all 0 is at least 2^-133 / 1024 / 127 > 2^-150, and not 0.)
 __device__ __forceinline__ uint32_t ordered(float x) {
   const uint32_t u = __float_as_uint(x);
   return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);

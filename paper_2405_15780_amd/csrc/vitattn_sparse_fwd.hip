@@ -32,6 +32,8 @@ namespace vitattn {
 
 namespace {
 
+constexpr int kMaxSplits = 32;
+
 // see vitattn_fwd.hip: score e of 16*KB per lane is exponentiated in slot
 // e*W/(16*KB), two slots before the PV op that reads it
 constexpr bool exp_fits(int NS, int CPB, int KB, int W) {
@@ -385,34 +387,32 @@ __global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && (NW == 4
   }
 }
 
-// Joins the splits of one query row: a wave per row and 64 columns.
+// Joins the splits (at most kMaxSplits) of one query row: a wave per row and 64 columns,
+// all of its loads on their way at once.
 __global__ __launch_bounds__(64) void sparse_join_kernel(const SparseArgs a, int n_split) {
-  constexpr int U = 8;
   const long long row = blockIdx.x, rows = (long long)a.B * a.H * a.Nq;
   const int lane = threadIdx.x, col = 64 * blockIdx.y + lane;
   const long long bh = row / a.Nq;
   const int i = (int)(row - bh * a.Nq), b = (int)(bh / a.H), head = (int)(bh - (long long)b * a.H);
   const float* const share = reinterpret_cast<const float*>(a.work);
-  const float* outs = share + (bh * n_split * a.Nq + i) * a.d;
-  const float* lses = share + rows * n_split * a.d + bh * n_split * a.Nq + i;
-  // (at most 64 splits)
+  const float* const outs = share + (bh * n_split * a.Nq + i) * a.d + min(col, a.d - 1);
+  const float* const lses = share + rows * n_split * a.d + bh * n_split * a.Nq + i;
   const float mine = lane < n_split ? lses[(long long)lane * a.Nq] : -INFINITY;
+  float x[kMaxSplits];
+#pragma unroll
+  for (int s = 0; s < kMaxSplits; ++s) x[s] = outs[(long long)min(s, n_split - 1) * a.Nq * a.d];
   float top = mine;
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
   const float ref = top == -INFINITY ? 0.f : top;
+  const float weight = mine == -INFINITY ? 0.f : expf(mine - ref);  // of the lane's split
+  const uint32_t there = (uint32_t)__ballot(mine != -INFINITY);
   float o = 0.f, sum = 0.f;
-  for (int s0 = 0; s0 < n_split; s0 += U) {
-    float x[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = s0 + u < n_split && col < a.d ? outs[(long long)(s0 + u) * a.Nq * a.d + col] : 0.f;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const float l = s0 + u < n_split ? __shfl(mine, s0 + u, 64) : -INFINITY;
-      const float w = l == -INFINITY ? 0.f : expf(l - ref);
-      sum += w;
-      o += l == -INFINITY ? 0.f : w * x[u];
-    }
+  for (int s = 0; s < kMaxSplits; ++s) {
+    const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(weight), s));
+    sum += w;
+    o += (there >> s) & 1 ? w * x[s] : 0.f;
   }
   if (lane == 0 && blockIdx.y == 0 && a.lse) a.lse[row] = top == -INFINITY ? -INFINITY : ref + logf(sum);
   if (col >= a.d) return;
@@ -444,12 +444,12 @@ hipError_t go_tile(const SparseArgs& a) {
 }  // namespace
 
 // Up to 256 queries: at least two tiles of 64 keys for each split of a tile's list,
-// at most 32 splits.
+// at most kMaxSplits.
 int sparse_splits(const SparseArgs& a) {
   if (a.Nq > 256) return 1;
   const int in_tile = one_group(a, 64) ? 1 : (min(a.Nq, 64) + a.q_block - 1) / a.q_block + 1;
   const long long most = min((long long)in_tile * a.topk, (long long)a.nb) * (a.block / 64);
-  return (int)max(1LL, min(32LL, most / 2));
+  return (int)max(1LL, min((long long)kMaxSplits, most / 2));
 }
 
 size_t sparse_fwd_workspace_bytes(const SparseArgs& a) {

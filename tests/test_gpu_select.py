@@ -77,6 +77,19 @@ def test_ties_go_to_the_lowest():
     assert (got == np.arange(4)).all()
 
 
+def test_the_smallest_keys():
+    """One key of 1,024 of bf16's least value: the scale is fp32's least, 2^-149 (2^-143 / 127 is above
+    half of it), and not 0, so that blocks below zero come behind those of zeros."""
+    t = torch()
+    q = t.ones((1, 1, 3, 64), dtype=t.bfloat16, device="cuda")
+    k = t.zeros((1, 1, 8 * 1024, 64), dtype=t.bfloat16, device="cuda")
+    for j in (0, 3, 4):
+        k[0, 0, 1024 * j, 5] = -2.0 ** -133
+    assert (k != 0).sum() == 3
+    got = check(q, k, 1024, 1, 5)
+    assert (got == [1, 2, 5, 6, 7]).all()
+
+
 @pytest.mark.parametrize("lens", [[0, 1, 700], [64, 65, 63], [0, 0, 0]])
 def test_key_lens(lens):
     """Samples with few keys or none; the keys behind are not read."""
