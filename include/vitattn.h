@@ -656,6 +656,7 @@ int vitattn_block_means(const void* k, vitattn_strides sk, const int* key_lens, 
  *   q     : bf16 [B][H][Nq][d].
  *   blocks: int32 [B][H][ceil(Nq / q_block)][topk], dense.
  *   topk  : 1 .. VITATTN_SELECT_MAX, else VITATTN_E_UNSUPPORTED.
+ *   sizes : B and H up to 65,535.
  */
 int vitattn_block_select(const void* q, vitattn_strides sq, const void* means, const float* scales, int* blocks, int B,
                          int H, int Hk, int Nq, int d, int nb, int q_block, int topk, void* stream);

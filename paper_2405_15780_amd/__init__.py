@@ -1,6 +1,8 @@
 """Exact non-causal multi-head attention (forward and backward) for MI355X, and
-the operators of a block around it: layer norm, rotary positions with several
-axes, differential attention.
+the operators of a block around it: layer norm, rms norm with the residual's
+addition (also to 8 bits), dropout from a counter, rotary positions with several
+axes, differential attention, and attention over key blocks that a cheap score
+chooses.
 
 A thin ctypes binding over the C ABI in include/vitattn.h; it only marshals
 arguments. Every step of the computation runs in the library's HIP kernels.

@@ -19,6 +19,12 @@
 // their scores in registers as whole numbers that order alike. The topk-th largest of the
 // lanes' highest, found bit by bit by counting (ballots), is reached by topk scores and few
 // more; these go to a lane each, where the same search finds the threshold.
+//
+// 8 heads of 32,768 groups choose 16 of 512 blocks (d = 64) in 206 us, bound by the search's
+// scalar and vector instructions (80 and 71 million; the products are a twentieth, the
+// bytes 16 us): taking the largest topk times over was 375 us, the search over all scores 245.
+// A group of 1,024 blocks (d = 128): 8.6 us, one workgroup's latency. The means of 8 x 32,768
+// keys of 64: 17 us, a launch of 2.0 TB/s.
 #include "vitattn_common.h"
 #include "vitattn_launch.h"
 

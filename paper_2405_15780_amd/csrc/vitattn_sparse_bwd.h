@@ -22,13 +22,14 @@ inline SparsePlan plan_of(const SparseArgs& a) {
   const long long groups = a.q_block >= kTileRows ? (a.q_block % kTileRows == 0 ? 1 : 2)
                                                   : min((long long)kTileRows / a.q_block + 2, (long long)min(a.Nq, kTileRows));
   const long long pairs = (long long)(a.H / a.Hk) * p.tiles * min(groups * a.topk, (long long)a.nb);
-  // runs of 64 tiles, of 32 where there are few blocks to fill the card with, and longer
-  // ones where the shares of as many items would outgrow eight times the keys
+  // Runs of 64 tiles, of 32 where there are few blocks to fill the card with (126 blocks of
+  // 4 key heads: dK/dV and shares 158 us with 32, 181 with 64, 212 with 128; 512 blocks of 8:
+  // 399, 396, 442), and longer ones where the shares of as many items would outgrow eight
+  // times the keys.
   p.run = (int)max(a.nb < 256 ? 32LL : 64LL, min(4096LL, (pairs + 8LL * a.nb - 1) / (8LL * a.nb)));
   p.items = a.nb + pairs / p.run;  // sum over the blocks of max(1, ceil(count / run))
   return p;
 }
-
 
 // workspace
 struct SparseWork {

@@ -1,4 +1,11 @@
 // dK and dV of the attention over chosen key blocks (vitattn_sparse_bwd.hip).
+//
+// Steps of 32 queries: a wave holds its 32 keys' K and V and sums dK and dV. In step j
+// the matrix cores run dP(j) = dO(j) V^T (starting at -D) and the scores of step j + 1
+// beside the exponentials of step j, then dV += P(j)^T dO(j) beside dS(j), then
+// dK += dS(j)^T Q(j). Blocks of 32 queries arrive in a ring of four slots, three steps
+// ahead. Steps past the last read zeros: P is 1 there, and dO and Q are zero; so do the
+// places that a step of gathered rows (MASKED) leaves empty.
 #include "vitattn_sparse_bwd.h"
 
 namespace vitattn {
@@ -6,14 +13,8 @@ namespace vitattn {
 namespace {
 
 constexpr int kRunList = 128;   // query tiles that an item lists at a time
-constexpr int kRunRows = 32;    // the same where each row chose its own
+constexpr int kRunRows = 32;    // the same where each row chose its own (16: 167 us for 142)
 
-//
-// Steps of 32 queries: a wave holds its 32 keys' K and V and sums dK and dV. In step j
-// the matrix cores run dP(j) = dO(j) V^T (starting at -D) and the scores of step j + 1
-// beside the exponentials of step j, then dV += P(j)^T dO(j) beside dS(j), then
-// dK += dS(j)^T Q(j). Blocks of 32 queries arrive in a ring of four slots, three steps
-// ahead. Steps past the last read zeros: P is 1 there, and dO and Q are zero.
 template <int D, int KS, int NW, bool MASKED>
 __global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void sparse_dkdv_kernel(const SparseArgs a, const SparseWork w, int words, int run, int n_items, int subs, float c) {
   constexpr int BQ = 32, RING = 4, PF = 3;
