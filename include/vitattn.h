@@ -679,7 +679,8 @@ int vitattn_block_select(const void* q, vitattn_strides sq, const void* means, c
  *                    which the backward reads; either may be null in the forward.
  *   topk           : 1 .. VITATTN_SPARSE_MAX_TOPK; d, block and nb as above, H / Hk up to
  *                    2047; else VITATTN_E_UNSUPPORTED.
- *   sizes          : Nq up to 2^26, B*H*(Nq + 128) and B*Hk*nb*block below 2^30.
+ *   sizes          : Nq up to 2^26, B*H*(Nq + 128) and B*Hk*nb*block below 2^30, B*H*(Nq + 4096)
+ *                    below 2^32.
  *   workspace      : at least the bytes the matching function gives (0 if invalid; the
  *                    forward's is 0 unless up to 256 queries split their blocks over
  *                    workgroups), 16-byte aligned.

@@ -45,10 +45,10 @@ int check_sparse(vitattn::SparseArgs& a, int B, int H, int Hk, int Nq, int Nk, i
   a.topk = topk;
   a.groups = (Nq - 1) / q_block + 1;
   a.nb = (Nk - 1) / block + 1;
-  // launches below 2^32 work-items: 4 per row, padded to 128 rows; 16 per row padded to 4,096 (the map);
+  // launches below 2^32 work-items: 4 per row, padded to 128 rows; one per row padded to 4,096 (the map);
   // 32 splits of few queries and 192 per row where they are joined; rows below 2^31
   const double rows = (double)B * H * (Nq + 128.), keys = (double)B * Hk * ((double)a.nb * block);
-  if (4. * rows >= kMaxWorkItems || (double)B * H * (Nq / 4096 + 1) * 1024. >= kMaxWorkItems || rows >= 0x7fffffff)
+  if (4. * rows >= kMaxWorkItems || (double)B * H * (Nq / 4096 + 1) * 4096. >= kMaxWorkItems || rows >= 0x7fffffff)
     return VITATTN_E_INVAL;
   if (Nq <= 256 && 192. * B * H * (Nq + 64.) >= kMaxWorkItems) return VITATTN_E_INVAL;
   if (4. * keys >= kMaxWorkItems) return VITATTN_E_INVAL;

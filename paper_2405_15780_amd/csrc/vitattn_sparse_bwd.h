@@ -23,7 +23,7 @@ inline SparsePlan plan_of(const SparseArgs& a) {
                                                   : min((long long)kTileRows / a.q_block + 2, (long long)min(a.Nq, kTileRows));
   const long long pairs = (long long)(a.H / a.Hk) * p.tiles * min(groups * a.topk, (long long)a.nb);
   // Runs of 64 tiles, of 32 where there are few blocks to fill the card with (126 blocks of
-  // 4 key heads: dK/dV and shares 158 us with 32, 181 with 64, 212 with 128; 512 blocks of 8:
+  // 4 key heads: dK/dV and shares 98 us with 32, 105 with 64, 118 with 128; 512 blocks of 8:
   // 399, 396, 442), and longer ones where the shares of as many items would outgrow eight
   // times the keys.
   p.run = (int)max(a.nb < 256 ? 32LL : 64LL, min(4096LL, (pairs + 8LL * a.nb - 1) / (8LL * a.nb)));
@@ -38,6 +38,10 @@ struct SparseWork {
   int* counts;       // [B Hk][nb]
   int* first;        // [B Hk][nb + 1]: a block's first item; the number of items
   int4* items;       // [B Hk][items]: an item's block, its run, the block's runs and query tiles
+  // where a query tile's rows choose apart (not one_group(a, 64)):
+  int* ranks;        // [BH][words][nb]: tiles that chose the block before the word's, of all heads that share keys
+  uint64_t* rows;    // [B Hk][items][run]: of an item's query tiles, the rows that chose the block
+  int* tiles;        // [B Hk][items][run]: and which they are, head of the group << 20 | tile
   float* shares;     // [B Hk][items][2][block][d]
   size_t bytes;
 };
@@ -57,6 +61,10 @@ inline SparseWork work_of(const SparseArgs& a, const SparsePlan& p) {
   w.counts = reinterpret_cast<int*>(take(bhk * a.nb * 4));
   w.first = reinterpret_cast<int*>(take(bhk * (a.nb + 1) * 4));
   w.items = reinterpret_cast<int4*>(take(bhk * p.items * sizeof(int4)));
+  const size_t apart = one_group(a, kTileRows) ? 0 : 1, slots = apart * bhk * p.items * p.run;
+  w.ranks = reinterpret_cast<int*>(take(apart * bh * p.words * a.nb * 4));
+  w.rows = reinterpret_cast<uint64_t*>(take(slots * 8));
+  w.tiles = reinterpret_cast<int*>(take(slots * 4));
   w.shares = reinterpret_cast<float*>(take(p.items > a.nb ? bhk * p.items * 2 * a.block * a.d * 4 : 0));
   w.bytes = n;
   return w;

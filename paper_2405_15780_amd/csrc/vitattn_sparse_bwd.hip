@@ -22,15 +22,18 @@
 // of all heads that share the keys.
 //
 // Where a query tile's rows chose apart (MASKED), dK/dV gathers those that chose the block,
-// 32 a step, from wherever they are: no other row is read. dQ's rows share the keys they
+// 32 a step, from wherever they are: no other row is read. Two more passes list them: the
+// rank of each word's first tile among a block's, then a workgroup per tile collects which
+// rows chose what, as the forward does, and puts a tile and its 64 bits in their item's place. dQ's rows share the keys they
 // read; there a tile whose dQ is not finite goes over its rows one at a time, as the
 // forward does.
 //
 // Heads of 64, 8 of them, 32,768 queries in groups of 64 of 32 blocks of 64 keys each: row pass
 // 17 us (5.0 TB/s), map 6, plan 5, dK/dV 369-397 (0.69 PFLOP/s; matrix cores busy 51-53 %, LDS
 // 41 %), shares 17, dQ 233-260. 2 samples of 4 heads (2 of keys) of 72, 8,003 queries of 8 blocks
-// each: 8, 8, 5, 139, 14 and 183 us; reading every half tile that any row chose from, dK/dV
-// took 266. There the lists are 92 of the 139 us (a wave for 64 rows' choices), the products 9.
+// each: 8, 8, 5, 82, 14 and 183 us, and 14 for the rows' lists. There dK/dV took 266 us reading
+// every half tile that any row chose from, and 139 where each item looked through its tiles'
+// choices itself.
 
 #include "vitattn_sparse_bwd.h"
 
@@ -152,6 +155,48 @@ __global__ __launch_bounds__(1024) void sparse_plan_kernel(const SparseArgs a, c
   if (threadIdx.x == 1023) first[a.nb] = at;
 }
 
+// Of query tiles whose rows choose apart, where each block's begin in the words of the map:
+// a thread per block.
+__global__ __launch_bounds__(256) void sparse_rank_kernel(const SparseArgs a, const SparseWork w, int words, int groups) {
+  const int bhk = blockIdx.x / groups, j = 256 * (blockIdx.x - bhk * groups) + threadIdx.x;
+  if (j >= a.nb) return;
+  const long long at = (long long)bhk * (a.H / a.Hk) * words * a.nb + j;
+  int n = 0;
+#pragma unroll 4
+  for (int i = 0; i < a.H / a.Hk * words; ++i) {
+    w.ranks[at + (long long)i * a.nb] = n;
+    n += __popcll(w.map[at + (long long)i * a.nb]);
+  }
+}
+
+// And the rows of each that chose its blocks, to the items' places: a workgroup per tile.
+__global__ __launch_bounds__(128) void sparse_rows_kernel(const SparseArgs a, const SparseWork w, int words, int tiles, int run, long long n_items) {
+  __shared__ BlockList<true> list;
+  debug_poison_lds(list);
+  const int bh = blockIdx.x / tiles, t = blockIdx.x - bh * tiles;
+  const int b = bh / a.H, head = bh - b * a.H, G = a.H / a.Hk;
+  const long long bhk = (long long)b * a.Hk + head / G;
+  const int Nk = sparse_keys(a, b), real = (Nk + a.block - 1) / a.block;
+  const Chosen chosen(a, bh, t * kTileRows, kTileRows);
+  const int left = a.Nq - t * kTileRows;
+  const uint64_t there = left >= 64 ? ~0ULL : (1ULL << left) - 1;
+  const int* const first = w.first + bhk * (a.nb + 1);
+  const long long word = ((long long)bh * words + t / kMapTiles) * a.nb;
+  const int count = list.build<128>(a, chosen, real, ~0ULL);
+  for (int r = 0; r < count; r += list.kCap) {
+    const int n = min(count - r, list.kCap);
+    list.fill<128>(a, chosen, real, ~0ULL, r, n);
+    for (int i = threadIdx.x; i < n; i += 128) {
+      const int j = list.id[i];
+      const int rank = w.ranks[word + j] + __popcll(w.map[word + j] & ((1ULL << (t % kMapTiles)) - 1));
+      const long long slot = (bhk * n_items + first[j]) * run + rank;
+      w.rows[slot] = list.masks[i] & there;
+      w.tiles[slot] = (head % G) << 20 | t;
+    }
+    __syncthreads();  // before another list
+  }
+}
+
 // Adds the shares of a key block of several runs in their order: four columns per thread.
 __global__ __launch_bounds__(256) void sparse_share_kernel(const SparseArgs a, const SparseWork w, long long n_items) {
   const int bhk = blockIdx.x / a.nb, j = blockIdx.x - bhk * a.nb;
@@ -202,6 +247,13 @@ hipError_t launch_sparse_bwd(const SparseArgs& a) {
   if ((err = hipGetLastError()) != hipSuccess) return err;
   sparse_plan_kernel<<<a.B * a.Hk, 1024, 0, a.stream>>>(a, w.counts, w.first, w.items, p.run, p.items);
   if ((err = hipGetLastError()) != hipSuccess) return err;
+  if (!one_group(a, kTileRows)) {
+    const int parts_of_blocks = (a.nb + 255) / 256;
+    sparse_rank_kernel<<<(unsigned)(a.B * a.Hk) * parts_of_blocks, 256, 0, a.stream>>>(a, w, p.words, parts_of_blocks);
+    if ((err = hipGetLastError()) != hipSuccess) return err;
+    sparse_rows_kernel<<<(unsigned)(a.B * a.H) * p.tiles, 128, 0, a.stream>>>(a, w, p.words, p.tiles, p.run, p.items);
+    if ((err = hipGetLastError()) != hipSuccess) return err;
+  }
   if ((err = launch_sparse_dkdv(a, w, p)) != hipSuccess) return err;
   if (p.items > a.nb) {
     sparse_share_kernel<<<dim3((unsigned)(a.B * a.Hk) * a.nb, (2 * a.block * a.d + 1023) / 1024), 256, 0, a.stream>>>(a, w, p.items);

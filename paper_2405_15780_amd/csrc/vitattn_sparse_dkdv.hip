@@ -13,7 +13,7 @@ namespace vitattn {
 namespace {
 
 constexpr int kRunList = 128;   // query tiles that an item lists at a time
-constexpr int kRunRows = 32;    // the same where each row chose its own (16: 167 us for 142)
+constexpr int kRunRows = 32;    // the same where each row chose its own
 
 template <int D, int KS, int NW, bool MASKED>
 __global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void sparse_dkdv_kernel(const SparseArgs a, const SparseWork w, int words, int run, int n_items, int subs, float c) {
@@ -171,53 +171,11 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void sparse_dkdv_kernel(c
   // Lists tiles r0 .. r0 + n - 1 of the block's (ranks over all heads of the group);
   // returns the steps.
   auto fill = [&](int r0, int n) __attribute__((always_inline)) -> int {
-    if (wave == 0) {
-      int base = 0;
-      for (int i0 = 0; i0 < G * words && base < r0 + n; i0 += 64) {
-        const int i = i0 + lane, g = i / words, word = i - g * words;
-        uint64_t m = i < G * words ? w.map[(((long long)b * a.H + hk * G + g) * words + word) * a.nb + j] : 0;
-        const int mine = __popcll(m);
-        int upto = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-          const int x = __shfl_up(upto, d, 64);
-          if (lane >= d) upto += x;
-        }
-        for (int r = base + upto - mine - r0; m != 0 && r < n; ++r, m &= m - 1)
-          if (r >= 0) list[r] = g << 20 | (word * kMapTiles + __builtin_ctzll(m));
-        base += __shfl(upto, 63, 64);
-      }
-    }
-    __syncthreads();
     if constexpr (MASKED) {
-      // four tiles at a time, a lane per row: whether its group chose the block
-      constexpr int TU = 4, IU = 8;
-      for (int e0 = TU * wave; e0 < n; e0 += TU * NW) {
-        const int* chosen[TU];
-        bool mine[TU];
-#pragma unroll
-        for (int u = 0; u < TU; ++u) {
-          const int x = list[min(e0 + u, n - 1)], row = (x & 0xfffff) * kTileRows + lane;
-          chosen[u] = a.blocks + (((long long)b * a.H + hk * G + (x >> 20)) * a.groups + min(row, a.Nq - 1) / a.q_block) * a.topk;
-          mine[u] = false;
-        }
-        for (int i = 0; i < a.topk; i += IU) {
-          int x[TU][IU];
-#pragma unroll
-          for (int u = 0; u < TU; ++u)
-#pragma unroll
-            for (int k = 0; k < IU; ++k) x[u][k] = chosen[u][min(i + k, a.topk - 1)];
-#pragma unroll
-          for (int u = 0; u < TU; ++u)
-#pragma unroll
-            for (int k = 0; k < IU; ++k) mine[u] |= x[u][k] == j;
-        }
-#pragma unroll
-        for (int u = 0; u < TU; ++u) {
-          const int e = min(e0 + u, n - 1);
-          const uint64_t bits = __ballot(mine[u] && (list[e] & 0xfffff) * kTileRows + lane < a.Nq);
-          if (lane == 0) rows[e] = bits;
-        }
+      const long long slot = ((long long)bhk * n_items + item) * run + r0 - rank0;
+      for (int e = threadIdx.x; e < n; e += 64 * NW) {
+        list[e] = w.tiles[slot + e];
+        rows[e] = w.rows[slot + e];
       }
       __syncthreads();
       // Their places: one after the other, a new step where the head (or the 65,536) ends.
@@ -254,6 +212,24 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void sparse_dkdv_kernel(c
       __syncthreads();
       return __builtin_amdgcn_readfirstlane(n_steps);
     }
+    if (wave == 0) {
+      int base = 0;
+      for (int i0 = 0; i0 < G * words && base < r0 + n; i0 += 64) {
+        const int i = i0 + lane, g = i / words, word = i - g * words;
+        uint64_t m = i < G * words ? w.map[(((long long)b * a.H + hk * G + g) * words + word) * a.nb + j] : 0;
+        const int mine = __popcll(m);
+        int upto = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+          const int x = __shfl_up(upto, d, 64);
+          if (lane >= d) upto += x;
+        }
+        for (int r = base + upto - mine - r0; m != 0 && r < n; ++r, m &= m - 1)
+          if (r >= 0) list[r] = g << 20 | (word * kMapTiles + __builtin_ctzll(m));
+        base += __shfl(upto, 63, 64);
+      }
+    }
+    __syncthreads();
     return 2 * n;
   };
 

@@ -150,6 +150,19 @@ def test_a_block_that_all_queries_choose(q_block):
     check(q, k, v, blocks, do, 128, q_block)
 
 
+@pytest.mark.parametrize("q_block", [1, 48, 63])
+def test_longer_sequences_that_choose_apart(q_block):
+    """Several words of the map, heads that share keys, samples of other lengths, tiles that hold two groups and more."""
+    q, k, v, do = inputs(2, 4, 2, 4300, 640, 72, 24)
+    check(q, k, v, choose(2, 4, -(-4300 // q_block), 10, 3, 25), do, 64, q_block, None, [640, 200])
+
+
+def test_more_blocks_in_a_tile_than_are_listed():
+    """A tile whose rows chose more than 128 blocks, of several heads, forward and backward."""
+    q, k, v, do = inputs(1, 2, 1, 200, 64 * 200, 64, 26)
+    check(q, k, v, choose(1, 2, 200, 200, 64, 27, 0), do, 64, 1)
+
+
 def test_longer_lists_than_fit():
     """A tile's rows that chose more blocks together than are listed at a time."""
     q, k, v, do = inputs(1, 1, 1, 70, 64 * 300, 8, 14)
