@@ -1253,6 +1253,11 @@ def _block_args(q, k, v, blocks, block, q_block, key_lens):
     return B, H, Hk, Nq, Nk, d, block, q_block, topk
 
 
+@functools.lru_cache(maxsize=1024)
+def _block_fwd_bytes(sizes):
+    return int(library().vitattn_block_fwd_workspace_bytes(*sizes))
+
+
 def block_fwd(q, k, v, blocks, block=128, q_block=1, scale=None, key_lens=None, out=None, save=True, workspace=None):
     """Attention of q (bf16 [B,H,Nq,d]) over chosen blocks of `block` keys (k, v [B,Hk,Nk,d],
     H a multiple of Hk): row i attends to the blocks blocks[b,h,i // q_block] (int32, from
@@ -1269,7 +1274,7 @@ def block_fwd(q, k, v, blocks, block=128, q_block=1, scale=None, key_lens=None, 
         o32 = torch.empty((B, H, Nq, d), dtype=torch.float32, device=q.device)
         lse = torch.empty((B, H, Nq), dtype=torch.float32, device=q.device)
     lib = library()
-    need = int(lib.vitattn_block_fwd_workspace_bytes(*sizes))
+    need = _block_fwd_bytes(sizes)
     ws = _diff_workspace(workspace, need, q.device) if need or workspace is not None else None
     _call(q, lib.vitattn_block_fwd, q.data_ptr(), _diff_strides(q), k.data_ptr(), _diff_strides(k), v.data_ptr(),
           _diff_strides(v), blocks.data_ptr(), _ptr(key_lens), o.data_ptr(), _diff_strides(o), _ptr(o32), _ptr(lse),

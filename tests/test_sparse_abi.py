@@ -199,7 +199,8 @@ SIZES = [
     (dict(d=20), UNSUP), (dict(d=168), UNSUP), (dict(block=32), UNSUP), (dict(block=100), UNSUP), (dict(block=2048), UNSUP),
     (dict(q_block=0), INVAL), (dict(topk=0), INVAL), (dict(topk=1025), UNSUP), (dict(Nk=16384 * 64 + 1), UNSUP), (dict(scale=0.0), INVAL),
     (dict(scale=float("nan")), INVAL), (dict(scale=-1.0), INVAL), (dict(H=4096, Hk=2), UNSUP), (dict(Nq=2 ** 26 + 1), INVAL),
-    (dict(B=2 ** 13, H=2 ** 11, Hk=2, Nq=1024), INVAL), (dict(sq=S(0, 0, 60)), INVAL), (dict(sk=S(0, 12, 64)), INVAL),
+    (dict(B=2 ** 13, H=2 ** 11, Hk=2, Nq=1024), INVAL), (dict(B=2 ** 10, H=2 ** 10, Hk=2 ** 10, Nq=300), INVAL),
+    (dict(sq=S(0, 0, 60)), INVAL), (dict(sk=S(0, 12, 64)), INVAL),
     (dict(sv=S(0, 0, 2 ** 31)), INVAL), (dict(Nk=2 ** 20, sk=S(0, 0, 1024)), INVAL), (dict(q=None), INVAL), (dict(k=None), INVAL),
     (dict(v=None), INVAL), (dict(blocks=None), INVAL)]
 
