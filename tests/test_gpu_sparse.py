@@ -157,6 +157,12 @@ def test_longer_sequences_that_choose_apart(q_block):
     check(q, k, v, choose(2, 4, -(-4300 // q_block), 10, 3, 25), do, 64, q_block, None, [640, 200])
 
 
+def test_rows_past_65536():
+    """Gathered rows are numbered within 65,536: steps that end there, of two heads that share keys."""
+    q, k, v, do = inputs(1, 2, 1, 140_001, 128, 8, 28)
+    check(q, k, v, choose(1, 2, 140_001, 3, 1, 29), do, 64, 1)
+
+
 def test_more_blocks_in_a_tile_than_are_listed():
     """A tile whose rows chose more than 128 blocks, of several heads, forward and backward."""
     q, k, v, do = inputs(1, 2, 1, 200, 64 * 200, 64, 26)
