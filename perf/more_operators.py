@@ -385,7 +385,7 @@ def _plain_gathered(s):
     v_ = v.reshape(-1, d)[rows.view(-1)].float().view(n, -1, d)
 
     def grouped(x):
-        return torch.nn.functional.pad(x.float(), (0, 0, 0, groups * qb - Nq)).reshape(n, qb, d)
+        return torch.nn.functional.pad(x.float(), (0, 0, 0, groups * qb - Nq)).view(n, qb, d)
 
     def whole(x):
         return x.view(B, H, groups * qb, d)[:, :, :Nq].to(torch.bfloat16)
