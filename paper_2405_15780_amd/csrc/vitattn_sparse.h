@@ -83,7 +83,8 @@ struct BlockList {
     __syncthreads();
     return __builtin_amdgcn_readfirstlane(total);
   }
-  // How many of build's `count` blocks lie before block x.
+  // How many of build's `count` blocks lie before block x. (Reads what the next build clears: a
+  // barrier belongs between the two, unless fill comes between them, which ends with one.)
   __device__ __forceinline__ int below(int x, int nb, int count) const {
     if (x >= nb) return count;
     return __builtin_amdgcn_readfirstlane(before[x >> 5] + __popc(bits[x >> 5] & ((1u << (x & 31)) - 1)));

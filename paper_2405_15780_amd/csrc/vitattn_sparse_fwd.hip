@@ -332,6 +332,9 @@ __global__ __launch_bounds__(64 * NW, MASKED && D > 96 ? 1 : D == 64 && (NW == 4
     const bool first = filter == ~0ULL;
     const int r0 = !SPLIT ? 0 : first ? (int)((long long)count * sp / n_split) : list.below(lo, a.nb, count);
     const int r1 = !SPLIT ? count : first ? (int)((long long)count * (sp + 1) / n_split) : list.below(hi, a.nb, count);
+    // A row that chose nothing of the split goes on to the next one's build, which clears what
+    // the other wave still reads here.
+    if (SPLIT && !first) __syncthreads();
     if constexpr (MASKED) {
       for (int r = r0; r < r1; r += list.kCap) {
         const int n = min(r1 - r, list.kCap);

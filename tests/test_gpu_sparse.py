@@ -217,6 +217,30 @@ def test_what_a_row_did_not_choose_does_not_reach_it(q_block, d, Nq):
         assert t.equal(got[n][0, 0, keys], want[n][0, 0, keys]), n
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Nq,block", [(2, 256), (5, 256), (64, 64), (65, 64), (256, 64)])
+def test_rows_that_chose_nothing_of_a_split(Nq, block, d):
+    """Few queries of one block each, split over workgroups: where a value is not finite the rows that share a tile are
+    gone over again, one after the other, most of them without a block in the split."""
+    print(f"case sparse redone rows Nq={Nq} block={block} d={d}", flush=True)
+    t = torch()
+    nb = 20
+    q, k, v, _ = inputs(2, 8, 8, Nq, nb * block, d, 23)
+    blocks = ((7 * t.arange(Nq, device="cuda", dtype=t.int32) + 3) % nb).expand(2, 8, Nq).unsqueeze(-1).contiguous()
+    want = run(q, k, v, blocks, None, block, 1)
+    vb = v.clone()
+    for j in (3, 11):
+        vb[:, :, j * block + 5] = float("inf")
+    hit = (blocks[0, 0, :, 0] == 3) | (blocks[0, 0, :, 0] == 11)
+    assert hit.any() and not hit.all()
+    for _ in range(4):
+        got = run(q, k, vb, blocks, None, block, 1)
+        for n in ("o", "o32"):
+            assert t.equal(got[n][:, :, ~hit], want[n][:, :, ~hit]), n
+            assert (got[n][:, :, hit] == float("inf")).all(), n
+        assert t.equal(got["lse"], want["lse"])
+
+
 @pytest.mark.parametrize("q_block", [1, 64])
 def test_large_and_masked_scores(q_block):
     """Scores of several hundred, and rows whose scores are all -inf."""
