@@ -519,8 +519,8 @@ int vitattn_rms_norm_bwd(const void* h, vitattn_strides sh, const void* w, const
  *     scale = max(max |y| / 448, 2^-126),  byte = y / scale rounded to the nearest even
  *
  * with the largest magnitude of the fp32 y over the row (group 0; scale [B*H*N]) or over
- * each `group` of columns (32, 64 or 128; scale [B*H*N][ceil(D / group)]), dense. NaN stays
- * NaN and does not count for a scale. Other groups: VITATTN_E_UNSUPPORTED.
+ * each `group` of columns (32, 64 or 128; scale [B*H*N][ceil(D / group)]), dense. The quotient
+ * of the fp32 y and the scale is rounded once. NaN stays NaN and does not count for a scale. Other groups: VITATTN_E_UNSUPPORTED.
  */
 int vitattn_rms_norm_fp8(const void* x, vitattn_strides sx, const void* residual, vitattn_strides sr, const void* w,
                          void* h, vitattn_strides sh, void* y, vitattn_strides sy, float* scale, int group, int B,

@@ -7,15 +7,15 @@
 // Without a residual h is x. What is normalised is h as it is stored: the backward
 // reads that, and the call gives the bits of the addition and the norm one after the
 // other. The output is of x's type, or e4m3 with fp32 scales of a row or of groups of
-// its columns: s = max(max |y| / 448, 2^-126), y / s rounded to the nearest even; the
-// largest magnitude is of the fp32 y, so that y is rounded once.
+// its columns: s = max(max |y| / 448, 2^-126), y / s rounded once, to the nearest even, of
+// the fp32 y, whose largest magnitude it is.
 //
 // Bound by HBM: x and the residual are read once and h and y written once; a row stays
 // in registers, in the residual's type, from the sum of squares to the output. Sums
 // and r are fp32. L lanes share a row as in vitattn_norm.hip; for groups of columns L
 // is rounded up so that a group's lanes are neighbours and its maximum a few
 // exchanges. 32,768 rows of 1,024 bf16 with residual and dropout: 53 us, 5.05 TB/s;
-// 32,768 of 2,048 to e4m3 with scales of 128 columns: 100 us, 4.7 TB/s.
+// 32,768 of 2,048 to e4m3 with scales of 128 columns: 109 us, 4.3 TB/s.
 #include "vitattn_rms.h"
 
 namespace vitattn {
@@ -53,15 +53,56 @@ __device__ __forceinline__ float row_max(const Place<BLOCK>& at, float x, float*
   return x;
 }
 
-// V values as e4m3 bytes, n of them stored
+// V values as e4m3 bytes
 template <int V>
-__device__ __forceinline__ void store_e4m3(uint8_t* p, const float (&v)[V], int n) {
-  uint32_t w[V / 4];
+__device__ __forceinline__ void to_e4m3(const float (&v)[V], uint32_t (&w)[V / 4]) {
 #pragma unroll
   for (int i = 0; i < V / 4; ++i) {
     int x = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i], v[4 * i + 1], 0, false);
     w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2], v[4 * i + 3], x, true);
   }
+}
+
+// The bytes of y / s, rounded once. Products with a reciprocal that is 2^-21 too small and one
+// that is too large (rcp is within 2^-23, the products' roundings are 2^-24) lie on both sides
+// of the quotient: where they give the same bytes, so does it. Where they do not it is near the
+// middle between two bytes, and goes to fp32 with its last bit set if it is not exact
+// (rounded to odd), so that the rounding to e4m3 is the only one. The residuals
+// fma(-q, s, |y|) are exact (q is within two fp32 steps, scales below 2^-64 are taken 2^96
+// times), their sign is the quotient's place beside q. 2 x 16,384 rows of 2,048 bf16 (groups of
+// 128, one element in 2,500 near a middle): 109 us; 116 with every quotient rounded to odd, and
+// 103 for a product with the reciprocal, which beside a middle falls on either side of it.
+template <int V>
+__device__ __forceinline__ void quotient_bytes(const float (&y)[V], float scale, uint32_t (&w)[V / 4]) {
+  const float back = __builtin_amdgcn_rcpf(scale), less = __builtin_fmaf(back, -0x1p-21f, back), more = __builtin_fmaf(back, 0x1p-21f, back);
+  float v[V];
+  uint32_t other[V / 4];
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = y[e] * less;
+  to_e4m3<V>(v, w);
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = y[e] * more;
+  to_e4m3<V>(v, other);
+  uint32_t differ = 0;
+#pragma unroll
+  for (int i = 0; i < V / 4; ++i) differ |= w[i] ^ other[i];
+  if (differ == 0) return;
+  const float up = scale < 0x1p-64f ? 0x1p96f : 1.f, s = scale * up, inv = __builtin_amdgcn_rcpf(s);
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    const float x = fabsf(y[e]) * up;
+    float q = x * inv;
+    q = __builtin_fmaf(__builtin_fmaf(-q, s, x), inv, q);
+    const float r = __builtin_fmaf(-q, s, x);
+    const int odd = (__float_as_int(q) + (__float_as_int(r) >> 31)) | 1;
+    v[e] = copysignf(r < 0.f || r > 0.f ? __int_as_float(odd) : q, y[e]);
+  }
+  to_e4m3<V>(v, w);
+}
+
+// V bytes, n of them stored
+template <int V>
+__device__ __forceinline__ void store_bytes(uint8_t* p, const uint32_t (&w)[V / 4], int n) {
   typedef uint32_t words __attribute__((ext_vector_type(V / 4), aligned(1)));
   if (n >= V) {
     words o;
@@ -199,11 +240,13 @@ __global__ __launch_bounds__(kThreads) void rms_fwd_kernel(const RmsArgs a) {
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
         const int c = (lane + i * L) * V, n = columns_of<V>(a.D, c);
-        const float scale = fmaxf(top[i] / kE4M3Max, kLeastScale), back = 1.f / scale;
+        const float scale = fmaxf(top[i] / kE4M3Max, kLeastScale);
         float v[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = row[u].h[i].get(e) * rstd * w[i][e] * back;
-        store_e4m3<V>(y + c, v, n);
+        for (int e = 0; e < V; ++e) v[e] = row[u].h[i].get(e) * rstd * w[i][e];
+        uint32_t bytes[V / 4];
+        quotient_bytes<V>(v, scale, bytes);
+        store_bytes<V>(y + c, bytes, n);
         if (a.group ? n > 0 && lane % gl == 0 : i == 0 && lane == 0)
           a.scale[logical * groups + (a.group ? c / a.group : 0)] = scale;
       }

@@ -195,6 +195,45 @@ def test_eight_bits(dtype, rtype, D, group):
     assert np.abs(np64(y.float())).max() <= 448
 
 
+@pytest.mark.parametrize("D,group", [(64, None), (256, 32), (1024, 64), (2048, 128), (2048, None), (8192, 128), (8192, None)])
+@pytest.mark.parametrize("dtype,rtype", TYPES)
+def test_eight_bits_round_once(dtype, rtype, D, group):
+    """Rows of +-1, whose norm is 1, so that |y| is the weight: values on and beside the middle between two bytes go
+    where y / scale is, to the even one in the middle (y, scale and their products with a middle are exact in fp64)."""
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    print(f"case fp8 once D={D} group={group} {dtype} {rtype}", flush=True)
+    values = np.arange(127, dtype=np.uint8)  # magnitudes 0 .. 448 by their bytes
+    values = t.from_numpy(values).view(t.float8_e4m3fn).double().numpy()
+    middles = (values[1:] + values[:-1]) / 2
+    rng = np.random.default_rng(D)
+    G = group or D
+    w = np.zeros(D, dtype=np.float32)
+    for g in range(D // G):
+        # the largest of the group: any, powers of two (ties that are met), scales at and near the least one
+        top = np.float32([rng.uniform(0.5, 2) * 10.0 ** rng.integers(-30, 30), 448 * 2.0 ** rng.integers(-60, 60),
+                          448 * 2.0 ** -126 * rng.uniform(0.3, 8)][g % 3])
+        s = np.maximum(top / np.float32(448), np.float32(2.0 ** -126))
+        x = (rng.choice(middles, G) * float(s)).astype(np.float32)
+        for _ in range(3):  # up to three steps beside the nearest
+            x = np.where(rng.random(G) < 0.3, np.nextafter(x, rng.choice(np.float32([0, np.inf]), G)), x)
+        w[g * G:(g + 1) * G] = np.minimum(x, top)
+        w[g * G + rng.integers(G)] = top
+    sign = t.from_numpy(rng.choice([-1.0, 1.0], (5, D))).cuda()
+    x, res = t.zeros((5, D), dtype=getattr(t, dtype), device="cuda"), sign.to(getattr(t, rtype))
+    assert (va.rms_norm_fwd(x, None, res, 0.0)[2] == 1).all()
+    y, scale, _ = va.rms_norm_fp8(x, t.from_numpy(w).cuda(), res, 0.0, group)
+    want = np.maximum(w.reshape(-1, G).max(1) / np.float32(448), np.float32(2.0 ** -126))
+    assert np.array_equal(scale.cpu().numpy().reshape(5, -1), np.tile(want, (5, 1)))
+    edge = middles * want.astype(np.float64).repeat(G)[:, None]
+    above, met = (w[:, None] > edge).sum(1), (w[:, None] == edge).any(1)
+    byte = above + (met & (above % 2 == 1))
+    got = y.view(t.uint8).cpu().numpy()
+    assert np.array_equal(got & 127, np.tile(byte, (5, 1))), int(((got & 127) != byte).sum())
+    assert np.array_equal(got >> 7, (sign < 0).cpu().numpy().astype(np.uint8))
+
+
 def test_eight_bits_of_other_layouts():
     import paper_2405_15780_amd as va
 
