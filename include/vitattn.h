@@ -670,8 +670,10 @@ int vitattn_block_select(const void* q, vitattn_strides sq, const void* means, c
  * and the backward as for vitattn_bwd, dK and dV summed over the heads that share them.
  * Numbers outside 0 .. nb - 1 stand for no block, a block given twice counts once, and the
  * order does not matter. A row without keys has O = 0, LSE = -inf and no gradients; so has a
- * row whose scores are all -inf. Keys that a row does not attend to do not reach it, also
- * where they are not finite.
+ * row whose scores are all -inf, of finite q, k and v (sums that overflow). Where infinite
+ * elements make scores -inf, O and LSE are those of the other keys, but gradients of the rows
+ * and keys that hold the elements, and of those that attend to each other with them, may be
+ * NaN. Keys that a row does not attend to do not reach it, also where they are not finite.
  *   q, o, dout, dq : bf16 [B][H][Nq][d]; k, v, dk, dv: bf16 [B][Hk][Nk][d]; strides as for
  *                    vitattn_fwd_strided, (rows + 1280) * row * 2 below 2^31.
  *   blocks         : int32, dense, from vitattn_block_select or any other choice.

@@ -5,7 +5,8 @@
 // beside the exponentials of step j, then dV += P(j)^T dO(j) beside dS(j), then
 // dK += dS(j)^T Q(j). Blocks of 32 queries arrive in a ring of four slots, three steps
 // ahead. Steps past the last read zeros: P is 1 there, and dO and Q are zero; so do the
-// places that a step of gathered rows (MASKED) leaves empty.
+// places that a step of gathered rows (MASKED) leaves empty. (Of a key with an infinite
+// element P is NaN there, as dK and dV of that key then are, and of no other.)
 #include "vitattn_sparse_bwd.h"
 
 namespace vitattn {

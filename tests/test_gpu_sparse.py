@@ -254,6 +254,59 @@ def test_large_and_masked_scores(q_block):
     assert t.isfinite(r["o32"]).all()
 
 
+@pytest.mark.parametrize("Nq", [32, 64, 130, 257])
+@pytest.mark.parametrize("q_block", [1, 64])
+def test_rows_whose_scores_overflow_have_no_gradients(q_block, Nq):
+    """Finite operands whose scores are all -inf: of every row (steps of the key side in fours and not), and of every
+    other group, whose keys have the gradients of the groups between."""
+    t = torch()
+    print(f"case sparse overflow q_block={q_block} Nq={Nq}", flush=True)
+    q, k, v, do = inputs(1, 2, 1, Nq, 300, 64, 33)
+    groups = -(-Nq // q_block)
+    blocks = choose(1, 2, groups, 5, 3, 34, 0)
+    k[..., 0], q[..., 0] = -3e38, 3e38
+    r = run(q, k, v, blocks, do, 64, q_block)
+    assert (r["lse"] == -np.inf).all() and not any(r[n].any() for n in ("o", "o32", "dq", "dk", "dv"))
+    none = t.arange(Nq, device="cuda") // q_block % 2 == 0
+    q[:, :, ~none, 0] = 0.0
+    got = run(q, k, v, blocks, do, 64, q_block)
+    mask = os_.allowed(blocks.cpu().numpy(), Nq, 300, 64, q_block)
+    mask[:, :, none.cpu().numpy()] = False
+    want = os_.block_attention(np64(q), np64(k), np64(v), mask, 0.125, np64(do))
+    for n in ("o", "o32", "lse", "dk", "dv"):
+        close(got[n], want[n], want[n + "_off"], n)
+    close(got["dq"][..., 1:], want["dq"][..., 1:], want["dq_off"][..., 1:], "dq")  # (column 0 meets the -3e38)
+    assert not got["dq"][:, :, none].any()
+
+
+@pytest.mark.parametrize("q_block", [1, 64])
+@pytest.mark.parametrize("Nq", [64, 150])
+def test_an_infinite_key_that_no_row_can_see(q_block, Nq):
+    """A key whose scores are -inf by an infinite element: outputs, and the gradients of the other keys and of rows that
+    did not choose its block, are those without it."""
+    t = torch()
+    print(f"case sparse infinite key q_block={q_block} Nq={Nq}", flush=True)
+    q, k, v, do = inputs(1, 2, 1, Nq, 300, 64, 35)
+    blocks = choose(1, 2, -(-Nq // q_block), 5, 3, 36, 0)
+    blocks[:, 0, 0] = t.tensor([1, 3, 1], device="cuda")
+    q[..., 0], k[..., 100, 0] = 1.0, -float("inf")
+    got = run(q, k, v, blocks, do, 64, q_block)
+    mask = os_.allowed(blocks.cpu().numpy(), Nq, 300, 64, q_block)
+    met = mask[..., 100].copy()
+    assert met.any()
+    mask[..., 100] = False
+    other = np.arange(300) != 100
+    kk = k.clone()
+    kk[..., 100, 0] = 0.0
+    want = os_.block_attention(np64(q), np64(kk), np64(v), mask, 0.125, np64(do))
+    for n in ("o", "o32", "lse"):
+        close(got[n], want[n], want[n + "_off"], n)
+    for n in ("dk", "dv"):
+        close(got[n][:, :, other], want[n][:, :, other], want[n + "_off"][:, :, other], n)
+    at = t.from_numpy(~met).cuda()
+    close(got["dq"][at], want["dq"][~met], want["dq_off"][~met], "dq")
+
+
 @pytest.mark.parametrize("q_block", [1, 64, 128])
 def test_layouts(q_block):
     """Sequence-major operands, a fused tensor's views, rows with a pitch; outputs in place of a buffer's part."""
