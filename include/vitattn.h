@@ -459,8 +459,8 @@ typedef struct vitattn_dropout_spec {
  * y = residual + dropout(x), or dropout(x) without a residual, of B*H*N rows of D
  * elements; the gradient of x is the same call on the gradient of y, without a
  * residual. A dropped element adds nothing, whatever it holds.
- *   x        : of `type`; residual (or null) and y of residual_type: type or fp32 (type
- *              without a residual). Rows at any element strides >= 0, the D elements of a
+ *   x        : of `type`; residual (or null) and y of residual_type: type or fp32; without a
+ *              residual type, or of an fp32 x also a 16-bit type. Rows at any element strides >= 0, the D elements of a
  *              row contiguous, no alignment beyond the element's. y must not overlap
  *              itself, and may be x or the residual (the same type and strides).
  *   sizes    : B*H*N below 2^31 - 2^22, B*H*N*ceil(D/8) below 2^34 - 2^14.

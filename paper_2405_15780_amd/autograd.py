@@ -119,21 +119,23 @@ class _Dropout:
 
             class Dropout(torch.autograd.Function):
                 @staticmethod
-                def forward(ctx, x, p, rng, residual):
+                def forward(ctx, x, p, rng, residual, dtype):
                     _save_rng(ctx, p, rng)
                     ctx.x_dtype = x.dtype
-                    return _b.dropout_fwd(x, p, rng, residual)
+                    return _b.dropout_fwd(x, p, rng, residual, dtype=dtype)
 
                 @staticmethod
                 def backward(ctx, dy):
                     # the same mask on the gradient, itself differentiable
                     dx = dres = None
                     if ctx.needs_input_grad[0]:
-                        # (of an fp32 residual's gradient in fp32, rounded once at the end)
-                        dx = Dropout.apply(_b.plain_memory(dy), ctx.p, _saved_rng(ctx), None).to(ctx.x_dtype)
+                        # (an fp32 residual's gradient is rounded once to x's type; that step's own
+                        # gradient is of fp32 again)
+                        g = _b.plain_memory(dy) if ctx.x_dtype != torch.float32 else _b.plain_memory(dy.float())
+                        dx = Dropout.apply(g, ctx.p, _saved_rng(ctx), None, ctx.x_dtype)
                     if ctx.needs_input_grad[3]:
                         dres = dy
-                    return dx, None, None, dres
+                    return dx, None, None, dres, None
 
             cls._fn = Dropout
         return cls._fn
@@ -159,7 +161,7 @@ def dropout(x, p, rng, residual=None):
     device; one of each call's own."""
     if not _wants_grad(x, residual):
         return _b.dropout_fwd(x, p, rng, residual)
-    return _Dropout.get().apply(x, p, rng, residual)
+    return _Dropout.get().apply(x, p, rng, residual, None)
 
 
 class _RmsNorm:

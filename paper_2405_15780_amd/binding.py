@@ -882,19 +882,25 @@ def _residual_of(x, residual):
     return code, _type_codes()[residual.dtype]
 
 
-def dropout_fwd(x, p, rng, residual=None, out=None):
+def dropout_fwd(x, p, rng, residual=None, out=None, dtype=None):
     """residual + dropout(x) (or dropout(x)): elements of x (bf16, fp16 or fp32, any
     strides with the last dim contiguous) are dropped with probability p (in steps of
     1/65536) and the others multiplied with 1/(1 - p). rng: (seed, offset), or an int64
     tensor of both on the device, which is read when the kernel runs. The mask goes by
     rng and an element's place alone and is not stored: the gradient of x is
     dropout_fwd(dy, p, rng). residual: x's shape, x's type or fp32; the output has its
-    type. out: the tensor to write, may be x or the residual."""
+    type. out: the tensor to write, may be x or the residual. dtype: the output's (bf16 or
+    fp16) of an fp32 x without a residual, rounded once."""
     code, rcode = _residual_of(x, residual)
+    y_dtype = x.dtype if residual is None else residual.dtype
+    if dtype is not None and dtype != y_dtype:
+        if residual is not None or code != VITATTN_FP32 or dtype not in _type_codes():
+            raise TypeError("dtype must be the output's type, or bf16 or fp16 of an fp32 x without a residual")
+        y_dtype, rcode = dtype, _type_codes()[dtype]
     spec = _rng(p, rng, x.device) or DropoutSpec(0, 0, None, 0.0)
     x4 = _rows_of(x, "x")
     r4 = None if residual is None else _rows_of(residual, "residual")
-    y, y4 = _row_out(out, "out", x, x.dtype if residual is None else residual.dtype, x4)
+    y, y4 = _row_out(out, "out", x, y_dtype, x4)
     sizes, (sx, sr, sy) = _row_args(x4, r4, y4)
     _call(x, library().vitattn_dropout, x4.data_ptr(), sx, _ptr(r4), sr, y4.data_ptr(), sy, *sizes, code, rcode, spec)
     if out is not None:

@@ -8,7 +8,8 @@
 // workgroup's first piece (64 bits, uniform) and one of a thread's small offset
 // (by a reciprocal that the host made). 4 x 8,192 rows of 4,096 bf16: 106 us, 5.05 TB/s
 // of the 5.10 that a copy reaches; 16 x 20,001 rows of 72 fp32 read sequence-major, with a
-// residual: 55 us, 5.0 TB/s, and 35 without.
+// residual: 55 us, 5.0 TB/s, and 35 without. An fp32 gradient is rounded to a 16-bit branch's
+// type as it is stored: 4 x 8,192 rows of 4,096 to bf16 156 us, 5.15 TB/s (337 with a cast behind).
 #include "vitattn_random.h"
 
 namespace vitattn {
@@ -54,7 +55,10 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const DropoutArgs
     const u32x4 w = drop.words(eighth[u], logical[u]);
     float y[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = drop.add(w, e, x[u].get(e), ADD ? r[u].get(e) : 0.f);
+    for (int e = 0; e < 8; ++e) {
+      y[e] = drop.add(w, e, x[u].get(e), ADD ? r[u].get(e) : 0.f);
+      if constexpr (sizeof(R) < sizeof(T)) pin(y[e]);  // (else fp16's rounding is the product's, and not the fp32 result's)
+    }
     Span<R, 8> o;
     o.set(y);
     o.store(static_cast<R*>(a.y) + at_y[u], n[u]);
@@ -69,8 +73,12 @@ hipError_t go(DropoutArgs a) {
   while ((2LL << a.shift) < a.pieces) ++a.shift;
   a.recip = (uint32_t)(((1ULL << (32 + a.shift)) + a.pieces - 1) / a.pieces);
   const long long per = kDropThreads * kDropPieces, blocks = ((long long)a.rows * a.pieces + per - 1) / per;
-  if (a.residual) dropout_kernel<T, R, true><<<(unsigned)blocks, kDropThreads, 0, a.stream>>>(a);
-  else dropout_kernel<T, R, false><<<(unsigned)blocks, kDropThreads, 0, a.stream>>>(a);
+  if constexpr (sizeof(R) >= sizeof(T))
+    if (a.residual) {
+      dropout_kernel<T, R, true><<<(unsigned)blocks, kDropThreads, 0, a.stream>>>(a);
+      return hipGetLastError();
+    }
+  dropout_kernel<T, R, false><<<(unsigned)blocks, kDropThreads, 0, a.stream>>>(a);
   return hipGetLastError();
 }
 
@@ -80,7 +88,8 @@ hipError_t launch_dropout(const DropoutArgs& a) {
   switch (a.type) {
     case kBf16: return a.residual_type == kFp32 ? go<__bf16, float>(a) : go<__bf16, __bf16>(a);
     case kFp16: return a.residual_type == kFp32 ? go<_Float16, float>(a) : go<_Float16, _Float16>(a);
-    default: return go<float, float>(a);
+    default:
+      return a.residual_type == kBf16 ? go<float, __bf16>(a) : a.residual_type == kFp16 ? go<float, _Float16>(a) : go<float, float>(a);
   }
 }
 

@@ -237,9 +237,11 @@ int vitattn_dropout(const void* x, vitattn_strides sx, const void* residual, vit
     const int st = check_rows(B, H, N, D);
     if (st != VITATTN_OK) return st;
     const int size = elem_bytes(type), rsize = elem_bytes(residual_type);
-    if (size == 0 || (residual_type != type && residual_type != VITATTN_FP32)) return VITATTN_E_UNSUPPORTED;
+    // (fp32 rows without a residual to 16 bits: the gradient of a branch beside an fp32 residual)
+    const bool narrow = residual == nullptr && type == VITATTN_FP32 && rsize == 2;
+    if (size == 0 || (residual_type != type && residual_type != VITATTN_FP32 && !narrow)) return VITATTN_E_UNSUPPORTED;
     if (x == nullptr || y == nullptr || dropout == nullptr) return VITATTN_E_INVAL;
-    if (residual == nullptr && residual_type != type) return VITATTN_E_INVAL;
+    if (residual == nullptr && residual_type != type && !narrow) return VITATTN_E_INVAL;
     vitattn::DropoutArgs a = {};
     if (to_drop(dropout, a.drop) != VITATTN_OK) return VITATTN_E_INVAL;
     a.pieces = (int)(((long long)D + 7) / 8);

@@ -127,6 +127,51 @@ def test_autograd():
     assert t.isfinite(z.grad).all()
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("D", [1, 5, 8, 13, 72, 1032])
+def test_a_wider_gradient_is_rounded_in_the_kernel(dtype, D):
+    """fp32 rows to 16 bits: the bits of the fp32 result rounded, in other layouts too."""
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    dt = getattr(t, dtype)
+    g = make((3, 4, 17, D), "float32", D)
+    want = va.dropout_fwd(g, 0.3, (1, D)).to(dt)
+    assert t.equal(va.dropout_fwd(g, 0.3, (1, D), dtype=dt), want)
+    other = g.transpose(1, 2).contiguous().transpose(1, 2)
+    out = t.full((3, 4, 17, D + 3), 7.0, dtype=dt, device="cuda")
+    assert t.equal(va.dropout_fwd(other, 0.3, (1, D), dtype=dt), want)
+    va.dropout_fwd(other, 0.3, (1, D), out=out[..., 1:1 + D], dtype=dt)
+    assert t.equal(out[..., 1:1 + D], want) and (out[..., 0] == 7).all() and (out[..., 1 + D:] == 7).all()
+    assert t.equal(va.dropout_fwd(g, 0.3, (1, D), dtype=t.float32).to(dt), want)
+    for call in (lambda: va.dropout_fwd(g, 0.3, (1, 2), g, dtype=dt), lambda: va.dropout_fwd(g.to(dt), 0.3, (1, 2), dtype=t.float32),
+                 lambda: va.dropout_fwd(g, 0.3, (1, 2), dtype=t.float64), lambda: va.dropout_fwd(g, 0.3, (1, 2), out=want)):
+        with pytest.raises(TypeError):
+            call()
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_a_branch_beside_an_fp32_residual(dtype):
+    """The branch's gradient is written in its own type, with no fp32 tensor in between; its own gradient is fp32."""
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    n = 1 << 22
+    x, res, g = make((n // 1024, 1024), dtype, 1), make((n // 1024, 1024), "float32", 2), make((n // 1024, 1024), "float32", 3)
+    y = va.dropout(x.requires_grad_(), 0.3, (5, 6), res)
+    t.cuda.synchronize()
+    t.cuda.reset_peak_memory_stats()
+    before = t.cuda.memory_allocated()
+    (dx,) = t.autograd.grad(y, x, g)
+    assert dx.dtype == x.dtype and t.cuda.max_memory_allocated() - before < 3 * n
+    assert t.equal(dx, va.dropout_fwd(g, 0.3, (5, 6)).to(x.dtype))
+    h = g.clone().requires_grad_()
+    (dx,) = t.autograd.grad(va.dropout(x, 0.3, (5, 6), res), x, h, create_graph=True)
+    u = make((n // 1024, 1024), dtype, 4)
+    (dh,) = t.autograd.grad(dx, h, u)
+    assert dh.dtype == t.float32 and t.equal(dh, va.dropout_fwd(u.float(), 0.3, (5, 6)))
+
+
 def test_graph_draws_new_masks():
     """A captured call reads its state when it is replayed."""
     import paper_2405_15780_amd as va

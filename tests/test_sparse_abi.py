@@ -130,6 +130,18 @@ def test_dropout_refusals(o, want):
     dropout(Bufs(), want, **o)
 
 
+@pytest.mark.parametrize("rtype", [BF16, FP16])
+def test_dropout_to_16_bits(rtype):
+    """fp32 rows without a residual may be rounded to 16 bits; what is checked of other calls is checked of these."""
+    dropout(Bufs(), INVAL, res=None, type=FP32, rtype=rtype, x=None)
+    dropout(Bufs(), INVAL, res=None, type=FP32, rtype=rtype, sy=S(256, 128, 16))
+    dropout(Bufs(), UNSUP, type=FP32, rtype=rtype)  # beside a residual
+    dropout(Bufs(), UNSUP, res=None, type=BF16, rtype=FP16)
+    dropout(Bufs(), UNSUP, res=None, type=FP32, rtype=3)
+    b = Bufs()
+    dropout(b, INVAL, res=None, type=FP32, rtype=rtype, y=b[0])  # another type in the input's place
+
+
 def test_dropout_overlap():
     b = Bufs()
     dropout(b, INVAL, y=b[0] + 64)
