@@ -366,8 +366,12 @@ template <int KT>
 hipError_t go(const SelectArgs& a) {
   const dim3 grid((a.groups + kTile - 1) / kTile, a.H, a.B);
   const int per_key = a.H / a.Hk;
-  // (a few queries: more waves read the means at once)
-  if (a.groups <= kTile && a.nb > 256 && a.nb <= 1024) select_kernel<16, KT, 16, false><<<grid, 1024, 0, a.stream>>>(a, per_key);
+  // A few groups (one workgroup a head): more waves read the means at once. 8 heads of 128, 1
+  // and 16 groups: 768 blocks in 7.7 and 15.4 us with sixteen waves, 9.5 and 17.7 with four;
+  // 1,024 in 8.2 and 15.8 (10.2 and 18.2). Not of up to 512 blocks (512: 7.6 and 14.1 with
+  // sixteen, 7.3 and 12.2 with four) nor of more than 1,024 (1,025: 12.8 and 27.5 with sixteen,
+  // 11.3 and 25.3 with eight; 2,048: 15.4 and 31.3, 13.9 and 28.9).
+  if (a.groups <= kTile && a.nb > 512 && a.nb <= 1024) select_kernel<16, KT, 16, false><<<grid, 1024, 0, a.stream>>>(a, per_key);
   else if (a.nb <= 256) select_kernel<4, KT, 4, false><<<grid, 256, 0, a.stream>>>(a, per_key);
   else if (a.nb <= 512) select_kernel<8, KT, 4, false><<<grid, 256, 0, a.stream>>>(a, per_key);
   else if (a.nb <= 1024) select_kernel<16, KT, 4, false><<<grid, 256, 0, a.stream>>>(a, per_key);
