@@ -55,10 +55,7 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const DropoutArgs
     const u32x4 w = drop.words(eighth[u], logical[u]);
     float y[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      y[e] = drop.add(w, e, x[u].get(e), ADD ? r[u].get(e) : 0.f);
-      if constexpr (sizeof(R) < sizeof(T)) pin(y[e]);  // (else fp16's rounding is the product's, and not the fp32 result's)
-    }
+    for (int e = 0; e < 8; ++e) y[e] = drop.add<R>(w, e, x[u].get(e), ADD ? r[u].get(e) : 0.f);
     Span<R, 8> o;
     o.set(y);
     o.store(static_cast<R*>(a.y) + at_y[u], n[u]);

@@ -47,9 +47,14 @@ struct Dropout {
   __device__ __forceinline__ bool keeps(const u32x4& w, int e) const {
     return ((e & 1) ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu) >= threshold;
   }
-  // r + x of column e (0 .. 7) of those times up, or r whatever x is
+  // r + x of column e (0 .. 7) of those times up, or r whatever x is, to be rounded to O: an
+  // fp32 number in every kernel. (Left to itself the compiler rounds to fp16 in the operation,
+  // which is another number once in 200,000.)
+  template <typename O>
   __device__ __forceinline__ float add(const u32x4& w, int e, float x, float r) const {
-    return keeps(w, e) ? __builtin_fmaf(x, up, r) : r;
+    float y = keeps(w, e) ? __builtin_fmaf(x, up, r) : r;
+    if constexpr (sizeof(O) == 2) asm("" : "+v"(y));
+    return y;
   }
 };
 

@@ -34,10 +34,11 @@ struct PieceMask {
   u32x4 w;
   int first;
   __device__ __forceinline__ PieceMask(const Dropout& d, int c, uint32_t row) : w(d.words((uint32_t)c >> 3, row)), first(c & 7) {}
+  template <typename O>
   __device__ __forceinline__ float add(const Dropout& d, int e, float x, float r) const {
-    if constexpr (V == 8) return d.add(w, e, x, r);
+    if constexpr (V == 8) return d.add<O>(w, e, x, r);
     const u32x4 half = first ? u32x4{w[2], w[3], 0, 0} : u32x4{w[0], w[1], 0, 0};
-    return d.add(half, e, x, r);
+    return d.add<O>(half, e, x, r);
   }
 };
 

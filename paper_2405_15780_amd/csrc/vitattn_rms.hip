@@ -178,7 +178,7 @@ __global__ __launch_bounds__(kThreads) void rms_fwd_kernel(const RmsArgs a) {
         if (a.drop_on) {
           const PieceMask<V> mask(drop, (lane + i * L) * V, (uint32_t)logical);
 #pragma unroll
-          for (int e = 0; e < V; ++e) v[e] = mask.add(drop, e, row[u].x[i].get(e), row[u].h[i].get(e));
+          for (int e = 0; e < V; ++e) v[e] = mask.template add<R>(drop, e, row[u].x[i].get(e), row[u].h[i].get(e));
         } else {
 #pragma unroll
           for (int e = 0; e < V; ++e) v[e] = row[u].x[i].get(e) + row[u].h[i].get(e);

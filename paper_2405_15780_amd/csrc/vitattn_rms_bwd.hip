@@ -120,7 +120,7 @@ __global__ __launch_bounds__(kThreads) void rms_bwd_kernel(const RmsArgs a) {
         if (a.drop_on) {
           const PieceMask<V> mask(drop, c, logical);
 #pragma unroll
-          for (int e = 0; e < V; ++e) v[e] = mask.add(drop, e, v[e], 0.f);
+          for (int e = 0; e < V; ++e) v[e] = mask.template add<T>(drop, e, v[e], 0.f);
         }
         Span<T, V> o;
         o.set(v);

@@ -172,6 +172,29 @@ def test_a_branch_beside_an_fp32_residual(dtype):
     assert dh.dtype == t.float32 and t.equal(dh, va.dropout_fwd(u.float(), 0.3, (5, 6)))
 
 
+@pytest.mark.parametrize("dtype,rtype", TYPES)
+def test_one_operation_and_one_rounding_everywhere(dtype, rtype):
+    """residual + x / (1 - p) is an fp32 number, rounded to the output's type: the same bits from dropout, as the norm's
+    h, and as its dx."""
+    import paper_2405_15780_amd as va
+
+    t = torch()
+    p, rng = 0.3, (5, 6)
+    up = np.float32(65536 / (65536 - round(65536 * p)))
+    for D in (1024, 1537, 5000):
+        x, res, dy = make((2048, D), dtype, D), make((2048, D), rtype, D + 1), make((2048, D), dtype, D + 2)
+        keep = va.dropout_fwd(t.ones(x.shape, device="cuda"), p, rng) != 0
+        y = va.dropout_fwd(x, p, rng, res)
+        _, h, rstd = va.rms_norm_fwd(x, None, res, 1e-6, p, rng)
+        assert t.equal(y, h)
+        # (fp64 holds the sum to far below an fp32 step's half)
+        want = t.where(keep, (x.double() * float(up) + res.double()).float(), res.float()).to(res.dtype)
+        assert t.equal(y, want)
+        if rtype == "float32":
+            dx, dres, _ = va.rms_norm_bwd(h, None, rstd, dy, res, p, rng)
+            assert t.equal(dx, va.dropout_fwd(dres, p, rng, dtype=x.dtype))
+
+
 def test_graph_draws_new_masks():
     """A captured call reads its state when it is replayed."""
     import paper_2405_15780_amd as va
