@@ -6,8 +6,8 @@
 // eight elements. A thread takes eight columns of a row, several of them in turn,
 // neighbours side by side; a row's index and column come from one division of the
 // workgroup's first piece (64 bits, uniform) and one of a thread's small offset
-// (by a reciprocal that the host made). 4 x 8,192 rows of 4,096 bf16: 106 us, 5.05 TB/s
-// of the 5.10 that a copy reaches; 16 x 20,001 rows of 72 fp32 read sequence-major, with a
+// (by a reciprocal that the host made). 4 x 8,192 rows of 4,096 bf16: 104 us, 5.2 TB/s
+// (a copy reaches 5.10); 16 x 20,001 rows of 72 fp32 read sequence-major, with a
 // residual: 55 us, 5.0 TB/s, and 35 without. An fp32 gradient is rounded to a 16-bit branch's
 // type as it is stored: 4 x 8,192 rows of 4,096 to bf16 156 us, 5.15 TB/s (337 with a cast behind).
 #include "vitattn_random.h"

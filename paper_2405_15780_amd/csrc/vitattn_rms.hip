@@ -7,8 +7,8 @@
 // Without a residual h is x. What is normalised is h as it is stored: the backward
 // reads that, and the call gives the bits of the addition and the norm one after the
 // other. The output is of x's type, or e4m3 with fp32 scales of a row or of groups of
-// its columns: s = max(max |y| / 448, 2^-126), y / s rounded once, to the nearest even, of
-// the fp32 y, whose largest magnitude it is.
+// its columns: s = max(max |y| / 448, 2^-126) of the fp32 y, and y / s rounded once, to the
+// nearest even.
 //
 // Bound by HBM: x and the residual are read once and h and y written once; a row stays
 // in registers, in the residual's type, from the sum of squares to the output. Sums
