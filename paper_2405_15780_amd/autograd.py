@@ -339,8 +339,8 @@ def block_attention(q, k, v, blocks, block=128, q_block=1, scale=None, key_lens=
     [B,Hk,Nk,d] bf16, H a multiple of Hk; blocks int32 [B,H,ceil(Nq/q_block),topk], as
     block_select gives them (see binding.block_fwd); scale defaults to 1/sqrt(d). Returns o,
     bf16 [B,H,Nq,d]. P and dS are bf16 operands of the products, as in attention(): against fp64,
-    o is about 2.1e-3 off in norm (bf16 outputs alone: 1.7e-3), dk and dv 2.4e-3 to 2.7e-3, and dq
-    3.4e-3 to 3.9e-3 where keys share a mean."""
+    o is about 2.1e-3 off in norm (bf16 outputs alone: 1.7e-3), dk and dv 2.4e-3, and dq 3.4e-3
+    to 3.9e-3 where keys share a mean."""
     if not _wants_grad(q, k, v):
         return _b.block_fwd(q, k, v, blocks, block, q_block, scale, key_lens, save=False)[0]
     return _BlockAttention.get().apply(q, k, v, blocks, block, q_block, scale, key_lens)
